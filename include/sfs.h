@@ -328,6 +328,72 @@ int32_t sfs_linear(const void *d_A, int64_t lda, const void *d_B, int64_t ldb, v
 int32_t sfs_attention(const void *d_qk, const void *d_vt, void *d_out, int32_t B, int32_t S,
                       int32_t n_heads, int32_t head_dim, void *stream);
 
+/* ---- microscaled 4-bit numbers ------------------------------------------------------------------------- */
+
+/* Matrices and caches in the MX format with 4-bit elements.  32 consecutive values of a row (the contraction dimension) are a
+ * block; a block has one scale byte c, which stands for 2^(c - 127), and 32 codes e2m1: bit 3 the sign, bits 2..0 one of the
+ * magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Two codes share a byte, the lower column in the low nibble.  c = 255 makes every value
+ * of the block NaN.
+ *   Quantisation: with a = the largest magnitude of the block, c = min(hi, max(lo, floor(log2 a) - 2 + 127)) (lo when a = 0),
+ *   codes = x 2^(127 - c) rounded to nearest, ties to the even code, saturated at 6.  A block that holds a NaN or an infinity gets
+ *   c = 255 and codes of 0.  Matrices have lo = 0, hi = 254; caches lo = 65, hi = 192 (see sfs_cache4).
+ *   A matrix of `rows` x `cols` has ceil(cols / 32) blocks per row; columns behind the last are codes of 0.  Codes: row-major,
+ *   16 bytes per block, ld_codes BYTES between rows (a multiple of 16, base 16-byte aligned; bytes behind a row's blocks are not touched).
+ *   Scales: tiles of 128 rows x 4 blocks, 512 bytes each, so that the tensor core's scale operand is one straight copy: the byte of
+ *   block b of row r is at ((r / 128) * ceil(blocks / 4) + b / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4; the buffer
+ *   (16-byte aligned) has SFS_MX4_SCALE_BYTES(rows, cols) bytes, and its padding holds zeros. */
+#define SFS_MX4_BLOCK 32
+#define SFS_MX4_CODE_BYTES(cols) ((((int64_t)(cols) + 31) / 32) * 16)
+#define SFS_MX4_SCALE_BYTES(rows, cols) ((((int64_t)(rows) + 127) / 128) * (((int64_t)(cols) + 127) / 128) * 512)
+
+/* d_x [rows, cols] (bf16 or fp32 per in_dtype, SFS_LOGITS_*; ldx elements between rows) -> codes and scales, padding included. */
+int32_t sfs_mx4_quantize(const void *d_x, int64_t ldx, int32_t in_dtype, int32_t rows, int32_t cols,
+                         void *d_codes, int64_t ld_codes, void *d_scales, void *stream);
+/* The reverse: the values that codes and scales stand for, rounded to out_dtype (exact in fp32; in bf16 down to 2^-133). */
+int32_t sfs_mx4_dequantize(const void *d_codes, int64_t ld_codes, const void *d_scales, int32_t rows, int32_t cols,
+                           void *d_x, int64_t ldx, int32_t out_dtype, void *stream);
+
+/* C[M, N] = scale * A[M, K] * B[N, K]^T of two such matrices (lda, ldb bytes between rows of codes), block-scaled tensor-core
+ * products with fp32 accumulation, C bf16 (out_dtype 0) or fp32 (1) with ldc elements between rows: sfs_linear for 4-bit operands.
+ * Products of codes and scales are exact; sums are fp32.  Makes no allocation after the first call on a device; make that one
+ * before any stream capture. */
+int32_t sfs_linear_mx4(const void *d_A, int64_t lda, const void *d_A_scales, const void *d_B, int64_t ldb, const void *d_B_scales,
+                       void *d_C, int64_t ldc, int32_t M, int32_t N, int32_t K, int32_t out_dtype, float scale, void *stream);
+
+/* Keys and values of batch sequences of up to `capacity` tokens in the same format, blocks along the head dimension.  Slot
+ * b * capacity + j holds token j of sequence b: codes uint8 [batch * capacity, n_kv_heads, head_dim / 2], scales uint8
+ * [batch * capacity, n_kv_heads, head_dim / 32], for keys and for values, caller's device memory, 16-byte aligned.  head_dim 64
+ * or 128.  Scales lie between 65 and 192 (2^-62 .. 2^65: every value is then exact in bf16 after a common factor), larger values
+ * saturate and smaller ones lose bits to the fixed step; a scale above 192 reads as NaN. */
+typedef struct {
+    void *k_codes, *k_scales, *v_codes, *v_scales;
+    int32_t batch, capacity, n_kv_heads, head_dim;
+} sfs_cache4;
+
+/* Quantises n_rows tokens into the cache: row r of d_k and d_v ([n_rows, n_kv_heads * head_dim], bf16 or fp32 per in_dtype, ld_k and
+ * ld_v elements between rows; keys with rotary embedding applied) goes to slot d_slots[r], or to slot r when d_slots is NULL.  A row
+ * whose slot lies outside the cache (negative, say) is left out; of several rows with one slot the last counts. */
+int32_t sfs_cache4_store(const sfs_cache4 *cache, const void *d_k, int64_t ld_k, const void *d_v, int64_t ld_v, int32_t in_dtype,
+                         const int32_t *d_slots, int32_t n_rows, void *stream);
+/* Values of the cached tokens d_slots[r] (slot r when NULL) as rows of d_k and d_v, each optional; a row whose slot lies outside
+ * the cache is left as it was. */
+int32_t sfs_cache4_load(const sfs_cache4 *cache, const int32_t *d_slots, int32_t n_rows, void *d_k, int64_t ld_k,
+                        void *d_v, int64_t ld_v, int32_t out_dtype, void *stream);
+
+/* Attention of n_q query rows per sequence over the cache: row b * n_q + i of d_q [batch * n_q, n_heads * head_dim] (bf16, ld_q
+ * elements between rows, rotary embedding applied; n_heads a multiple of n_kv_heads, head h reads key head h / (n_heads / n_kv_heads))
+ * gives the same row of d_out (bf16, ld_out): softmax(q k^T / sqrt(head_dim)) v over the keys that it sees.  A row at position p sees
+ * key j of its own sequence when
+ *     j < length_b  and  (right < 0 or j <= p + right)  and  (left < 0 or j >= p - left or j < sinks).
+ * left = right = -1 is the bidirectional attention of the mask predictor, right = 0 a causal one, left = window and sinks > 0 a sliding
+ * window with first tokens that stay visible.  d_lengths int32 [batch] (clamped to [0, capacity]; NULL: capacity).  d_positions int32
+ * [batch * n_q], a row with a negative position is not computed and its output left as it was; NULL: row i is at length_b - n_q + i.
+ * A row that sees no key gets zeros.  Keys and values that no row sees may hold anything.  Scores, maxima, sums and outputs are fp32,
+ * probabilities are rounded to bf16 for their product with the values.  No workspace. */
+int32_t sfs_attention_cache4(const sfs_cache4 *cache, const void *d_q, int64_t ld_q, void *d_out, int64_t ld_out, int32_t n_heads,
+                             int32_t n_q, const int32_t *d_lengths, const int32_t *d_positions, int32_t left, int32_t right, int32_t sinks,
+                             void *stream);
+
 /* Synchronises `stream` and returns (then clears) the sticky device status word: SFS_OK, or SFS_ERR_TIMEOUT
  * if a kernel's bounded wait gave up since the last check. */
 int32_t sfs_check_device_status(void *stream);

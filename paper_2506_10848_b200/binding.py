@@ -87,6 +87,8 @@ _PROTOTYPES = {
     "sfs_check_device_status": "p", "sfs_attention": "pppiiiip", "sfs_model_create": "ppp", "sfs_model_destroy": "p",
     "sfs_session_create": "piip", "sfs_forward": "ppiippipip", "sfs_cache_enable": "pp", "sfs_cache_reset": "p", "sfs_cache_dump": "ppp",
     "sfs_forward_cached": "ppiiipppipipppp", "sfs_generate": "ppiiippppip", "sfs_generate_begin": "ppiiipp", "sfs_generate_steps": "pipipppp",
+    "sfs_mx4_quantize": "pliiiplpp", "sfs_mx4_dequantize": "plpiiplip", "sfs_linear_mx4": "plpplppliiiifp",
+    "sfs_cache4_store": "pplplipip", "sfs_cache4_load": "ppiplplip", "sfs_attention_cache4": "pplpliippiiip",
     "sfs_generate_end": "pppppp", "sfs_profile": "pippp", "sfs_select_static": "ipilppippiiippppppppp",
 }
 
@@ -176,6 +178,55 @@ def sfs_check_device_status(stream=None):
 def sfs_attention(qk, vt, out, B, S, n_heads, head_dim, stream=None):
     _check(lib().sfs_attention(_ptr(qk), _ptr(vt), _ptr(out), B, S, n_heads, head_dim,
                                _stream(stream)))
+
+
+MX4_BLOCK = 32
+
+
+def mx4_code_bytes(cols):
+    """Bytes of one row's codes."""
+    return (cols + 31) // 32 * 16
+
+
+def mx4_scale_bytes(rows, cols):
+    """Bytes of a matrix's scales, padding included."""
+    return (rows + 127) // 128 * ((cols + 127) // 128) * 512
+
+
+def sfs_mx4_quantize(x, ldx, in_dtype, rows, cols, codes, ld_codes, scales, stream=None):
+    _check(lib().sfs_mx4_quantize(_ptr(x), ldx, in_dtype, rows, cols, _ptr(codes), ld_codes, _ptr(scales), _stream(stream)))
+
+
+def sfs_mx4_dequantize(codes, ld_codes, scales, rows, cols, x, ldx, out_dtype, stream=None):
+    _check(lib().sfs_mx4_dequantize(_ptr(codes), ld_codes, _ptr(scales), rows, cols, _ptr(x), ldx, out_dtype, _stream(stream)))
+
+
+def sfs_linear_mx4(A, lda, A_scales, Bm, ldb, B_scales, C, ldc, M, N, K, out_dtype=0, scale=1.0, stream=None):
+    _check(lib().sfs_linear_mx4(_ptr(A), lda, _ptr(A_scales), _ptr(Bm), ldb, _ptr(B_scales), _ptr(C), ldc, M, N, K,
+                                out_dtype, scale, _stream(stream)))
+
+
+class Cache4(Structure):
+    """A 4-bit key / value cache in the caller's tensors, which the handle keeps alive."""
+    _fields_ = [(n, c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")] + \
+               [(n, c_int32) for n in ("batch", "capacity", "n_kv_heads", "head_dim")]
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, batch, capacity, n_kv_heads, head_dim):
+        super().__init__(*(_ptr(t) for t in (k_codes, k_scales, v_codes, v_scales)), batch, capacity, n_kv_heads, head_dim)
+        self._tensors = (k_codes, k_scales, v_codes, v_scales)
+
+
+def sfs_cache4_store(cache, k, ld_k, v, ld_v, in_dtype, slots, n_rows, stream=None):
+    _check(lib().sfs_cache4_store(byref(cache), _ptr(k), ld_k, _ptr(v), ld_v, in_dtype, _ptr(slots), n_rows, _stream(stream)))
+
+
+def sfs_cache4_load(cache, slots, n_rows, k, ld_k, v, ld_v, out_dtype, stream=None):
+    _check(lib().sfs_cache4_load(byref(cache), _ptr(slots), n_rows, _ptr(k), ld_k, _ptr(v), ld_v, out_dtype, _stream(stream)))
+
+
+def sfs_attention_cache4(cache, q, ld_q, out, ld_out, n_heads, n_q, lengths=None, positions=None, left=-1, right=-1, sinks=0, stream=None):
+    _check(lib().sfs_attention_cache4(byref(cache), _ptr(q), ld_q, _ptr(out), ld_out, n_heads, n_q, _ptr(lengths), _ptr(positions),
+                                      left, right, sinks, _stream(stream)))
 
 
 class Model:

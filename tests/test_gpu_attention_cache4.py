@@ -1,0 +1,242 @@
+"""Attention over a 4-bit cache against the plain 64-bit implementation, row by row within bounds taken from the arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+import mx4_reference as R
+from paper_2506_10848_b200 import binding as sfs
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+class Case:
+    """A cache filled with random codes (every slot, also those that no length covers) and queries."""
+
+    def __init__(self, batch, capacity, heads, kv, dim, n_q, seed=0, sharp=1.0, scale_span=2):
+        rng = np.random.default_rng(seed)
+        self.batch, self.capacity, self.heads, self.kv, self.dim, self.n_q = batch, capacity, heads, kv, dim, n_q
+        slots = batch * capacity
+        self.codes = [rng.integers(0, 16, size=(slots, kv, dim)).astype(np.uint8) for _ in range(2)]
+        self.scales = [(126 + rng.integers(-scale_span, scale_span + 1, size=(slots, kv, dim // 32))).astype(np.uint8) for _ in range(2)]
+        self.q = (torch.from_numpy(rng.normal(size=(batch * n_q, heads * dim)) * sharp)).to(torch.bfloat16)
+        self.rng = rng
+
+    def run(self, lengths=None, positions=None, left=-1, right=-1, sinks=0, ld_pad=0, stream=None):
+        c = sfs.Cache4(dev(R.pack(self.codes[0])), dev(self.scales[0]), dev(R.pack(self.codes[1])), dev(self.scales[1]), self.batch, self.capacity, self.kv, self.dim)
+        width = self.heads * self.dim
+        rows = self.batch * self.n_q
+        q = torch.full((rows, width + ld_pad), float("nan"), dtype=torch.bfloat16, device=DEV)
+        q[:, :width] = self.q.to(DEV)
+        out = torch.full((rows + 1, width + ld_pad), 77.0, dtype=torch.bfloat16, device=DEV)
+        n = None if lengths is None else dev(np.asarray(lengths, np.int32))
+        p = None if positions is None else dev(np.asarray(positions, np.int32))
+        sfs.sfs_attention_cache4(c, q, width + ld_pad, out, width + ld_pad, self.heads, self.n_q, n, p, left, right, sinks, stream=stream)
+        sfs.sfs_check_device_status(stream)
+        got = out.double().cpu().numpy()
+        assert (got[rows] == 77.0).all() and (got[:, width:] == 77.0).all()
+        return got[:rows, :width]
+
+    def check(self, lengths=None, positions=None, left=-1, right=-1, sinks=0, ld_pad=0):
+        got = self.run(lengths, positions, left, right, sinks, ld_pad)
+        k, v = (R.values(c, s, nan_above=192).reshape(self.batch, self.capacity, self.kv, self.dim) for c, s in zip(self.codes, self.scales))
+        q = self.q.double().numpy().reshape(self.batch, self.n_q, self.heads, self.dim)
+        got = got.reshape(self.batch, self.n_q, self.heads, self.dim)
+        for b in range(self.batch):
+            n = self.capacity if lengths is None else min(max(int(lengths[b]), 0), self.capacity)
+            at = [int(np.asarray(positions).reshape(self.batch, self.n_q)[b, i]) if positions is not None else n - self.n_q + i for i in range(self.n_q)]
+            computed = np.array([positions is None or p >= 0 for p in at])
+            mask = np.stack([R.seen(n, p, left, right, sinks) for p in at])
+            for h in range(self.heads):
+                g = h // (self.heads // self.kv)
+                want, bound = R.attention(q[b, :, h], k[b, :n, g], v[b, :n, g], mask)
+                bound = bound + 2.0 ** -8 * (np.abs(want) + bound)
+                with np.errstate(invalid="ignore"):
+                    fine = np.abs(got[b, :, h] - want) <= bound
+                fine |= np.isnan(want) & np.isnan(got[b, :, h])
+                fine[~computed] = got[b, ~computed, h] == 77.0
+                assert fine.all(), (b, h, np.argwhere(~fine)[:4], float(np.nanmax(np.abs(got[b, computed, h] - want[computed]) / np.maximum(bound[computed], 1e-300))))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("capacity", [1, 2, 7, 16, 31, 63, 64, 65, 127, 128, 129, 200, 500])
+def test_single_tokens_over_every_length(capacity, dim):
+    Case(2, capacity, 3, 3, dim, 1, seed=capacity).check()
+
+
+@pytest.mark.parametrize("n_q", [1, 2, 5, 15, 16, 17, 31, 33, 64, 65, 127, 128, 129, 200, 260])
+def test_query_counts(n_q):
+    Case(1, 300, 2, 2, 128, n_q, seed=n_q).check()
+    Case(2, 150, 1, 1, 64, n_q, seed=n_q).check(lengths=[150, 97])
+
+
+@pytest.mark.parametrize("heads,kv", [(1, 1), (4, 1), (6, 2), (8, 8), (10, 2), (16, 1), (24, 3), (40, 2), (7, 7)])
+@pytest.mark.parametrize("n_q", [1, 3, 40])
+def test_shared_key_heads(heads, kv, n_q):
+    Case(2, 100, heads, kv, 128 if kv % 2 else 64, n_q, seed=heads + n_q).check(lengths=[100, 41])
+
+
+@pytest.mark.parametrize("n_q", [1, 4, 70, 150])
+@pytest.mark.parametrize("left,right,sinks", [(0, 0, 0), (5, 5, 0), (16, -1, 3), (-1, 0, 0), (20, 0, 4), (0, 0, 1), (64, 64, 130), (-1, 7, 2), (1000, 1000, 5), (3, 200, 64)])
+def test_windows(left, right, sinks, n_q):
+    c = Case(2, 333, 2, 1, 64, n_q, seed=left + 3 * right + n_q)
+    c.check(left=left, right=right, sinks=sinks)
+    c.check(lengths=[333, 180], positions=c.rng.integers(0, 333, size=(2, n_q)), left=left, right=right, sinks=sinks)
+
+
+@pytest.mark.parametrize("n_q", [1, 3, 130])
+def test_rows_that_see_nothing_rows_left_out_and_lengths_out_of_range(n_q):
+    c = Case(4, 90, 2, 2, 128, n_q, seed=1)
+    pos = c.rng.integers(0, 90, size=(4, n_q))
+    pos[:, -1] = -1                                         # left as it was
+    pos[1, 0] = 2 ** 31 - 1
+    c.check(lengths=[0, 90, 1000, -5], positions=pos)
+    c.check(lengths=[0, 90, 1, 37], positions=pos, left=4, right=4)
+    c.check(lengths=[10, 0, 1, 37], left=2, right=0)       # positions below zero, derived from a length shorter than the queries
+
+
+@pytest.mark.parametrize("n_q", [1, 20, 140])
+def test_what_is_masked_may_hold_anything(n_q):
+    c = Case(2, 200, 2, 2, 128, n_q, seed=4)
+    lengths = np.array([120, 33])
+    for part in range(2):
+        s = c.scales[part].reshape(2, 200, 2, 4)
+        s[0, 120:], s[1, 33:] = 255, 255
+        s[0, 20:60, :, 1] = 255                             # behind the window, inside the length
+        s[1, 5:7, 0] = 193
+    pos = np.stack([np.full(n_q, 110), np.full(n_q, 30)])
+    c.check(lengths=lengths, positions=pos, left=40, right=30, sinks=2)
+    # and where some rows of a tile see it, those alone are NaN
+    pos = np.stack([np.arange(n_q) % 100 + 10, np.arange(n_q) % 30])
+    c.check(lengths=lengths, positions=pos, left=9, right=2, sinks=3)
+
+
+@pytest.mark.parametrize("sharp", [0.0, 30.0])
+def test_flat_and_peaked_scores(sharp):
+    for n_q in (1, 130):
+        Case(1, 257, 2, 2, 64, n_q, seed=2, sharp=sharp).check()
+
+
+def test_infinite_and_nan_queries_stay_in_their_rows():
+    for n_q in (4, 140):
+        c = Case(1, 70, 1, 1, 64, n_q, seed=3)
+        c.codes[0][:, :, 0] = 2                             # the first component of every key is positive
+        q = c.q.clone()
+        q[1, 0], q[2, 5] = float("inf"), float("nan")
+        c.q = q
+        got = c.run()
+        assert np.isnan(got[1]).all() and np.isnan(got[2]).all()
+        assert not np.isnan(np.delete(got, [1, 2], 0)).any()
+
+
+@pytest.mark.parametrize("n_q", [1, 130])
+def test_scales_over_their_whole_range(n_q):
+    c = Case(1, 120, 2, 2, 128, n_q, seed=8)
+    c.scales[1][:] = c.rng.integers(65, 193, size=c.scales[1].shape)                 # values of 2^-63 .. 6 2^65 side by side
+    c.scales[0][:] = 127 - 10
+    c.check()
+    c.q = (c.q.double() * 2.0 ** -60).to(torch.bfloat16)
+    c.scales[0][:] = 127 + 60
+    c.check()
+
+
+def test_strided_queries_and_repeatability():
+    for n_q in (1, 9, 150):
+        c = Case(3, 140, 4, 2, 128, n_q, seed=5)
+        c.check(lengths=[140, 3, 77], ld_pad=8)
+        assert np.array_equal(c.run(), c.run())
+
+
+def test_long_cache_with_offsets_beyond_32_bits():
+    """Code bytes of the last sequence lie behind 2^32."""
+    batch, capacity, kv, dim = 3, 1 << 17, 128, 128
+    slots = batch * capacity
+    if torch.cuda.mem_get_info()[0] < 10 * 2 ** 30:
+        pytest.skip("needs 10 GB of device memory")
+    z = lambda w: torch.zeros((slots, kv, w), dtype=torch.uint8, device=DEV)  # noqa: E731
+    kc, ks, vc, vs = z(dim // 2), z(dim // 32), z(dim // 2), z(dim // 32)
+    assert kc.numel() < 2 ** 32 and slots * kv * dim // 2 == 3 * 2 ** 30
+    c = sfs.Cache4(kc, ks, vc, vs, batch, capacity, kv, dim)
+    # a few tokens at the end of the last sequence, seen through a window
+    n, width = 40, kv * dim
+    x = torch.randn((n, 2 * width), generator=torch.Generator().manual_seed(0)).to(torch.bfloat16)
+    first = slots - n
+    sfs.sfs_cache4_store(c, x.to(DEV), 2 * width, x.to(DEV)[:, width:], 2 * width, 0, torch.arange(first, slots, dtype=torch.int32, device=DEV), n)
+    q = torch.randn((batch, width), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    out = torch.zeros((batch, width), dtype=torch.bfloat16, device=DEV)
+    sfs.sfs_attention_cache4(c, q.to(DEV), width, out, width, kv, 1, None, None, n - 1, 0, 0)
+    sfs.sfs_check_device_status()
+    kq, vq = (R.values(*R.quantize(t.double().numpy(), R.CACHE)).reshape(n, kv, dim) for t in (x[:, :width], x[:, width:]))
+    for h in (0, 77, 127):
+        want, bound = R.attention(q[2].double().numpy().reshape(kv, dim)[h:h + 1], kq[:, h], vq[:, h], np.ones((1, n), bool))
+        got = out[2].double().cpu().numpy().reshape(kv, dim)[h]
+        assert (np.abs(got - want[0]) <= bound[0] + 2.0 ** -8 * (np.abs(want[0]) + bound[0])).all(), h
+    assert (out[:2] == 0).all()                             # the other sequences hold zeros
+
+
+def test_a_layer_of_4_bit_operators_in_a_captured_graph():
+    """Projection, cache, attention and output projection as a program runs them, captured once and replayed: the values are those of the
+    plain implementation fed with the device's own projections."""
+    B, n, cap, H, dim = 2, 24, 64, 4, 64
+    d = H * dim
+    gen = torch.Generator().manual_seed(11)
+    rand = lambda *s: torch.randn(s, generator=gen)  # noqa: E731
+    w_qkv, w_o = (rand(3 * d, d) * 0.06).to(torch.bfloat16).to(DEV), (rand(d, d) * 0.06).to(torch.bfloat16).to(DEV)
+    u8 = lambda *s: torch.zeros(s, dtype=torch.uint8, device=DEV)  # noqa: E731
+
+    def weight(w):
+        codes, scales = u8(w.shape[0], w.shape[1] // 2), u8(sfs.mx4_scale_bytes(*w.shape))
+        sfs.sfs_mx4_quantize(w, w.shape[1], 0, w.shape[0], w.shape[1], codes, w.shape[1] // 2, scales)
+        return codes, scales
+    wq, wo = weight(w_qkv), weight(w_o)
+    c = sfs.Cache4(u8(B * cap, H, dim // 2), u8(B * cap, H, dim // 32), u8(B * cap, H, dim // 2), u8(B * cap, H, dim // 32), B, cap, H, dim)
+    x = torch.zeros((B * n, d), dtype=torch.bfloat16, device=DEV)
+    xc, xs = u8(B * n, d // 2), u8(sfs.mx4_scale_bytes(B * n, d))
+    qkv, att, y = (torch.zeros((B * n, w), dtype=torch.bfloat16, device=DEV) for w in (3 * d, d, d))
+    first = torch.zeros(1, dtype=torch.int32, device=DEV)
+    row = torch.arange(n, dtype=torch.int32, device=DEV)
+    slots, positions, lengths = (torch.zeros(s, dtype=torch.int32, device=DEV) for s in (B * n, B * n, B))
+
+    def step():
+        positions.copy_((first + row).repeat(B))
+        slots.copy_(positions + cap * torch.arange(B, dtype=torch.int32, device=DEV).repeat_interleave(n))
+        lengths.copy_((first + n).repeat(B))
+        sfs.sfs_mx4_quantize(x, d, 0, B * n, d, xc, d // 2, xs)
+        sfs.sfs_linear_mx4(xc, d // 2, xs, wq[0], d // 2, wq[1], qkv, 3 * d, B * n, 3 * d, d)
+        sfs.sfs_cache4_store(c, qkv[:, d:], 3 * d, qkv[:, 2 * d:], 3 * d, 0, slots, B * n)
+        sfs.sfs_attention_cache4(c, qkv, 3 * d, att, d, H, n, lengths, positions, 20, -1, 2)
+        sfs.sfs_mx4_quantize(att, d, 0, B * n, d, xc, d // 2, xs)
+        sfs.sfs_linear_mx4(xc, d // 2, xs, wo[0], d // 2, wo[1], y, d, B * n, d, d)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    keys, vals = np.zeros((B, cap, H, dim)), np.zeros((B, cap, H, dim))
+    wov = R.values(*R.quantize(w_o.double().cpu().numpy(), R.MATRIX))
+    for t in range(2):
+        x.copy_(rand(B * n, d).to(torch.bfloat16))
+        first.fill_(t * n)
+        graph.replay()
+        torch.cuda.synchronize()
+        now = qkv.double().cpu().numpy().reshape(B, n, 3, H, dim)
+        lo, hi = t * n, t * n + n
+        for to, part in ((keys, 1), (vals, 2)):
+            to[:, lo:hi] = R.values(*R.quantize(now[:, :, part].reshape(-1, d), R.CACHE)).reshape(B, n, H, dim)
+        got = att.double().cpu().numpy().reshape(B, n, H, dim)
+        mask = np.stack([R.seen(hi, lo + i, 20, -1, 2) for i in range(n)])
+        for b in range(B):
+            for h in range(H):
+                want, bound = R.attention(now[b, :, 0, h], keys[b, :hi, h], vals[b, :hi, h], mask)
+                assert (np.abs(got[b, :, h] - want) <= bound + 2.0 ** -8 * (np.abs(want) + bound)).all()
+        av = R.values(*R.quantize(att.double().cpu().numpy(), R.MATRIX))
+        want = av @ wov.T
+        bound = (4 + 4 + 16) * 2.0 ** -23 * (np.abs(av) @ np.abs(wov).T)
+        assert (np.abs(y.double().cpu().numpy() - want) <= bound + 2.0 ** -8 * (np.abs(want) + bound)).all()
+    sfs.sfs_check_device_status()

@@ -1,0 +1,271 @@
+"""Microscaled 4-bit matrices and caches against the plain 64-bit implementation: codes, scales and values exactly, products within
+32-bit sums."""
+import numpy as np
+import pytest
+import torch
+
+import mx4_reference as R
+from paper_2506_10848_b200 import binding as sfs
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": (torch.bfloat16, sfs.LOGITS_BF16), "f32": (torch.float32, sfs.LOGITS_F32)}
+GUARD = 0xA5
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def matrix(rows, cols, seed, spread=3.0):
+    """Normal values whose blocks differ in size by powers of two."""
+    rng = np.random.default_rng(seed)
+    x = rng.normal(size=(rows, cols))
+    return x * 2.0 ** np.repeat(rng.integers(-spread, spread + 1, size=(rows, (cols + 31) // 32)), 32, 1)[:, :cols]
+
+
+def as_input(x, dtype):
+    t = torch.from_numpy(x).to(TYPES[dtype][0])
+    return t, t.double().numpy()
+
+
+def quantize_on_gpu(t, dtype, ld=None, offset=0, pad=0):
+    """-> (codes uint8 [rows, bytes + pad], scales, as written into buffers filled with GUARD bytes)."""
+    rows, cols = t.shape
+    ld = ld or cols
+    buf = torch.zeros(rows * ld + offset, dtype=t.dtype, device=DEV)
+    x = buf[offset:].view(rows, ld)
+    x[:, :cols] = t.to(DEV)
+    codes = torch.full((rows, sfs.mx4_code_bytes(cols) + pad), GUARD, dtype=torch.uint8, device=DEV)
+    scales = torch.full((sfs.mx4_scale_bytes(rows, cols) + 64,), GUARD, dtype=torch.uint8, device=DEV)
+    sfs.sfs_mx4_quantize(x, ld, TYPES[dtype][1], rows, cols, codes, codes.stride(0), scales)
+    torch.cuda.synchronize()
+    return codes, scales
+
+
+SHAPES = [(1, 1), (1, 32), (3, 40), (128, 128), (129, 96), (5, 688), (130, 257), (33, 4096), (257, 1000)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_quantize_gives_the_formats_codes_and_scales(rows, cols, dtype):
+    t, x = as_input(matrix(rows, cols, rows * 7 + cols), dtype)
+    want_codes, want_scales = R.quantize(x, R.MATRIX)
+    for ld, offset, pad in ((cols, 0, 0), (cols + 3, 1, 16)):       # aligned rows, and rows at odd addresses beside a guard
+        codes, scales = quantize_on_gpu(t, dtype, ld, offset, pad)
+        n = sfs.mx4_code_bytes(cols)
+        assert (codes[:, :n].cpu().numpy() == R.pack(want_codes)).all()
+        assert (codes[:, n:] == GUARD).all() and (scales[-64:] == GUARD).all()
+        assert (scales[:-64].cpu().numpy() == R.tile_scales(want_scales)).all()       # the tiles' padding holds zeros
+
+
+def test_quantize_at_the_edges_of_the_numbers():
+    x = np.zeros((12, 96))
+    x[0, :8] = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0]         # half-way points under a scale of 1
+    x[1, :8] = [-0.25, -0.75, -1.25, -1.75, -2.5, -3.5, -5.0, -7.9]
+    x[2, 0], x[2, 40], x[2, 70] = 3.0e38, -3.38e38, 2.0 ** 127
+    x[3, 5] = np.nan
+    x[4, 33], x[4, 64] = np.inf, -np.inf
+    x[5, 0], x[5, 1] = 2.0 ** -126, 2.0 ** -133                     # the smallest normal number and a bf16 subnormal
+    x[6, 0] = 2.0 ** -133
+    x[7, :2] = [4.0, 2.0 ** -40]
+    x[8, 31], x[8, 32] = 1.0, 1.0                                   # last of one block, first of the next
+    x[9] = -0.0
+    x[10] = 7.99
+    x[11, 95] = 1e-30
+    for dtype in ("bf16", "f32"):
+        t, y = as_input(x, dtype)
+        codes, scales = quantize_on_gpu(t, dtype)
+        want_codes, want_scales = R.quantize(y, R.MATRIX)
+        got = R.unpack(codes.cpu().numpy())
+        same = (got == want_codes) | ((got & 7 == 0) & (want_codes & 7 == 0))         # (either zero)
+        assert same.all(), np.argwhere(~same)
+        assert (scales[:-64].cpu().numpy() == R.tile_scales(want_scales)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_dequantize_gives_the_values(rows, cols, dtype):
+    rng = np.random.default_rng(rows + cols)
+    blocks = (cols + 31) // 32
+    codes = rng.integers(0, 16, size=(rows, blocks * 32)).astype(np.uint8)
+    scales = rng.integers(90, 160, size=(rows, blocks)).astype(np.uint8)
+    scales[0, 0] = 255
+    scales[-1, -1] = 0 if dtype == "f32" else 30
+    want = R.values(codes, scales)[:, :cols]
+    for ld, offset in ((cols, 0), (cols + 5, 1)):
+        buf = torch.full((rows * ld + offset,), 77.0, dtype=TYPES[dtype][0], device=DEV)
+        out = buf[offset:].view(rows, ld)
+        sfs.sfs_mx4_dequantize(dev(R.pack(codes)), blocks * 16, dev(R.tile_scales(scales)), rows, cols, out, ld, TYPES[dtype][1])
+        got = out.double().cpu().numpy()
+        assert np.array_equal(got[:, :cols], want, equal_nan=True) and (got[:, cols:] == 77.0).all()
+
+
+# ---- the product --------------------------------------------------------------------------------------------------------------------
+
+def operand(rows, cols, seed):
+    codes, scales = R.quantize(matrix(rows, cols, seed), R.MATRIX)
+    return dev(R.pack(codes)), dev(R.tile_scales(scales)), R.values(codes, scales)
+
+
+def check_linear(M, N, K, out="bf16", scale=1.0, seed=0, ld_pad=0, ldc_pad=0, offset=0):
+    a, a_s, av = operand(M, K, seed + 1)
+    b, b_s, bv = operand(N, K, seed + 2)
+    if ld_pad:
+        a, b = (torch.nn.functional.pad(t, (0, ld_pad), value=0x77) for t in (a, b))       # codes behind the rows that nothing may read as values
+    dtype, code = TYPES[out]
+    buf = torch.full((M * (N + ldc_pad) + offset,), 77.0, dtype=dtype, device=DEV)
+    c = buf[offset:].view(M, N + ldc_pad)
+    sfs.sfs_linear_mx4(a, a.stride(0), a_s, b, b.stride(0), b_s, c, N + ldc_pad, M, N, K, code, scale)
+    sfs.sfs_check_device_status()
+    want = scale * (av @ bv.T)
+    # products are exact; every addition of a 32-bit sum is off by at most 2^-23 of the terms' magnitudes, whichever way it rounds.
+    # In any order no term passes through more additions than there are blocks of 64 columns, four levels inside them and the joining
+    # of up to 16 parts and the scale.
+    steps = (K + 63) // 64 + 4 + 16 + 1
+    bound = steps * 2.0 ** -23 * abs(scale) * (np.abs(av) @ np.abs(bv).T)
+    if out == "bf16":
+        bound = bound * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)
+    got = c.double().cpu().numpy()
+    err = np.abs(got[:, :N] - want)
+    assert (err <= bound).all(), (float((err / np.maximum(bound, 1e-300)).max()), np.argwhere(err > bound)[:4])
+    assert (got[:, N:] == 77.0).all() and (buf[:offset] == 77.0).all()
+
+
+@pytest.mark.parametrize("M", [1, 2, 7, 16, 17, 33, 64, 100, 128, 129, 200, 257, 300])
+def test_linear_rows(M):
+    check_linear(M, 384, 512, seed=M)
+
+
+@pytest.mark.parametrize("N", [1, 8, 31, 127, 128, 129, 250, 256, 700, 2048])
+def test_linear_columns(N):
+    for M in (3, 140):
+        check_linear(M, N, 256, seed=N + M)
+
+
+@pytest.mark.parametrize("K", [1, 16, 32, 48, 64, 96, 128, 160, 250, 256, 320, 688, 1024, 1056, 4096])
+def test_linear_depths(K):
+    for M in (5, 150):
+        check_linear(M, 136, K, seed=K + M)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (8, 4096, 12288), (128, 1024, 4096), (640, 1536, 2048), (16, 12288, 64), (1000, 1000, 1000)])
+def test_linear_larger(M, N, K):
+    check_linear(M, N, K, seed=5)
+
+
+@pytest.mark.parametrize("M,N", [(4, 100), (150, 257), (300, 512)])
+def test_linear_types_strides_and_scale(M, N):
+    check_linear(M, N, 352, out="f32", scale=0.375, ld_pad=16, ldc_pad=3, offset=1)
+    check_linear(M, N, 352, out="bf16", scale=-2.5, ld_pad=48, ldc_pad=5, offset=1)
+    check_linear(M, N, 352, out="bf16", ldc_pad=8)
+
+
+def test_linear_does_not_let_a_nan_leave_its_row():
+    a, a_s, av = operand(150, 256, 1)
+    b, b_s, bv = operand(70, 256, 2)
+    places = R.scale_places(150, 8)
+    a_s[int(places[149, 7])] = 255
+    out = torch.zeros((150, 70), dtype=torch.float32, device=DEV)
+    sfs.sfs_linear_mx4(a, 128, a_s, b, 128, b_s, out, 70, 150, 70, 256, 1)
+    assert out[149].isnan().all() and not out[:149].isnan().any()
+    sfs.sfs_check_device_status()
+
+
+def test_quantise_and_multiply_in_a_graph_on_another_stream():
+    """Two projections captured in one graph, replayed on new inputs: no state is kept between calls."""
+    M, N, K = 40, 512, 1024
+    b, b_s, bv = operand(N, K, 9)
+    x = torch.zeros((M, K), dtype=torch.bfloat16, device=DEV)
+    codes = torch.zeros((M, K // 2), dtype=torch.uint8, device=DEV)
+    scales = torch.zeros(sfs.mx4_scale_bytes(M, K), dtype=torch.uint8, device=DEV)
+    out = torch.zeros((M, N), dtype=torch.float32, device=DEV)
+
+    def step():
+        sfs.sfs_mx4_quantize(x, K, 0, M, K, codes, K // 2, scales)
+        sfs.sfs_linear_mx4(codes, K // 2, scales, b, K // 2, b_s, out, N, M, N, K, 1)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (1, 2):
+        t, xv = as_input(matrix(M, K, seed), "bf16")
+        x.copy_(t)
+        with torch.cuda.stream(torch.cuda.Stream()):
+            torch.cuda.current_stream().wait_stream(torch.cuda.default_stream())
+            graph.replay()
+        torch.cuda.synchronize()
+        av = R.values(*R.quantize(xv, R.MATRIX))
+        bound = (16 + 4 + 16) * 2.0 ** -23 * (np.abs(av) @ np.abs(bv).T)
+        assert (np.abs(out.double().cpu().numpy() - av @ bv.T) <= bound).all()
+
+
+# ---- the cache ------------------------------------------------------------------------------------------------------------------------
+
+def new_cache(batch, capacity, heads, dim):
+    slots = batch * capacity
+    full = lambda *s: torch.full(s, GUARD, dtype=torch.uint8, device=DEV)  # noqa: E731
+    return sfs.Cache4(full(slots, heads, dim // 2), full(slots, heads, dim // 32), full(slots, heads, dim // 2), full(slots, heads, dim // 32),
+                      batch, capacity, heads, dim)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,dim", [(1, 64), (3, 64), (4, 128), (5, 128)])
+def test_store_and_load(heads, dim, dtype):
+    batch, capacity, n = 2, 37, 21
+    width = heads * dim
+    c = new_cache(batch, capacity, heads, dim)
+    rng = np.random.default_rng(heads + dim)
+    slots = rng.permutation(batch * capacity)[:n].astype(np.int32)
+    slots[3], slots[4], slots[5] = -1, batch * capacity, -2 ** 31   # rows that are left out
+    t, kv = as_input(matrix(n, 2 * width + 3, 3), dtype)
+    t = t.to(DEV)
+    k, v = t[:, :width], t[:, width + 3:]                           # rows of keys and values side by side, at odd addresses
+    sfs.sfs_cache4_store(c, k, t.stride(0), v, t.stride(0), TYPES[dtype][1], dev(slots), n)
+    torch.cuda.synchronize()
+    kept = (slots >= 0) & (slots < batch * capacity)
+    for x, codes, scales in ((kv[:, :width], c._tensors[0], c._tensors[1]), (kv[:, width + 3:], c._tensors[2], c._tensors[3])):
+        want_codes, want_scales = R.quantize(x, R.CACHE)
+        all_codes = np.full((batch * capacity, width // 2), GUARD, np.uint8)
+        all_scales = np.full((batch * capacity, width // 32), GUARD, np.uint8)
+        all_codes[slots[kept]], all_scales[slots[kept]] = R.pack(want_codes)[kept], want_scales[kept]
+        assert (codes.cpu().numpy().reshape(all_codes.shape) == all_codes).all() and (scales.cpu().numpy().reshape(all_scales.shape) == all_scales).all()
+    out = torch.full((n, 2, width + 1), 77.0, dtype=TYPES[dtype][0], device=DEV)
+    sfs.sfs_cache4_load(c, dev(slots), n, out, out.stride(0), out[:, 1], out.stride(0), TYPES[dtype][1])
+    got = out.double().cpu().numpy()
+    for i, x in enumerate((kv[:, :width], kv[:, width + 3:])):
+        want = R.values(*R.quantize(x, R.CACHE))
+        assert (got[kept, i, :width] == want[kept]).all() and (got[~kept, i] == 77.0).all() and (got[:, i, width:] == 77.0).all()
+    only = torch.full((n, width), 77.0, dtype=TYPES[dtype][0], device=DEV)
+    sfs.sfs_cache4_load(c, dev(slots), n, None, 0, only, width, TYPES[dtype][1])    # values alone
+    assert torch.equal(only.cpu(), out[:, 1, :width].cpu())
+
+
+def test_of_rows_with_one_slot_the_last_counts():
+    heads, dim, n, slots_n = 2, 64, 1000, 7
+    c = new_cache(1, slots_n, heads, dim)
+    slots = (np.arange(n) * 31 % slots_n).astype(np.int32)
+    t, x = as_input(matrix(n, heads * dim, 1), "bf16")
+    t = t.to(DEV)
+    for _ in range(3):
+        sfs.sfs_cache4_store(c, t, heads * dim, t, heads * dim, 0, dev(slots), n)
+    out = torch.zeros((slots_n, heads * dim), dtype=torch.bfloat16, device=DEV)
+    sfs.sfs_cache4_load(c, None, slots_n, out, heads * dim, None, 0, 0)
+    last = [max(r for r in range(n) if slots[r] == s) for s in range(slots_n)]
+    assert (out.double().cpu().numpy() == R.values(*R.quantize(x[last], R.CACHE))).all()
+
+
+def test_slots_in_order_and_scales_at_the_ends_of_their_range():
+    heads, dim = 1, 128
+    x = np.ones((4, 128))
+    x[0] *= 2.0 ** 100; x[1] *= 2.0 ** -100; x[2, 7] = np.nan; x[3, 64:] = 0.0
+    c = new_cache(1, 5, heads, dim)
+    t, y = as_input(x, "bf16")
+    sfs.sfs_cache4_store(c, t.to(DEV), dim, t.to(DEV), dim, 0, None, 4)
+    out = torch.full((5, dim), 77.0, dtype=torch.float32, device=DEV)
+    sfs.sfs_cache4_load(c, None, 4, out, dim, None, 0, 1)
+    want = R.values(*R.quantize(y, R.CACHE))
+    assert want[0, 0] == 6 * 2.0 ** 65 and want[1, 0] == 0 and np.isnan(want[2, :32]).all()
+    got = out.double().cpu().numpy()
+    assert np.array_equal(got[:4], want, equal_nan=True) and (got[4] == 77.0).all()
