@@ -1,32 +1,287 @@
-// C = scale * A * B^T of two matrices of microscaled 4-bit numbers: one thread per element of C.
+// C = scale * A * B^T of two matrices of microscaled 4-bit numbers on the block-scaled tensor-core instruction
+// (tcgen05.mma kind::mxf4: 64 columns per step, two scale bytes per row and step read from tensor memory).
+//
+// A CTA computes a tile of 128 rows of one operand ("lanes") by BN rows of the other ("columns"): with many tokens the lanes are
+// tokens, with at most 128 of them the lanes are features, so that one column tile of 16 .. 128 holds all tokens and the weights
+// stream through every SM.  A stage of the shared-memory ring is 256 columns of codes (128 bytes a row, 128-byte swizzle, by TMA) and
+// the scale tiles that belong to them, which lie in global memory as the copy into tensor memory wants them: 512 bytes for 128
+// rows and 128 columns, one bulk copy.  Warp 0 loads, warp 1 copies scales to tensor memory and issues (both in the order of issue on
+// the tensor core's pipe), warps 2-5 store.
+//
+// Few tiles: K is divided over a cluster of up to 8 CTAs, whose 32-bit partial sums are exchanged through shared memory and added
+// in the order of the ranks, so no workspace and no atomics are needed and the same call gives the same bits.
 #include "mx4.cuh"
+#include "tc05.cuh"
+#include "gemm.cuh"
+#include <algorithm>
 
 namespace sfs {
 namespace {
 
-__global__ void __launch_bounds__(256)
-linear_mx4_elements(const uint8_t *A, long long lda, const uint8_t *As, const uint8_t *B, long long ldb, const uint8_t *Bs, void *C, long long ldc,
-                    int M, int N, int blocks, int out_f32, float scale)
+constexpr int kThreads = 192;
+constexpr int kDepth = 256;                                 // columns of a stage
+constexpr int kCodes = 128;                                 // bytes of a row in a stage
+constexpr int kScaleTile = 512;                             // 128 rows x 4 blocks
+
+template <int BN> struct Shape {
+    static constexpr int kRowTiles = BN > 128 ? 2 : 1;      // scale tiles along the columns' rows
+    static constexpr int kA = 128 * kCodes, kB = BN * kCodes;
+    static constexpr int kScaleA = 2 * kScaleTile, kScaleB = kRowTiles * 2 * kScaleTile;
+    static constexpr int kStage = kA + kB + kScaleA + kScaleB;
+    static constexpr int kPerSm = BN > 128 ? 1 : 2;
+    static constexpr int kStages = (kPerSm == 1 ? 210 * 1024 : 106 * 1024) / kStage;
+    static constexpr int kScaleCols = 8 + 8 * kRowTiles;    // tensor-memory columns of a stage's scales
+    // every stage has scales of its own in tensor memory: a copy may overtake an MMA issued before it, but not the stage's release
+    static constexpr int kColumns = BN + kStages * kScaleCols;
+    static constexpr int kTmem = kColumns <= 64 ? 64 : kColumns <= 128 ? 128 : kColumns <= 256 ? 256 : 512;
+    static constexpr int kBarriers = 2 * kStages + 1;
+    static constexpr int kShared = kStages * kStage + 1024 /* alignment */ + kBarriers * 8 + 16;
+    static_assert(kB % 1024 == 0 && kColumns <= kTmem && kPerSm * kTmem <= 512, "tile");
+    static_assert(kStages * kStage >= 128 * BN * 4 || BN > 128, "partial sums fit the ring");
+};
+
+struct Mx4Args {
+    const uint8_t *lane_scales, *col_scales;
+    void *C; long long ldc;
+    int lanes, cols;                                        // rows of the two operands
+    int blocks, quads;                                      // blocks of 32 columns in a row, tiles of four of them
+    int col_tiles, splits;
+    int out_f32, features_on_lanes, wide;                   // wide: rows of C take 16-byte stores
+    float scale;
+    int32_t *err;
+};
+
+// kind::mxf4, both operands e2m1 and K-major, E8M0 scales of 32 columns, fp32 accumulator; `half`: which two of a column's four scale bytes
+constexpr uint32_t idesc_mxf4(int N, int half) { return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | (1u << 27) | ((uint32_t)(2 * half) << 29); }
+
+__device__ __forceinline__ void mma_mxf4_elect(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, uint32_t accumulate)
 {
+    asm volatile("{\n\t.reg .pred P, Q;\n\telect.sync _|P, 0xffffffff;\n\tsetp.ne.b32 Q, %6, 0;\n\t"
+                 "@P tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], Q;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate) : "memory");
+}
+// 32 rows of 16 bytes -> the same 32 lanes of all four quarters of tensor memory, four columns
+__device__ __forceinline__ void copy_scales_elect(uint32_t tmem, uint32_t smem)
+{
+    const uint64_t d = (uint64_t)((smem >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+    asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\t"
+                 "@P tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem), "l"(d) : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t smem, const void *global, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem), "l"(global), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ float load_remote(uint32_t cluster_addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+    return v;
+}
+
+// n consecutive columns of one lane
+template <int N>
+__device__ __forceinline__ void store_columns(const Mx4Args &a, int lane, int col, const float *v)
+{
+    if (lane >= a.lanes) return;
+    if (a.features_on_lanes) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (col + i < a.cols) {
+                const long long at = (long long)(col + i) * a.ldc + lane;
+                if (a.out_f32) static_cast<float *>(a.C)[at] = v[i]; else static_cast<__nv_bfloat16 *>(a.C)[at] = __float2bfloat16_rn(v[i]);
+            }
+    } else {
+        const long long at = (long long)lane * a.ldc + col;
+        if (a.wide && col + N <= a.cols && N % 8 == 0) {
+            if (a.out_f32) {
+#pragma unroll
+                for (int i = 0; i < N / 4; ++i) reinterpret_cast<float4 *>(static_cast<float *>(a.C) + at)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N / 8; ++i) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) { const __nv_bfloat162 h = __floats2bfloat162_rn(v[8 * i + 2 * t], v[8 * i + 2 * t + 1]); w[t] = *reinterpret_cast<const uint32_t *>(&h); }
+                    reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.C) + at)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (col + i < a.cols) {
+                    if (a.out_f32) static_cast<float *>(a.C)[at + i] = v[i]; else static_cast<__nv_bfloat16 *>(a.C)[at + i] = __float2bfloat16_rn(v[i]);
+                }
+        }
+    }
+}
+
+template <int BN>
+__global__ void __launch_bounds__(kThreads, Shape<BN>::kPerSm)
+linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_constant__ CUtensorMap tm_cols, Mx4Args a)
+{
+    using S = Shape<BN>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    // codes first (1024-byte aligned), then every stage's scales
+    uint8_t *scales = ring + S::kStages * (S::kA + S::kB);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(ring + S::kStages * S::kStage);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + S::kBarriers);
+    __shared__ int s_abort;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits;
+    const int col_tile = tile % a.col_tiles, lane_tile = tile / a.col_tiles;
+    const int n_steps = (a.blocks + kDepth / 32 - 1) / (kDepth / 32);
+    const int first = (int)((long long)n_steps * split / a.splits), last = (int)((long long)n_steps * (split + 1) / a.splits);
+    const uint32_t full = tc::smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) { tc::mbar_init(full + 8 * s, 1); tc::mbar_init(empty + 8 * s, 1); }
+        tc::mbar_init(done, 1);
+        s_abort = 0;
+        tc::mbar_init_fence();
+    }
+    if (warp == 0 && lane == 0) { tc::tma_prefetch_desc(&tm_lanes); tc::tma_prefetch_desc(&tm_cols); }
+    if (warp == 1) { tc::tmem_alloc(tc::smem_u32(tmem_slot), S::kTmem); tc::tmem_relinquish(); }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tmem_slot);
     pdl_wait();
     pdl_trigger();
-    const int n = blockIdx.x * 16 + (threadIdx.x & 15), m = blockIdx.y * 16 + threadIdx.x / 16, quads = (blocks + 3) / 4;
-    if (m >= M || n >= N) return;
-    auto place = [&](int r, int b) { return ((size_t)(r >> 7) * quads + (b >> 2)) * 512 + (r & 31) * 16 + ((r & 127) >> 5) * 4 + (b & 3); };
-    float sum = 0.f;
-    for (int b = 0; b < blocks; ++b) {
-        float part = 0.f;
-        for (int w = 0; w < 4; ++w) {
-            float x[8], y[8];
-            mx4::decode8(*reinterpret_cast<const uint32_t *>(A + m * lda + b * 16 + w * 4), x);
-            mx4::decode8(*reinterpret_cast<const uint32_t *>(B + n * ldb + b * 16 + w * 4), y);
-            for (int i = 0; i < 8; ++i) part = fmaf(x[i], y[i], part);
+
+    auto codes_of = [&](int s) { return tc::smem_u32(ring) + s * (S::kA + S::kB); };
+    auto scales_of = [&](int s) { return tc::smem_u32(scales) + s * (S::kScaleA + S::kScaleB); };
+    if (warp == 0) {
+        if (lane == 0) {
+            int issued = first;
+            for (int k = first, s = 0, ph = 0; k < last; ++k) {
+                if (!tc::mbar_wait(empty + 8 * s, (uint32_t)ph ^ 1u, &s_abort)) break;
+                const uint32_t bar = full + 8 * s, part = (uint32_t)min(2, a.quads - 2 * k) * kScaleTile;   // (the last stage may hold one tile of scales)
+                const bool second = S::kRowTiles == 2 && (col_tile * 2 + 1) * 128 < a.cols;
+                tc::mbar_expect_tx(bar, (uint32_t)(S::kA + S::kB) + part * (second ? 3u : 2u));
+                tc::tma_load_2d(codes_of(s), &tm_lanes, k * (kCodes / 2), lane_tile * 128, bar);
+                tc::tma_load_2d(codes_of(s) + S::kA, &tm_cols, k * (kCodes / 2), col_tile * BN, bar);
+                bulk_load(scales_of(s), a.lane_scales + ((size_t)lane_tile * a.quads + 2 * k) * kScaleTile, part, bar);
+                bulk_load(scales_of(s) + S::kScaleA, a.col_scales + ((size_t)col_tile * S::kRowTiles * a.quads + 2 * k) * kScaleTile, part, bar);
+                if (second) bulk_load(scales_of(s) + 2 * S::kScaleA, a.col_scales + ((size_t)(col_tile * 2 + 1) * a.quads + 2 * k) * kScaleTile, part, bar);
+                issued = k + 1;
+                if (++s == S::kStages) { s = 0; ph ^= 1; }
+            }
+            if (s_abort)                                    // copies in flight get a bounded time to land before the CTA retires
+                for (int k = max(first, issued - S::kStages); k < issued; ++k) {
+                    const int s = (k - first) % S::kStages, ph = ((k - first) / S::kStages) & 1;
+                    for (int i = 0; i < (1 << 16) && !tc::mbar_try(full + 8 * s, (uint32_t)ph); ++i) {}
+                }
         }
-        sum += part * mx4::scale_value(As[place(m, b)]) * mx4::scale_value(Bs[place(n, b)]);
+        __syncwarp();
+    } else if (warp == 1) {
+        const uint32_t tmem_scales = tmem + BN;
+        bool ok = true;
+        for (int k = first, s = 0, ph = 0; k < last; ++k) {
+            ok = __all_sync(0xffffffffu, tc::mbar_wait(full + 8 * s, (uint32_t)ph, &s_abort));
+            if (!ok) break;
+            tc::tc_fence_after();
+            const uint32_t ta = tmem_scales + (uint32_t)(s * S::kScaleCols), tb = ta + 8;
+            const int tiles = min(2, a.quads - 2 * k);
+            for (int q = 0; q < tiles; ++q) {
+                copy_scales_elect(ta + 4 * q, scales_of(s) + q * kScaleTile);
+#pragma unroll
+                for (int r = 0; r < S::kRowTiles; ++r) copy_scales_elect(tb + q * 4 * S::kRowTiles + 4 * r, scales_of(s) + S::kScaleA + r * 2 * kScaleTile + q * kScaleTile);
+            }
+            const uint64_t da = tc::smem_desc_sw128(codes_of(s)), db = tc::smem_desc_sw128(codes_of(s) + S::kA);
+            const int mmas = min(4, (a.blocks - k * 8 + 1) / 2);                // 64 columns each
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < mmas)
+                    mma_mxf4_elect(tmem, da + (uint64_t)(2 * i), db + (uint64_t)(2 * i), idesc_mxf4(BN, i & 1), ta + 4 * (i >> 1), tb + (i >> 1) * 4 * S::kRowTiles,
+                                   (k != first || i != 0) ? 1u : 0u);
+            tc::mma_commit_elect(empty + 8 * s);
+            if (++s == S::kStages) { s = 0; ph ^= 1; }
+        }
+        if (ok) tc::mma_commit_elect(done);
+        __syncwarp();
     }
-    sum *= scale;
-    if (out_f32) static_cast<float *>(C)[m * ldc + n] = sum;
-    else static_cast<__nv_bfloat16 *>(C)[m * ldc + n] = __float2bfloat16_rn(sum);
+    // ---------------- the tile: warps 2-5, each its quarter of the lanes
+    const int q = warp & 3, row = q * 32 + lane;
+    const bool storing = warp >= 2;
+    bool ok = storing && tc::mbar_wait(done, 0, &s_abort);
+    ok = __all_sync(0xffffffffu, ok);
+    if (ok) tc::tc_fence_after();
+    const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16);
+    constexpr int CH = BN < 32 ? BN : 32;
+    if (a.splits == 1) {
+        if (ok) {
+#pragma unroll 1
+            for (int c = 0; c < BN; c += CH) {
+                uint32_t u[32];
+                float v[CH];
+                tc::tmem_ld32(acc + c, u);                  // (a narrow tile reads columns of scales too)
+                tc::tmem_ld_wait32(u);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) v[i] = __uint_as_float(u[i]) * a.scale;
+                store_columns<CH>(a, lane_tile * 128 + row, col_tile * BN + c, v);
+            }
+        }
+    } else if constexpr (BN <= 128) {
+        // partial sums to this CTA's ring (every copy into it has landed and been read by now), then each rank adds its columns of all ranks'
+        float *mine = reinterpret_cast<float *>(ring);
+        if (ok) {
+#pragma unroll 1
+            for (int c = 0; c < BN; c += CH) {
+                uint32_t u[32];
+                tc::tmem_ld32(acc + c, u);
+                tc::tmem_ld_wait32(u);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) mine[(c + i) * 128 + row] = __uint_as_float(u[i]);
+            }
+        }
+        tc::cluster_sync();
+        if (storing) {
+            constexpr int W = BN / 8;                       // columns of a slice
+            for (int slice = split; slice < 8; slice += a.splits) {
+                float v[W];
+#pragma unroll
+                for (int i = 0; i < W; ++i) v[i] = 0.f;
+                for (int r = 0; r < a.splits; ++r) {
+                    const uint32_t from = tc::mapa(tc::smem_u32(mine + (slice * W) * 128 + row), (uint32_t)r);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) v[i] += load_remote(from + i * 512);
+                }
+#pragma unroll
+                for (int i = 0; i < W; ++i) v[i] *= a.scale;
+                if (!s_abort) store_columns<W>(a, lane_tile * 128 + row, col_tile * BN + slice * W, v);
+            }
+        }
+        tc::cluster_sync();                                 // the ring stays until every rank has read it
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (warp == 1) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, S::kTmem); }
+    if (threadIdx.x == 0 && s_abort && a.err) atomicExch(a.err, SFS_ERR_TIMEOUT);
+}
+
+int32_t codes_map(CUtensorMap *out, const void *base, uint64_t rows, uint64_t bytes, uint64_t ld, uint32_t box_rows)
+{
+    // pairs of code bytes as 16-bit elements: 64 of them are one swizzled row
+    return make_tmap_bf16(out, base, rows, bytes / 2, ld / 2, box_rows);
+}
+
+template <int BN>
+int32_t launch(const Mx4Args &a, const void *lanes, long long ld_lanes, const void *cols, long long ld_cols, cudaStream_t stream)
+{
+    using S = Shape<BN>;
+    CUtensorMap tl, tcol;
+    int32_t rc;
+    if ((rc = codes_map(&tl, lanes, (uint64_t)a.lanes, (uint64_t)a.blocks * 16, (uint64_t)ld_lanes, 128)) != SFS_OK) return rc;
+    if ((rc = codes_map(&tcol, cols, (uint64_t)a.cols, (uint64_t)a.blocks * 16, (uint64_t)ld_cols, BN)) != SFS_OK) return rc;
+    SFS_CUDA(allow_shared(linear_mx4_kernel<BN>, S::kShared));
+    const long long ctas = (long long)((a.lanes + 127) / 128) * a.col_tiles * a.splits;
+    SFS_REQUIRE(ctas <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "linear_mx4: too many tiles");
+    if (a.splits > 1) SFS_CUDA(launch_pdl_cluster(linear_mx4_kernel<BN>, a.splits, dim3((unsigned)ctas), dim3(kThreads), (size_t)S::kShared, stream, tl, tcol, a));
+    else SFS_CUDA(launch_pdl(linear_mx4_kernel<BN>, dim3((unsigned)ctas), dim3(kThreads), (size_t)S::kShared, stream, tl, tcol, a));
+    return SFS_OK;
 }
 
 }  // namespace
@@ -47,8 +302,31 @@ extern "C" int32_t sfs_linear_mx4(const void *d_A, int64_t lda, const void *d_A_
     SFS_REQUIRE(lda % 16 == 0 && ldb % 16 == 0 && lda >= bytes && ldb >= bytes, SFS_ERR_INVALID_ARG,
                 "linear_mx4: lda and ldb must be multiples of 16 and hold a row");
     SFS_REQUIRE(ldc >= N && aligned_to(d_C, out_dtype ? 4 : 2), SFS_ERR_INVALID_ARG, "linear_mx4: misaligned C, or ldc below N");
-    SFS_CUDA(launch_pdl(linear_mx4_elements, dim3((unsigned)((N + 15) / 16), (unsigned)((M + 15) / 16)), dim3(256), 0, (cudaStream_t)stream,
-                        (const uint8_t *)d_A, (long long)lda, (const uint8_t *)d_A_scales, (const uint8_t *)d_B, (long long)ldb, (const uint8_t *)d_B_scales,
-                        d_C, (long long)ldc, M, N, (K + 31) / 32, out_dtype, scale));
-    return SFS_OK;
+    int32_t *err = device_status_word();
+    SFS_REQUIRE(err != nullptr, SFS_ERR_OOM, "cannot allocate the device status word");
+
+    const bool features_on_lanes = M <= 128;
+    const int lanes = features_on_lanes ? N : M, cols = features_on_lanes ? M : N;
+    const int lane_tiles = (lanes + 127) / 128, n_steps = (K + kDepth - 1) / kDepth, sms = gemm_num_sms();
+    int bn = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+    if (!features_on_lanes && (long long)lane_tiles * ((cols + 255) / 256) > sms) bn = 256;
+    const int col_tiles = (cols + bn - 1) / bn;
+    int splits = 1;
+    if (bn <= 128)
+        while (splits < 8 && (long long)lane_tiles * col_tiles * splits * 2 <= 2 * sms && n_steps >= splits * 4) splits *= 2;
+    Mx4Args a = {};
+    a.lane_scales = (const uint8_t *)(features_on_lanes ? d_B_scales : d_A_scales);
+    a.col_scales = (const uint8_t *)(features_on_lanes ? d_A_scales : d_B_scales);
+    a.C = d_C; a.ldc = ldc; a.lanes = lanes; a.cols = cols; a.blocks = (K + 31) / 32; a.quads = (K + 127) / 128;
+    a.col_tiles = col_tiles; a.splits = splits; a.out_f32 = out_dtype; a.features_on_lanes = features_on_lanes; a.scale = scale; a.err = err;
+    a.wide = aligned_to(d_C, 16) && ldc * (out_dtype ? 4 : 2) % 16 == 0;
+    const void *lp = features_on_lanes ? d_B : d_A, *cp = features_on_lanes ? d_A : d_B;
+    const long long ll = features_on_lanes ? ldb : lda, lc = features_on_lanes ? lda : ldb;
+    switch (bn) {
+    case 16: return launch<16>(a, lp, ll, cp, lc, (cudaStream_t)stream);
+    case 32: return launch<32>(a, lp, ll, cp, lc, (cudaStream_t)stream);
+    case 64: return launch<64>(a, lp, ll, cp, lc, (cudaStream_t)stream);
+    case 128: return launch<128>(a, lp, ll, cp, lc, (cudaStream_t)stream);
+    default: return launch<256>(a, lp, ll, cp, lc, (cudaStream_t)stream);
+    }
 }
