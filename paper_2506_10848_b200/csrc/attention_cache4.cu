@@ -1,51 +1,398 @@
-// Attention over a key / value cache of microscaled 4-bit numbers: one warp per query row and head.
+// Attention over a key / value cache of microscaled 4-bit numbers, few query rows per key head: every code is read once and decoded in
+// registers, straight into the operands of mma.sync.
+//
+// Codes become bf16 by moving bits: the sign to the top, the three others to the low end of the exponent and the high end of the
+// mantissa, which is the value times 2^-126 (0.5 as a subnormal number).  One product with 2^(c - 65) gives the value times 2^-64,
+// exactly, for every scale a cache holds (65 .. 192); scores get the 2^64 back in 32 bits, values from the probabilities, which are
+// taken 2^64 times as large.
+//
+// Tokens are the rows of the first product's tile, queries its columns: S^T = K Q^T (16 tokens x 8 queries), then O^T += V^T P^T
+// (features x queries), so that a single query wastes half as much of the tensor core as it would as one row of 16.  The order of the
+// features within a product is free as long as both operands agree, so a lane takes whole words of codes: of a key 32 neighbouring
+// features (one scale), of values 16 neighbouring features of four tokens, whose codes are paired token by token.
+//
+// The tokens that any row of the CTA sees are divided over a cluster of up to 16 CTAs of 8 warps; partial outputs are joined through
+// shared memory, first the warps', then the CTAs', in a fixed order: no workspace.
 #include "attention_cache4.cuh"
+#include "tc05.cuh"
+#include "gemm.cuh"
+#include <algorithm>
 
 namespace sfs {
 namespace {
 
-template <int DH>
-__global__ void __launch_bounds__(128)
-attention_cache4_rows(Cache4Args a)
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+constexpr int kStep = 16;                                   // tokens of a warp's step
+constexpr float kLazy = 8.0f;                               // the reference maximum may lag by 2^8
+constexpr float kUnscale = 18446744073709551616.0f;         // 2^64
+
+__device__ __forceinline__ void mma_bf16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1)
 {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// the two codes at bits 4 j of each half of `w`, times 2^-126
+template <int J>
+__device__ __forceinline__ uint32_t codes_as_bf16(uint32_t w)
+{
+    const uint32_t s = J == 3 ? w : w << (12 - 4 * J);
+    const uint32_t m = J == 0 ? w << 6 : J == 1 ? w << 2 : J == 2 ? w >> 2 : w >> 6;
+    return (s & 0x80008000u) | (m & 0x01C001C0u);
+}
+// 2^(c - 65) as bf16 bits; scales above a cache's are NaN
+__device__ __forceinline__ uint32_t factor_bits(uint32_t c) { return c > mx4::kCacheHi ? 0x7FC0u : (c + 62) << 7; }
+
+__device__ __forceinline__ float load_remote(uint32_t cluster_addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+    return v;
+}
+
+// what a warp reads of 16 tokens: raw codes and scale bytes of its lanes
+template <int DH> struct Raw;
+template <> struct Raw<128> { uint4 k[2]; uint2 v[4]; uint32_t ks[2], vs[4]; };
+template <> struct Raw<64> { uint2 k[2]; uint32_t v[4]; uint32_t ks[2], vs[4]; };
+
+template <int DH, int NT>                                   // NT tiles of 8 query rows
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
+attention_cache4_few(Cache4Args a, int splits, int row_tiles)
+{
+    constexpr int ROWS = 8 * NT, KS = DH / 16, WORDS = DH / 8, BLOCKS = DH / 32;
+    constexpr int MT = DH / 16;                             // feature tiles of O^T
+    constexpr int PITCH = DH + 4;
+    extern __shared__ float s_mem[];
+    float *s_part = s_mem;                                  // [kWarps][ROWS][PITCH]
+    float *s_out = s_mem + kWarps * ROWS * PITCH;           // [ROWS][DH], unnormalised, of this CTA
+    __shared__ float s_m[kWarps][ROWS], s_l[kWarps][ROWS];  // reference maximum and denominator
+    __shared__ float s_cm[ROWS], s_cl[ROWS];                // of this CTA
+    __shared__ float s_f[16][ROWS], s_inv[ROWS];
+    __shared__ int s_lo[ROWS], s_hi[ROWS], s_first[ROWS], s_live[ROWS];
+
     pdl_wait();
     pdl_trigger();
-    constexpr int E = DH / 32;                              // dimensions of a lane
-    const int lane = threadIdx.x & 31, heads = a.n_kv * a.group;
-    const long long item = (long long)blockIdx.x * 4 + threadIdx.x / 32;
-    if (item >= (long long)a.batch * a.n_q * heads) return;
-    const int head = (int)(item % heads), kv = head / a.group;
-    const long long row = item / heads;
-    const int b = (int)(row / a.n_q), i = (int)(row % a.n_q), length = cache4_length(a, b);
-    long long p = (long long)length - a.n_q + i;
-    if (a.positions) { p = a.positions[row]; if (p < 0) return; }
-    const Seen seen = cache4_seen(a, length, p);
-    float q[E], o[E], m = -INFINITY, l = 0.f;
-    for (int e = 0; e < E; ++e) { q[e] = __bfloat162float(a.q[row * a.ld_q + head * DH + lane * E + e]); o[e] = 0.f; }
-    auto value = [&](const uint8_t *codes, const uint8_t *scales, size_t at, float *v) {
-        const int c = scales[at * (DH / 32) + lane * E / 32];
-        const float f = mx4::scale_value(c > mx4::kCacheHi ? 255 : c);
-        for (int e = 0; e < E; e += 2) {
-            const uint32_t w = codes[at * (DH / 2) + (lane * E + e) / 2];
-            float d[8];
-            mx4::decode8(w, d);
-            v[e] = d[0] * f; v[e + 1] = d[1] * f;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int rank = blockIdx.x % splits;
+    int item = blockIdx.x / splits;
+    const int row_tile = item % row_tiles; item /= row_tiles;
+    const int kv = item % a.n_kv, b = item / a.n_kv;
+    const int rows = min(ROWS, a.n_q * a.group - row_tile * ROWS);          // rows of this tile, query by query, the group's heads together
+    const int length = cache4_length(a, b);
+
+    if (threadIdx.x < ROWS) {
+        Seen s = {0, 0, 0};
+        int live = 0;
+        if ((int)threadIdx.x < rows) {
+            const int i = (row_tile * ROWS + threadIdx.x) / a.group;
+            long long p = (long long)length - a.n_q + i;
+            live = 1;
+            if (a.positions) { p = a.positions[(long long)b * a.n_q + i]; live = p >= 0; }
+            if (live) s = cache4_seen(a, length, p);
+        }
+        s_first[threadIdx.x] = s.first; s_lo[threadIdx.x] = s.lo; s_hi[threadIdx.x] = s.hi; s_live[threadIdx.x] = live;
+    }
+    __syncthreads();
+    // what any row sees: [0, first) and [lo, hi); what all rows see: [all_lo, all_hi)
+    int first = 0, lo = 0x7FFFFFFF, hi = 0, all_lo = 0, all_hi = 0x7FFFFFFF;
+    for (int r = 0; r < rows; ++r) {
+        all_lo = max(all_lo, s_lo[r]); all_hi = min(all_hi, s_hi[r]);
+        if (s_hi[r] > s_lo[r] || s_first[r] > 0) { first = max(first, s_first[r]); lo = min(lo, s_lo[r]); hi = max(hi, s_hi[r]); }
+    }
+    lo = min(lo, hi);
+    first = min(first, lo);                                 // (one row's first tokens may lie in another row's window)
+    const int n_first = (first + kStep - 1) / kStep, n_steps = n_first + (hi - lo + kStep - 1) / kStep;
+    const int my_first = (int)((long long)n_steps * rank / splits), my_last = (int)((long long)n_steps * (rank + 1) / splits);
+    auto tokens_of = [&](int s, int &j0, int &end) {
+        if (s < n_first) { j0 = s * kStep; end = first; } else { j0 = lo + (s - n_first) * kStep; end = hi; }
+    };
+
+    // the queries, as the second operand of S^T: lane (g, t) holds row g, the features of its words in pairs (j, j + 4)
+    uint32_t q[NT][KS][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = n * 8 + g;
+        const int i = (row_tile * ROWS + r) / a.group, head = kv * a.group + (row_tile * ROWS + r) % a.group;
+        const __nv_bfloat16 *src = a.q + ((long long)b * a.n_q + i) * a.ld_q + (long long)head * DH + t * (DH / 4);
+#pragma unroll
+        for (int w = 0; w < WORDS / 4; ++w) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (r < rows) x = *reinterpret_cast<const uint4 *>(src + w * 8);
+            q[n][2 * w][0] = __byte_perm(x.x, x.z, 0x5410); q[n][2 * w][1] = __byte_perm(x.x, x.z, 0x7632);
+            q[n][2 * w + 1][0] = __byte_perm(x.y, x.w, 0x5410); q[n][2 * w + 1][1] = __byte_perm(x.y, x.w, 0x7632);
+        }
+    }
+    int r_lo[NT][2], r_hi[NT][2], r_first[NT][2];           // of rows 2 t and 2 t + 1
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { const int r = n * 8 + 2 * t + e; r_lo[n][e] = s_lo[r]; r_hi[n][e] = s_hi[r]; r_first[n][e] = s_first[r]; }
+
+    float o[NT][MT][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.f; }
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n][j][e] = 0.f;
+    }
+    const float c = a.scale_log2 * kUnscale;
+
+    // tokens of a lane: keys j0 + g and j0 + g + 8; values j0 + 2 t, + 1, + 8, + 9
+    const size_t base = (size_t)b * a.capacity * a.n_kv + kv;
+    auto fetch = [&](int s, Raw<DH> &raw) {
+        int j0, end;
+        tokens_of(s, j0, end);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const size_t at = base + (size_t)min(j0 + g + 8 * e, end - 1) * a.n_kv;
+            if constexpr (DH == 128) raw.k[e] = *reinterpret_cast<const uint4 *>(a.k_codes + at * 64 + t * 16);
+            else raw.k[e] = *reinterpret_cast<const uint2 *>(a.k_codes + at * 32 + t * 8);
+            raw.ks[e] = a.k_scales[at * BLOCKS + t * BLOCKS / 4];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const size_t at = base + (size_t)min(j0 + 2 * t + (e & 1) + 8 * (e >> 1), end - 1) * a.n_kv;
+            if constexpr (DH == 128) raw.v[e] = *reinterpret_cast<const uint2 *>(a.v_codes + at * 64 + g * 8);
+            else raw.v[e] = *reinterpret_cast<const uint32_t *>(a.v_codes + at * 32 + g * 4);
+            raw.vs[e] = a.v_scales[at * BLOCKS + g * BLOCKS / 8];
         }
     };
-    for (int j = 0; j < seen.hi; ++j) {
-        if (j >= seen.first && j < seen.lo) { j = seen.lo - 1; continue; }
-        const size_t at = ((size_t)b * a.capacity + j) * a.n_kv + kv;
-        float k[E], v[E], s = 0.f;
-        value(a.k_codes, a.k_scales, at, k);
-        value(a.v_codes, a.v_scales, at, v);
-        for (int e = 0; e < E; ++e) s = fmaf(q[e], k[e], s);
-        s = warp_sum(s) * a.scale_log2;
-        const float m1 = fmaxf(m, s), base = m1 == -INFINITY ? 0.f : m1, f = exp2f(m - base), w = exp2f(s - base);
-        l = l * f + w;
-        for (int e = 0; e < E; ++e) o[e] = o[e] * f + w * v[e];
-        m = m1;
+    auto word_k = [](const Raw<DH> &raw, int e, int w) -> uint32_t {
+        if constexpr (DH == 128) return w == 0 ? raw.k[e].x : w == 1 ? raw.k[e].y : w == 2 ? raw.k[e].z : raw.k[e].w;
+        else return w == 0 ? raw.k[e].x : raw.k[e].y;
+    };
+
+    Raw<DH> raw;
+    int s = my_first + warp;
+    if (s < my_last) fetch(s, raw);
+    for (; s < my_last; s += kWarps) {
+        Raw<DH> cur = raw;
+        if (s + kWarps < my_last) fetch(s + kWarps, raw);
+        int j0, end;
+        tokens_of(s, j0, end);
+        // ---- scores
+        float sc[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
+        uint32_t f[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { f[e] = factor_bits(cur.ks[e]); f[e] |= f[e] << 16; }
+#pragma unroll
+        for (int w = 0; w < WORDS / 4; ++w) {
+            const uint32_t x0 = word_k(cur, 0, w), x1 = word_k(cur, 1, w);
+            uint32_t A[4];
+            A[0] = mul_bf16x2(codes_as_bf16<0>(x0), f[0]); A[1] = mul_bf16x2(codes_as_bf16<0>(x1), f[1]);
+            A[2] = mul_bf16x2(codes_as_bf16<1>(x0), f[0]); A[3] = mul_bf16x2(codes_as_bf16<1>(x1), f[1]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_bf16(sc[n], A, q[n][2 * w][0], q[n][2 * w][1]);
+            A[0] = mul_bf16x2(codes_as_bf16<2>(x0), f[0]); A[1] = mul_bf16x2(codes_as_bf16<2>(x1), f[1]);
+            A[2] = mul_bf16x2(codes_as_bf16<3>(x0), f[0]); A[3] = mul_bf16x2(codes_as_bf16<3>(x1), f[1]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_bf16(sc[n], A, q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
+        }
+        // ---- what the rows do not see
+        const bool whole = j0 >= all_lo && j0 + kStep <= min(end, all_hi);
+        if (!whole) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = j0 + g + 8 * (e >> 1);
+                    const bool in = j < end && (j < r_first[n][e & 1] || (j >= r_lo[n][e & 1] && j < r_hi[n][e & 1]));
+                    if (!in) sc[n][e] = -INFINITY;
+                }
+        }
+        // ---- softmax against a reference that follows the maximum lazily
+        float p[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float x0 = fmaxf(sc[n][0], sc[n][2]) * c, x1 = fmaxf(sc[n][1], sc[n][3]) * c;
+            if (__any_sync(0xffffffffu, x0 > m[n][0] + kLazy || x1 > m[n][1] + kLazy)) {
+                float y[2] = {x0, x1};
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) y[e] = fmaxf(y[e], __shfl_xor_sync(0xffffffffu, y[e], d));
+                    const float to = fmaxf(m[n][e], y[e]), alpha = to == -INFINITY ? 1.f : tc::ex2_approx(m[n][e] - to);
+                    m[n][e] = to;
+                    l[n][e] *= alpha;
+#pragma unroll
+                    for (int j = 0; j < MT; ++j) { o[n][j][e] *= alpha; o[n][j][2 + e] *= alpha; }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float ref = m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1] - 64.f;       // probabilities times 2^64
+                p[n][e] = tc::ex2_approx(fmaf(sc[n][e], c, -ref));
+            }
+            l[n][0] += p[n][0] + p[n][2]; l[n][1] += p[n][1] + p[n][3];
+        }
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) { pb[n][0] = transpose8(pack_bf16(p[n][0], p[n][1])); pb[n][1] = transpose8(pack_bf16(p[n][2], p[n][3])); }
+        // ---- values
+        uint32_t fv[2];
+        uint32_t bad = 0;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t c0 = cur.vs[2 * e], c1 = cur.vs[2 * e + 1];
+            if (c0 > mx4::kCacheHi) bad |= 1u << (2 * e);
+            if (c1 > mx4::kCacheHi) bad |= 2u << (2 * e);
+            fv[e] = (c0 > mx4::kCacheHi ? 0u : (c0 + 62) << 7) | (c1 > mx4::kCacheHi ? 0u : (c1 + 62) << 23);
+        }
+        uint32_t lo4[2][2], hi4[2][2];                      // [token pair][word]: the low and the high four codes of both tokens
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if constexpr (DH == 128) {
+                lo4[e][0] = __byte_perm(cur.v[2 * e].x, cur.v[2 * e + 1].x, 0x5410); hi4[e][0] = __byte_perm(cur.v[2 * e].x, cur.v[2 * e + 1].x, 0x7632);
+                lo4[e][1] = __byte_perm(cur.v[2 * e].y, cur.v[2 * e + 1].y, 0x5410); hi4[e][1] = __byte_perm(cur.v[2 * e].y, cur.v[2 * e + 1].y, 0x7632);
+            } else {                                        // one word: its low codes are the tile's first eight features, its high codes the others
+                lo4[e][0] = __byte_perm(cur.v[2 * e], cur.v[2 * e + 1], 0x5410); lo4[e][1] = __byte_perm(cur.v[2 * e], cur.v[2 * e + 1], 0x7632);
+            }
+        }
+        auto product = [&](auto J, int j, const uint32_t (&x)[2][2]) {
+            uint32_t A[4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int w = 0; w < 2; ++w) A[2 * e + w] = mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[e][w]), fv[e]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_bf16(o[n][j], A, pb[n][0], pb[n][1]);
+        };
+        product(std::integral_constant<int, 0>(), 0, lo4); product(std::integral_constant<int, 1>(), 1, lo4);
+        product(std::integral_constant<int, 2>(), 2, lo4); product(std::integral_constant<int, 3>(), 3, lo4);
+        if constexpr (DH == 128) {
+            product(std::integral_constant<int, 0>(), 4, hi4); product(std::integral_constant<int, 1>(), 5, hi4);
+            product(std::integral_constant<int, 2>(), 6, hi4); product(std::integral_constant<int, 3>(), 7, hi4);
+        }
+        // ---- NaN blocks reach the rows that see them, and no others: how many of them a row sees, by one more product
+        if (__any_sync(0xffffffffu, bad != 0)) {
+            uint32_t A[4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) A[2 * e] = A[2 * e + 1] = ((bad >> (2 * e)) & 1u ? 0x3F80u : 0u) | ((bad >> (2 * e)) & 2u ? 0x3F800000u : 0u);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float in[4], count[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = j0 + g + 8 * (e >> 1);
+                    in[e] = j < end && (j < r_first[n][e & 1] || (j >= r_lo[n][e & 1] && j < r_hi[n][e & 1])) ? 1.f : 0.f;
+                }
+                mma_bf16(count, A, transpose8(pack_bf16(in[0], in[1])), transpose8(pack_bf16(in[2], in[3])));
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (count[e] != 0.f)
+#pragma unroll
+                        for (int j = 0; j < MT; ++j) o[n][j][e] = __uint_as_float(0x7FC00000u);
+            }
+        }
     }
-    for (int e = 0; e < E; ++e) a.out[row * a.ld_out + head * DH + lane * E + e] = __float2bfloat16_rn(l == 0.f ? 0.f : o[e] / l);
+
+    // ---- join the warps
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float x = l[n][e];
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+            if (g == 0) { s_m[warp][n * 8 + 2 * t + e] = m[n][e]; s_l[warp][n * 8 + 2 * t + e] = x; }
+        }
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)                     // rows 2 t + (e & 1); features of the lane's first or second word (or half word)
+                s_part[(warp * ROWS + n * 8 + 2 * t + (e & 1)) * PITCH + g * (DH / 8) + (e >> 1) * (DH / 16) + j] = o[n][j][e];
+    }
+    __syncthreads();
+    if (threadIdx.x < ROWS) {
+        float M = -INFINITY, L = 0.f;
+        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w][threadIdx.x]);
+        for (int w = 0; w < kWarps; ++w) {
+            const float mw = s_m[w][threadIdx.x], fw = mw == -INFINITY ? 0.f : tc::ex2_approx(mw - M);
+            L += fw * s_l[w][threadIdx.x];
+            s_m[w][threadIdx.x] = fw;
+        }
+        s_cm[threadIdx.x] = M; s_cl[threadIdx.x] = L;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < ROWS * DH; i += kThreads) {
+        const int r = i / DH, d = i % DH;
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) x += s_m[w][r] * s_part[(w * ROWS + r) * PITCH + d];
+        s_out[i] = x;
+    }
+    // ---- join the CTAs: each writes a share of the outputs
+    if (splits > 1) tc::cluster_sync(); else __syncthreads();
+    if (threadIdx.x < ROWS) {
+        float M = -INFINITY, L = 0.f;
+        for (int k = 0; k < splits; ++k) { s_f[k][threadIdx.x] = splits > 1 ? load_remote(tc::mapa(tc::smem_u32(&s_cm[threadIdx.x]), (uint32_t)k)) : s_cm[threadIdx.x]; M = fmaxf(M, s_f[k][threadIdx.x]); }
+        for (int k = 0; k < splits; ++k) {
+            const float mk = s_f[k][threadIdx.x], fk = mk == -INFINITY ? 0.f : tc::ex2_approx(mk - M);
+            L += fk * (splits > 1 ? load_remote(tc::mapa(tc::smem_u32(&s_cl[threadIdx.x]), (uint32_t)k)) : s_cl[threadIdx.x]);
+            s_f[k][threadIdx.x] = fk;
+        }
+        s_inv[threadIdx.x] = L == 0.f ? 0.f : kUnscale / L;
+    }
+    __syncthreads();
+    const int pairs = rows * DH / 2;
+    for (int i = rank * kThreads + threadIdx.x; i < pairs; i += splits * kThreads) {
+        const int r = 2 * i / DH, d = 2 * i % DH;
+        if (!s_live[r]) continue;
+        float x = 0.f, y = 0.f;
+        for (int k = 0; k < splits; ++k) {
+            const float fk = s_f[k][r];
+            if (splits > 1) {
+                const uint32_t from = tc::mapa(tc::smem_u32(&s_out[2 * i]), (uint32_t)k);
+                x += fk * load_remote(from); y += fk * load_remote(from + 4);
+            } else { x += fk * s_out[2 * i]; y += fk * s_out[2 * i + 1]; }
+        }
+        const int qi = (row_tile * ROWS + r) / a.group, head = kv * a.group + (row_tile * ROWS + r) % a.group;
+        *reinterpret_cast<uint32_t *>(a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + d) = pack_bf16(x * s_inv[r], y * s_inv[r]);
+    }
+    if (splits > 1) tc::cluster_sync();                     // shared memory stays until every rank has read it
+}
+
+template <int DH, int NT>
+int32_t launch_few(const Cache4Args &a, cudaStream_t stream)
+{
+    constexpr int ROWS = 8 * NT;
+    constexpr size_t shared = (size_t)(kWarps * ROWS * (DH + 4) + ROWS * DH) * 4;
+    const int row_tiles = (int)(((long long)a.n_q * a.group + ROWS - 1) / ROWS);
+    const long long items = (long long)a.batch * a.n_kv * row_tiles;
+    // as many CTAs as the machine holds at a time, but no fewer than two steps of 16 tokens for every warp
+    const int slots = gemm_num_sms() * (NT == 1 ? 2 : 1);
+    int splits = 1;
+    while (splits < 16 && items * splits * 2 <= slots && a.capacity > splits * kWarps * kStep * 2) splits *= 2;
+    SFS_REQUIRE(items * splits <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
+    SFS_CUDA(allow_shared(attention_cache4_few<DH, NT>, shared));
+    if (splits > 8) SFS_CUDA(cudaFuncSetAttribute(attention_cache4_few<DH, NT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    if (splits > 1) SFS_CUDA(launch_pdl_cluster(attention_cache4_few<DH, NT>, splits, dim3((unsigned)(items * splits)), dim3(kThreads), shared, stream, a, splits, row_tiles));
+    else SFS_CUDA(launch_pdl(attention_cache4_few<DH, NT>, dim3((unsigned)items), dim3(kThreads), shared, stream, a, splits, row_tiles));
+    return SFS_OK;
 }
 
 }  // namespace
@@ -74,9 +421,7 @@ extern "C" int32_t sfs_attention_cache4(const sfs_cache4 *cache, const void *d_q
                     cache->batch, cache->capacity, cache->n_kv_heads, n_heads / cache->n_kv_heads,
                     (const __nv_bfloat16 *)d_q, (long long)ld_q, (__nv_bfloat16 *)d_out, (long long)ld_out, n_q, d_lengths, d_positions,
                     left, right, sinks, (float)(1.4426950408889634 / sqrt((double)cache->head_dim)), nullptr};
-    const long long items = (long long)cache->batch * n_q * n_heads;
-    SFS_REQUIRE(items / 4 < 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
-    SFS_CUDA(launch_pdl(cache->head_dim == 128 ? attention_cache4_rows<128> : attention_cache4_rows<64>, dim3((unsigned)((items + 3) / 4)), dim3(128), 0,
-                        (cudaStream_t)stream, a));
-    return SFS_OK;
+    const bool one = (int64_t)n_q * a.group <= 8;
+    if (cache->head_dim == 128) return one ? launch_few<128, 1>(a, (cudaStream_t)stream) : launch_few<128, 2>(a, (cudaStream_t)stream);
+    return one ? launch_few<64, 1>(a, (cudaStream_t)stream) : launch_few<64, 2>(a, (cudaStream_t)stream);
 }
