@@ -421,7 +421,13 @@ extern "C" int32_t sfs_attention_cache4(const sfs_cache4 *cache, const void *d_q
                     cache->batch, cache->capacity, cache->n_kv_heads, n_heads / cache->n_kv_heads,
                     (const __nv_bfloat16 *)d_q, (long long)ld_q, (__nv_bfloat16 *)d_out, (long long)ld_out, n_q, d_lengths, d_positions,
                     left, right, sinks, (float)(1.4426950408889634 / sqrt((double)cache->head_dim)), nullptr};
-    const bool one = (int64_t)n_q * a.group <= 8;
+    const int64_t rows = (int64_t)n_q * a.group;
+    if (rows > 16) {
+        a.err = device_status_word();
+        SFS_REQUIRE(a.err != nullptr, SFS_ERR_OOM, "cannot allocate the device status word");
+        return attention_cache4_many(a, cache->head_dim, (cudaStream_t)stream);
+    }
+    const bool one = rows <= 8;
     if (cache->head_dim == 128) return one ? launch_few<128, 1>(a, (cudaStream_t)stream) : launch_few<128, 2>(a, (cudaStream_t)stream);
     return one ? launch_few<64, 1>(a, (cudaStream_t)stream) : launch_few<64, 2>(a, (cudaStream_t)stream);
 }

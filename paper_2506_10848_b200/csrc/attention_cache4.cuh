@@ -31,6 +31,8 @@ __device__ __forceinline__ Seen cache4_seen(const Cache4Args &a, int length, lon
 }
 #endif
 
+// rows are many: the tensor-memory kernel
+int32_t attention_cache4_many(const Cache4Args &a, int head_dim, cudaStream_t stream);
 int32_t cache4_check(const sfs_cache4 *c, const char *what);
 
 }  // namespace sfs

@@ -1,0 +1,521 @@
+// Attention over a key / value cache of microscaled 4-bit numbers, many query rows per key head: the products run on the fifth-generation
+// tensor cores (tcgen05, accumulators in tensor memory), keys and values are decoded once per CTA into the operands' shared-memory layout.
+//
+// A CTA has two streams of 128 rows x 128-key tiles, so that the tensor core works on one while the other is in its softmax: two row tiles
+// that share every decoded key and value tile (PAIR), or the even and the odd key tiles of one row tile.  A row is a (query, head) pair of
+// the key head's group.  Warps 0-3 decode: a thread takes one key's codes, whose words of 8 features become 16-byte chunks of the
+// 128-byte-swizzled K-major tile (the order of features within a word is that of the decoding, the same for queries), and 8 x 8 pieces of
+// values, which come out transposed, eight tokens of a feature to a chunk.  The codes of the next tile are in flight meanwhile.  Warps 4-11
+// are the softmax of the streams, one thread per row, warp 12 issues the MMAs.
+//
+// Decoded values are exact: bits moved into bf16 (times 2^-126), one product with 2^(c - 65), so a common factor of 2^-64 remains, which
+// scores get back in 32 bits and values from the probabilities, taken 2^64 times as large.
+//
+// Only key tiles that some row sees are visited.  With few CTAs the tiles are divided over a cluster of up to 8, whose partial outputs
+// meet in shared memory, in rank order.
+#include "attention_cache4.cuh"
+#include "tc05.cuh"
+#include "gemm.cuh"
+#include <algorithm>
+
+namespace sfs {
+namespace {
+
+constexpr int kThreads = 13 * 32;                           // 4 decoding warps, 2 x 4 softmax warps, the MMA warp
+constexpr int kDecoders = 128;
+constexpr int QT = 128;                                     // rows of a stream
+constexpr int KT = 128;                                     // keys of a tile
+constexpr int kStages = 2;
+constexpr int kBars = 4 * kStages + 7;                      // K full / empty, V full / empty, S (two), P (two halves of two), exchange
+constexpr float kLazy = 8.0f;
+constexpr float kUnscale = 18446744073709551616.0f;         // 2^64
+
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <int J>
+__device__ __forceinline__ uint32_t codes_as_bf16(uint32_t w)
+{
+    const uint32_t s = J == 3 ? w : w << (12 - 4 * J);
+    const uint32_t m = J == 0 ? w << 6 : J == 1 ? w << 2 : J == 2 ? w >> 2 : w >> 6;
+    return (s & 0x80008000u) | (m & 0x01C001C0u);
+}
+__device__ __forceinline__ uint32_t factor_bits(uint32_t c) { return c > mx4::kCacheHi ? 0x7FC0u : (c + 62) << 7; }
+__device__ __forceinline__ void store_chunk(uint32_t smem, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ float load_remote(uint32_t cluster_addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 load_remote4(uint32_t cluster_addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
+    return v;
+}
+// bits k of [0, 64) with from <= k < to
+__device__ __forceinline__ unsigned long long bit_range(int from, int to)
+{
+    from = min(max(from, 0), 64); to = min(max(to, 0), 64);
+    const unsigned long long below_to = to >= 64 ? ~0ull : (1ull << to) - 1, below_from = from >= 64 ? ~0ull : (1ull << from) - 1;
+    return below_to & ~below_from;
+}
+
+template <int DH, bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1)
+attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
+{
+    constexpr int NQ = PAIR ? 2 : 1;
+    constexpr int KB = DH / 64, WORDS = DH / 8, BLOCKS = DH / 32;
+    constexpr int Q_BYTES = QT * DH * 2, K_BYTES = KT * DH * 2, V_BYTES = DH * KT * 2;
+    constexpr int ROWS = NQ * QT;
+    constexpr uint32_t TMEM_COLS = 512;                     // S / P and O of each stream: 2 x (128 + DH) columns
+
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t *sQ = smem, *sK = smem + NQ * Q_BYTES, *sV = sK + kStages * K_BYTES;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(sV + kStages * V_BYTES);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + kBars);
+    float *s_o = reinterpret_cast<float *>(sK);             // [QT][DH], this CTA's partial output once all MMAs are done
+    __shared__ int s_abort, s_any_bad, s_range[3];          // first, lo, hi over the CTA's rows
+    __shared__ int s_lo[ROWS], s_hi[ROWS], s_first[ROWS];
+    __shared__ uint8_t s_bad[4][BLOCKS][KT / 8];            // tokens whose values are NaN, by tile (four in turn) and block of features
+    __shared__ float s_max[2][QT], s_den[2][QT];
+    __shared__ float s_cm[QT], s_cl[QT];
+    __shared__ uint32_t s_nan[2][QT];
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = blockIdx.x % splits;
+    int item = blockIdx.x / splits;
+    const int row0 = (item % row_tiles) * ROWS; item /= row_tiles;
+    const int kv = item % a.n_kv, b = item / a.n_kv;
+    const int n_rows = a.n_q * a.group - row0;              // rows from this CTA's first on
+
+    const uint32_t bar_kfull = tc::smem_u32(bars), bar_kempty = bar_kfull + 8 * kStages;
+    const uint32_t bar_vfull = bar_kempty + 8 * kStages, bar_vempty = bar_vfull + 8 * kStages;
+    const uint32_t bar_s = bar_vempty + 8 * kStages /* two */, bar_p = bar_s + 16 /* + 16 w + 8 half */, bar_x = bar_s + 48;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            tc::mbar_init(bar_kfull + 8 * s, kDecoders); tc::mbar_init(bar_kempty + 8 * s, 1);
+            tc::mbar_init(bar_vfull + 8 * s, kDecoders); tc::mbar_init(bar_vempty + 8 * s, 1);
+        }
+        for (int w = 0; w < 2; ++w) { tc::mbar_init(bar_s + 8 * w, 1); tc::mbar_init(bar_p + 16 * w, QT); tc::mbar_init(bar_p + 16 * w + 8, QT); }
+        tc::mbar_init(bar_x, 2 * QT);
+        s_abort = 0; s_any_bad = 0;
+        s_range[0] = 0; s_range[1] = 0x7FFFFFFF; s_range[2] = 0;
+        tc::mbar_init_fence();
+    }
+    if (warp == 12) { tc::tmem_alloc(tc::smem_u32(tmem_slot), TMEM_COLS); tc::tmem_relinquish(); }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(tmem_slot);
+    const uint32_t tmem_S = tmem_base, tmem_O = tmem_base + 2 * KT;          // stream w: + w * KT, + w * DH
+
+    pdl_wait();
+    pdl_trigger();
+    const int length = cache4_length(a, b);
+    for (int r = threadIdx.x; r < ROWS; r += kThreads) {
+        Seen s = {0, 0, 0};
+        bool live = r < n_rows;
+        if (live) {
+            const int i = (row0 + r) / a.group;
+            long long p = (long long)length - a.n_q + i;
+            if (a.positions) { p = a.positions[(long long)b * a.n_q + i]; live = p >= 0; }
+            if (live) s = cache4_seen(a, length, p);
+        }
+        s_lo[r] = s.lo; s_hi[r] = s.hi; s_first[r] = live ? s.first : -1;      // -1: a row that is left as it was
+        if (s.hi > s.lo || s.first > 0) { atomicMax(&s_range[0], s.first); atomicMin(&s_range[1], s.lo); atomicMax(&s_range[2], s.hi); }
+    }
+    // queries, in the features' order of a decoded word: (0, 4), (1, 5), (2, 6), (3, 7)
+    for (int x = threadIdx.x; x < ROWS * WORDS; x += kThreads) {
+        const int r = x / WORDS, w = x % WORDS;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < n_rows) {
+            const int i = (row0 + r) / a.group, head = kv * a.group + (row0 + r) % a.group;
+            v = *reinterpret_cast<const uint4 *>(a.q + ((long long)b * a.n_q + i) * a.ld_q + (long long)head * DH + w * 8);
+        }
+        const int tile = r / QT, rr = r % QT;
+        store_chunk(tc::smem_u32(sQ) + tile * Q_BYTES + (w / 8) * (QT * 128) + rr * 128 + (((w % 8) ^ (rr & 7)) * 16),
+                    __byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+    }
+    fence_async_shared();
+    __syncthreads();
+    const int hi = s_range[2], lo = min(s_range[1], hi), first = min(s_range[0], lo);
+    const int n_first = (first + KT - 1) / KT, n_all = n_first + (hi - lo + KT - 1) / KT;
+    const int tile0 = (int)((long long)n_all * rank / splits), n_tiles = (int)((long long)n_all * (rank + 1) / splits) - tile0;
+    auto tile_start = [&](int j) { j += tile0; return j < n_first ? j * KT : lo + (j - n_first) * KT; };
+    auto tile_end = [&](int j) { return j + tile0 < n_first ? first : hi; };
+    const int n_streams = PAIR ? (n_tiles == 0 ? 0 : n_rows > QT ? 2 : 1) : min(n_tiles, 2);
+    auto tiles_of = [&](int w) { return w >= n_streams ? 0 : (PAIR ? n_tiles : (n_tiles - w + 1) / 2); };
+    auto key_tile = [&](int w, int i) { return PAIR ? i : 2 * i + w; };
+
+    if (warp < 4) {
+        // ---------------- decoding
+        const int n = threadIdx.x;
+        const size_t base = (size_t)b * a.capacity * a.n_kv + kv;
+        uint4 kc[WORDS / 4]; uint32_t ks[BLOCKS];
+        // values: a piece is the tokens 8 ct .. of half `kb` and a word of features; lanes of a warp: ct, and four words
+        constexpr int PIECES = WORDS / 8;                   // of a thread (16 token groups x WORDS pieces over 128 threads)
+        uint32_t vc[PIECES][8]; uint32_t vs[PIECES][8];
+        const int ct = lane & 7;
+        auto piece = [&](int e, int &kb, int &w) { const int u = (warp + 4 * e) * 4 + (lane >> 3); kb = u / WORDS; w = u % WORDS; };
+        auto fetch_k = [&](int j) {
+            const size_t at = base + (size_t)min(tile_start(j) + n, tile_end(j) - 1) * a.n_kv;
+#pragma unroll
+            for (int i = 0; i < WORDS / 4; ++i) kc[i] = reinterpret_cast<const uint4 *>(a.k_codes + at * (DH / 2))[i];
+            if constexpr (BLOCKS == 4) { const uint32_t x = *reinterpret_cast<const uint32_t *>(a.k_scales + at * 4); ks[0] = x & 255; ks[1] = (x >> 8) & 255; ks[2] = (x >> 16) & 255; ks[3] = x >> 24; }
+            else { const uint32_t x = *reinterpret_cast<const uint16_t *>(a.k_scales + at * 2); ks[0] = x & 255; ks[1] = x >> 8; }
+        };
+        auto fetch_v = [&](int j) {
+            const int j0 = tile_start(j), last = tile_end(j) - 1;
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) {
+                int kb, w;
+                piece(e, kb, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const size_t at = base + (size_t)min(j0 + kb * 64 + ct * 8 + i, last) * a.n_kv;
+                    vc[e][i] = *reinterpret_cast<const uint32_t *>(a.v_codes + at * (DH / 2) + w * 4);
+                    vs[e][i] = a.v_scales[at * BLOCKS + w / 4];
+                }
+            }
+        };
+        if (n_tiles > 0) { fetch_k(0); fetch_v(0); }
+        for (int j = 0; j < n_tiles; ++j) {
+            const int s = j % kStages;
+            const uint32_t ph = (uint32_t)(j / kStages) & 1u;
+            if (!tc::mbar_wait(bar_kempty + 8 * s, ph ^ 1u, &s_abort)) break;
+            const uint32_t sk = tc::smem_u32(sK) + s * K_BYTES + n * 128;
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w) {
+                const uint32_t x = w % 4 == 0 ? kc[w / 4].x : w % 4 == 1 ? kc[w / 4].y : w % 4 == 2 ? kc[w / 4].z : kc[w / 4].w;
+                const uint32_t f = factor_bits(ks[w / 4]), ff = f | f << 16;
+                store_chunk(sk + (w / 8) * (KT * 128) + (((w % 8) ^ (n & 7)) * 16), mul_bf16x2(codes_as_bf16<0>(x), ff), mul_bf16x2(codes_as_bf16<1>(x), ff),
+                            mul_bf16x2(codes_as_bf16<2>(x), ff), mul_bf16x2(codes_as_bf16<3>(x), ff));
+            }
+            fence_async_shared();
+            tc::mbar_arrive(bar_kfull + 8 * s);
+            if (j + 1 < n_tiles) fetch_k(j + 1);
+            if (!tc::mbar_wait(bar_vempty + 8 * s, ph ^ 1u, &s_abort)) break;
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) {
+                int kb, w;
+                piece(e, kb, w);
+                uint32_t f[4], lo4[4], hi4[4], bad = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t c0 = vs[e][2 * i], c1 = vs[e][2 * i + 1];
+                    // a NaN block counts as zeros here: it must not reach the rows that do not see its token
+                    if (c0 > mx4::kCacheHi) bad |= 1u << (2 * i);
+                    if (c1 > mx4::kCacheHi) bad |= 2u << (2 * i);
+                    f[i] = (c0 > mx4::kCacheHi ? 0u : (c0 + 62) << 7) | (c1 > mx4::kCacheHi ? 0u : (c1 + 62) << 23);
+                    lo4[i] = __byte_perm(vc[e][2 * i], vc[e][2 * i + 1], 0x5410);
+                    hi4[i] = __byte_perm(vc[e][2 * i], vc[e][2 * i + 1], 0x7632);
+                }
+                if (w % 4 == 0) s_bad[j & 3][w / 4][kb * 8 + ct] = (uint8_t)bad;
+                if (bad) s_any_bad = 1;
+                const uint32_t sv = tc::smem_u32(sV) + s * V_BYTES + kb * (DH * 128) + w * 8 * 128;
+                auto feature = [&](auto J, const uint32_t *x, int d) {
+                    store_chunk(sv + d * 128 + ((ct ^ d) * 16), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[0]), f[0]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[1]), f[1]),
+                                mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[2]), f[2]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[3]), f[3]));
+                };
+                feature(std::integral_constant<int, 0>(), lo4, 0); feature(std::integral_constant<int, 1>(), lo4, 1);
+                feature(std::integral_constant<int, 2>(), lo4, 2); feature(std::integral_constant<int, 3>(), lo4, 3);
+                feature(std::integral_constant<int, 0>(), hi4, 4); feature(std::integral_constant<int, 1>(), hi4, 5);
+                feature(std::integral_constant<int, 2>(), hi4, 6); feature(std::integral_constant<int, 3>(), hi4, 7);
+            }
+            fence_async_shared();
+            tc::mbar_arrive(bar_vfull + 8 * s);
+            if (j + 1 < n_tiles) fetch_v(j + 1);
+        }
+    } else if (warp == 12) {
+        // ---------------- MMA issuer: the whole warp runs the loop with warp-uniform operands, one elected lane issues
+        constexpr uint32_t idesc_s = tc::idesc_bf16_f32(QT, KT);
+        constexpr uint32_t idesc_o = tc::idesc_bf16_f32(QT, DH);
+        const int last = n_streams - 1;
+        auto issue_S = [&](int w, int j) {
+            const int s = j % kStages;
+            if (!__all_sync(0xffffffffu, tc::mbar_wait(bar_kfull + 8 * s, (uint32_t)(j / kStages) & 1u, &s_abort))) return false;
+            tc::tc_fence_after();
+            const uint32_t sk = tc::smem_u32(sK) + s * K_BYTES, sq = tc::smem_u32(sQ) + (PAIR ? w : 0) * Q_BYTES, d = tmem_S + (uint32_t)(w * KT);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const uint64_t dq = tc::smem_desc_sw128(sq + kb * (QT * 128)), dk = tc::smem_desc_sw128(sk + kb * (KT * 128));
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) tc::mma_bf16_elect(d, dq + (uint64_t)(kk * 2), dk + (uint64_t)(kk * 2), idesc_s, (kb | kk) != 0 ? 1u : 0u);
+            }
+            tc::mma_commit_elect(bar_s + 8 * w);
+            if (!PAIR || w == last) tc::mma_commit_elect(bar_kempty + 8 * s);
+            return true;
+        };
+        bool ok = true;
+        for (int w = 0; w < n_streams && ok; ++w) ok = issue_S(w, key_tile(w, 0));
+        const int n0 = tiles_of(0);
+        for (int i = 0; i < n0 && ok; ++i) {
+            for (int w = 0; w < n_streams && ok; ++w) {
+                if (i >= tiles_of(w)) continue;
+                const int j = key_tile(w, i), s = j % kStages;
+                ok = __all_sync(0xffffffffu, tc::mbar_wait(bar_vfull + 8 * s, (uint32_t)(j / kStages) & 1u, &s_abort));
+                const uint32_t sv = tc::smem_u32(sV) + s * V_BYTES, tp = tmem_S + (uint32_t)(w * KT), d = tmem_O + (uint32_t)(w * DH);
+#pragma unroll
+                for (int kb = 0; kb < KT / 64; ++kb) {
+                    ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(bar_p + 16 * w + 8 * kb, (uint32_t)i & 1u, &s_abort));
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    const uint64_t dv = tc::smem_desc_sw128(sv + kb * (DH * 128));
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)          // 16 keys are 8 columns of packed pairs
+                        tc::mma_bf16_ts_elect(d, tp + (uint32_t)(kb * 32 + kk * 8), dv + (uint64_t)(kk * 2), idesc_o, (i | kb | kk) != 0 ? 1u : 0u);
+                }
+                if (!ok) break;
+                if (!PAIR || w == last) tc::mma_commit_elect(bar_vempty + 8 * s);
+                if (i + 1 < tiles_of(w)) ok = issue_S(w, key_tile(w, i + 1));
+                else tc::mma_commit_elect(bar_s + 8 * w);                                   // O of the stream is complete
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------- online softmax, one thread per row, against a reference maximum that follows the true one lazily
+        const int w = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+        const int r = (PAIR ? w * QT : 0) + row;            // row of the CTA
+        const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t ts = tmem_S + (uint32_t)(w * KT) + lane_off, to = tmem_O + (uint32_t)(w * DH) + lane_off;
+        const float c = a.scale_log2 * kUnscale;
+        const int n_mine = tiles_of(w);
+        const int r_lo = s_lo[r], r_hi = s_hi[r], r_first = s_first[r];
+        float m = -INFINITY, l = 0.f;                       // reference maximum, denominator (times 2^64)
+        uint32_t nan_blocks = 0;
+        bool ok = true;
+        auto seen64 = [&](int j, int q) {                   // which of 64 keys of tile j the row sees
+            const int j0 = tile_start(j) + q * 64, end = tile_end(j);
+            return bit_range(r_lo - j0, min(r_hi, end) - j0) | bit_range(0, min(r_first, end) - j0);
+        };
+        auto nan_of = [&](int j) {                          // blocks of features in which the row sees a NaN of tile j
+            for (int blk = 0; blk < BLOCKS; ++blk)
+                for (int q = 0; q < 2; ++q) {
+                    unsigned long long bad = 0;
+                    for (int k = 0; k < 8; ++k) bad |= (unsigned long long)s_bad[j & 3][blk][q * 8 + k] << (8 * k);
+                    if (bad & seen64(j, q)) nan_blocks |= 1u << blk;
+                }
+        };
+        for (int i = 0; i < n_mine && ok; ++i) {
+            ok = tc::mbar_wait(bar_s + 8 * w, (uint32_t)i & 1u, &s_abort);      // (P V of the tile before has finished too)
+            if (!ok) break;
+            tc::tc_fence_after();
+            const int j = key_tile(w, i), j0 = tile_start(j);
+            if (i > 0 && *reinterpret_cast<volatile int *>(&s_any_bad)) nan_of(key_tile(w, i - 1));      // its values were decoded by then
+            const bool whole = j0 >= r_lo && j0 + KT <= min(r_hi, tile_end(j));
+            uint32_t v[64], pk[32];
+            auto load = [&](int q) {                        // 64 scores, those of keys that the row does not see -inf
+                tc::tmem_ld32(ts + q * 64, v); tc::tmem_ld32(ts + q * 64 + 32, v + 32);
+                tc::tmem_ld_wait32(v); tc::tmem_ld_wait32(v + 32);
+                if (!whole) {
+                    const unsigned long long in = seen64(j, q);
+                    const uint32_t in0 = (uint32_t)in, in1 = (uint32_t)(in >> 32);
+#pragma unroll
+                    for (int k = 0; k < 64; ++k)
+                        if (!(((k < 32 ? in0 : in1) >> (k & 31)) & 1u)) v[k] = 0xFF800000u;
+                }
+            };
+            auto row_max = [&]() {
+                float mx[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mx[k] = __uint_as_float(v[k]);
+#pragma unroll
+                for (int k = 4; k + 7 < 64; k += 8)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mx[e] = tc::max3(mx[e], __uint_as_float(v[k + e]), __uint_as_float(v[k + 4 + e]));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], __uint_as_float(v[60 + e]));
+                return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            };
+            unsigned long long sum2[2];
+            auto half = [&]() {                             // 64 keys: 32 columns of packed pairs
+                const float mc = m == -INFINITY ? 0.f : 64.f - m * c;
+                const unsigned long long c2 = tc::pack_f32x2(c, c), mc2 = tc::pack_f32x2(mc, mc);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    float e0, e1;
+                    tc::unpack_f32x2(tc::fma_f32x2(tc::pack_f32x2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), c2, mc2), e0, e1);
+                    const float p0 = tc::ex2_approx(e0), p1 = tc::ex2_approx(e1);
+                    sum2[k & 1] = tc::add_f32x2(sum2[k & 1], tc::pack_f32x2(p0, p1));
+                    __nv_bfloat162 hh = __floats2bfloat162_rn(p0, p1);
+                    pk[k] = *reinterpret_cast<uint32_t *>(&hh);
+                }
+            };
+            auto hand = [&](int q) {
+                tc::tmem_st32(ts + q * 32, pk);
+                tc::tmem_st_wait();
+                tc::tc_fence_before();                      // S has been read, this half of P written, O rescaled
+                tc::mbar_arrive(bar_p + 16 * w + 8 * q);
+            };
+            load(1);
+            const float m_hi = row_max();
+            load(0);
+            sum2[0] = sum2[1] = 0ull;
+            const float m_row = fmaxf(row_max(), m_hi);
+            if (i == 0) {
+                m = m_row;
+            } else {
+                const bool move = (m_row - m) * c > kLazy;
+                if (__any_sync(0xffffffffu, move)) {
+                    const float alpha = move ? tc::ex2_approx((m - m_row) * c) : 1.0f;
+#pragma unroll 1
+                    for (int q = 0; q < DH / 32; ++q) {
+                        uint32_t o[32];
+                        tc::tmem_ld32(to + q * 32, o);
+                        tc::tmem_ld_wait32(o);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                        tc::tmem_st32(to + q * 32, o);
+                    }
+                    if (move) { l *= alpha; m = m_row; }
+                }
+            }
+            half();
+            hand(0);
+            load(1);
+            half();
+            hand(1);
+            float s0, s1;
+            tc::unpack_f32x2(tc::add_f32x2(sum2[0], sum2[1]), s0, s1);
+            l += s0 + s1;
+        }
+        if (n_mine > 0) {
+            ok = ok && tc::mbar_wait(bar_s + 8 * w, (uint32_t)n_mine & 1u, &s_abort);       // the last P V
+            if (ok && *reinterpret_cast<volatile int *>(&s_any_bad)) nan_of(key_tile(w, n_mine - 1));
+        }
+        // output columns of this thread, and the factors of the streams' accumulators
+        constexpr int COLS = PAIR ? DH : DH / 2;
+        const int col0 = PAIR ? 0 : w * COLS;
+        float f0 = 0.f, f1 = 0.f;                           // PAIR: f0 of the own stream
+        bool write = ok && !s_abort;
+        if (PAIR) {
+            f0 = l == 0.f ? 0.f : kUnscale / l;
+        } else {
+            s_max[w][row] = m; s_den[w][row] = l; s_nan[w][row] = nan_blocks;
+            tc::tc_fence_before();
+            tc::mbar_arrive(bar_x);
+            write = tc::mbar_wait(bar_x, 0, &s_abort) && write && !s_abort;
+            const float m0 = s_max[0][row], m1 = s_max[1][row], mm = fmaxf(m0, m1);
+            f0 = m0 == -INFINITY ? 0.f : tc::ex2_approx((m0 - mm) * c); f1 = m1 == -INFINITY ? 0.f : tc::ex2_approx((m1 - mm) * c);
+            const float den = f0 * s_den[0][row] + f1 * s_den[1][row];
+            nan_blocks = s_nan[0][row] | s_nan[1][row];
+            if (splits == 1) {
+                const float inv = den == 0.f ? 0.f : kUnscale / den;
+                f0 *= inv; f1 *= inv;
+            } else if (w == 0) { s_cm[row] = mm; s_cl[row] = den; }
+        }
+        if (__all_sync(0xffffffffu, write)) {
+            tc::tc_fence_after();
+            const bool in = r < n_rows && r_first >= 0;
+            const uint32_t t0 = tmem_O + lane_off + (uint32_t)(PAIR ? w * DH : col0);
+            const int qi = (row0 + r) / a.group, head = kv * a.group + (row0 + r) % a.group;
+            __nv_bfloat16 *dst = a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + col0;
+#pragma unroll
+            for (int q = 0; q < COLS / 32; ++q) {
+                uint32_t o[32], o1[32];
+#pragma unroll
+                for (int k = 0; k < 32; ++k) o[k] = o1[k] = 0u;
+                if (PAIR ? n_mine > 0 : n_streams > 0) { tc::tmem_ld32(t0 + q * 32, o); tc::tmem_ld_wait32(o); }
+                if (!PAIR && n_streams > 1) { tc::tmem_ld32(t0 + DH + q * 32, o1); tc::tmem_ld_wait32(o1); }
+                const bool nan = (nan_blocks >> (col0 / 32 + q)) & 1u;
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    float x = __uint_as_float(o[k]) * f0;
+                    if (!PAIR) x = fmaf(__uint_as_float(o1[k]), f1, x);
+                    o[k] = nan ? 0x7FC00000u : __float_as_uint(x);
+                }
+                if (!PAIR && splits > 1) {
+                    // rows are 16-byte chunks in turn, rotated by the row so that a warp's stores spread over the banks
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int chunk = (col0 / 4 + q * 8 + i + row) % (DH / 4);
+                        store_chunk(tc::smem_u32(s_o + row * DH + chunk * 4), o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    }
+                } else if (in) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t wd[4];
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[8 * i + 2 * t]), __uint_as_float(o[8 * i + 2 * t + 1]));
+                            wd[t] = *reinterpret_cast<uint32_t *>(&hh);
+                        }
+                        reinterpret_cast<uint4 *>(dst)[q * 4 + i] = make_uint4(wd[0], wd[1], wd[2], wd[3]);
+                    }
+                }
+            }
+        }
+    }
+    if (!PAIR && splits > 1) {
+        // ---------------- join the ranks: each writes its share of the rows
+        tc::cluster_sync();
+        if (!s_abort) {
+            const int share = QT / splits;
+            for (int x = threadIdx.x; x < share * (DH / 4); x += kThreads) {
+                const int row = rank * share + x / (DH / 4), col = x % (DH / 4);
+                if (row >= n_rows || s_first[row] < 0) continue;
+                float mk[8], M = -INFINITY, L = 0.f;
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) { mk[k] = k < splits ? load_remote(tc::mapa(tc::smem_u32(&s_cm[row]), (uint32_t)k)) : -INFINITY; M = fmaxf(M, mk[k]); }
+                const uint32_t at = tc::smem_u32(s_o + row * DH + ((col + row) % (DH / 4)) * 4);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < splits) {
+                        const float fk = mk[k] == -INFINITY ? 0.f : tc::ex2_approx((mk[k] - M) * (a.scale_log2 * kUnscale));
+                        const float4 o = load_remote4(tc::mapa(at, (uint32_t)k));
+                        L += fk * load_remote(tc::mapa(tc::smem_u32(&s_cl[row]), (uint32_t)k));
+                        sum.x += fk * o.x; sum.y += fk * o.y; sum.z += fk * o.z; sum.w += fk * o.w;
+                    }
+                const float inv = L == 0.f ? 0.f : kUnscale / L;
+                const int qi = (row0 + row) / a.group, head = kv * a.group + (row0 + row) % a.group;
+                const __nv_bfloat162 x0 = __floats2bfloat162_rn(sum.x * inv, sum.y * inv), x1 = __floats2bfloat162_rn(sum.z * inv, sum.w * inv);
+                *reinterpret_cast<uint2 *>(a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + col * 4) =
+                    make_uint2(*reinterpret_cast<const uint32_t *>(&x0), *reinterpret_cast<const uint32_t *>(&x1));
+            }
+        }
+        tc::cluster_sync();                                 // shared memory stays until every rank has read it
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (warp == 12) { tc::tc_fence_after(); tc::tmem_dealloc(tmem_base, TMEM_COLS); }
+    if (threadIdx.x == 0 && s_abort && a.err) atomicExch(a.err, SFS_ERR_TIMEOUT);
+}
+
+template <int DH, bool PAIR>
+int32_t launch(const Cache4Args &a, int splits, cudaStream_t stream)
+{
+    constexpr int NQ = PAIR ? 2 : 1;
+    constexpr size_t shared = 1024 + (size_t)NQ * QT * DH * 2 + (size_t)kStages * 2 * KT * DH * 2 + kBars * 8 + 16;
+    const long long row_tiles = ((long long)a.n_q * a.group + NQ * QT - 1) / (NQ * QT), ctas = (long long)a.batch * a.n_kv * row_tiles * splits;
+    SFS_REQUIRE(ctas <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
+    SFS_CUDA(allow_shared(attention_cache4_many_kernel<DH, PAIR>, shared));
+    if (splits > 1) SFS_CUDA(launch_pdl_cluster(attention_cache4_many_kernel<DH, PAIR>, splits, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, splits, (int)row_tiles));
+    else SFS_CUDA(launch_pdl(attention_cache4_many_kernel<DH, PAIR>, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, 1, (int)row_tiles));
+    return SFS_OK;
+}
+
+}  // namespace
+
+int32_t attention_cache4_many(const Cache4Args &a, int head_dim, cudaStream_t stream)
+{
+    const long long row_tiles = ((long long)a.n_q * a.group + QT - 1) / QT, heads = (long long)a.batch * a.n_kv, sms = gemm_num_sms();
+    if (row_tiles > 1 && heads * ((row_tiles + 1) / 2) >= sms)               // pairs of row tiles fill the machine
+        return head_dim == 128 ? launch<128, true>(a, 1, stream) : launch<64, true>(a, 1, stream);
+    int splits = 1;                                         // up to one wave of CTAs, two key tiles for each
+    while (splits < 8 && heads * row_tiles * splits * 2 <= sms && a.capacity > splits * 2 * KT) splits *= 2;
+    return head_dim == 128 ? launch<128, false>(a, splits, stream) : launch<64, false>(a, splits, stream);
+}
+
+}  // namespace sfs
