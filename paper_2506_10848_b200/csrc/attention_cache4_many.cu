@@ -3,10 +3,10 @@
 //
 // A CTA has two streams of 128 rows x 128-key tiles, so that the tensor core works on one while the other is in its softmax: two row tiles
 // that share every decoded key and value tile (PAIR), or the even and the odd key tiles of one row tile.  A row is a (query, head) pair of
-// the key head's group.  Warps 0-3 decode: a thread takes one key's codes, whose words of 8 features become 16-byte chunks of the
-// 128-byte-swizzled K-major tile (the order of features within a word is that of the decoding, the same for queries), and 8 x 8 pieces of
-// values, which come out transposed, eight tokens of a feature to a chunk.  The codes of the next tile are in flight meanwhile.  Warps 4-11
-// are the softmax of the streams, one thread per row, warp 12 issues the MMAs.
+// the key head's group.  Warps 0-3 decode keys: a thread takes one key's codes, whose words of 8 features become 16-byte chunks of the
+// 128-byte-swizzled K-major tile (the order of features within a word is that of the decoding, the same for queries), warps 4-7 take 8 x 8
+// pieces of values, which come out transposed, eight tokens of a feature to a chunk.  The codes of the next tile are in flight meanwhile.
+// Warps 8-15 are the softmax of the streams, one thread per row, warp 16 issues the MMAs.
 //
 // Decoded values are exact: bits moved into bf16 (times 2^-126), one product with 2^(c - 65), so a common factor of 2^-64 remains, which
 // scores get back in 32 bits and values from the probabilities, taken 2^64 times as large.
@@ -21,8 +21,12 @@
 namespace sfs {
 namespace {
 
-constexpr int kThreads = 13 * 32;                           // 4 decoding warps, 2 x 4 softmax warps, the MMA warp
-constexpr int kDecoders = 128;
+constexpr int kMmaWarp = 16;
+constexpr int kThreads = (kMmaWarp + 1) * 32;               // 4 warps that decode keys, 4 values, 2 x 4 softmax warps, the MMA warp
+constexpr int kDecoders = 128;                              // threads of either kind
+// Registers: the launch's share is what five warps of a quarter of the SM can have; the decoders give some to the softmax.
+constexpr int kRegs = 96, kDecodeRegs = 64, kSoftmaxRegs = 128;
+static_assert(2 * kDecoders * kDecodeRegs + 256 * kSoftmaxRegs + 32 * kRegs <= kThreads * kRegs, "what is taken was given or is free");
 constexpr int QT = 128;                                     // rows of a stream
 constexpr int KT = 128;                                     // keys of a tile
 constexpr int kStages = 2;
@@ -113,7 +117,7 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
         s_range[0] = 0; s_range[1] = 0x7FFFFFFF; s_range[2] = 0;
         tc::mbar_init_fence();
     }
-    if (warp == 12) { tc::tmem_alloc(tc::smem_u32(tmem_slot), TMEM_COLS); tc::tmem_relinquish(); }
+    if (warp == kMmaWarp) { tc::tmem_alloc(tc::smem_u32(tmem_slot), TMEM_COLS); tc::tmem_relinquish(); }
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
@@ -158,24 +162,43 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
     auto tiles_of = [&](int w) { return w >= n_streams ? 0 : (PAIR ? n_tiles : (n_tiles - w + 1) / 2); };
     auto key_tile = [&](int w, int i) { return PAIR ? i : 2 * i + w; };
 
+    const size_t base = (size_t)b * a.capacity * a.n_kv + kv;
     if (warp < 4) {
-        // ---------------- decoding
+        // ---------------- keys: a thread decodes one key
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
         const int n = threadIdx.x;
-        const size_t base = (size_t)b * a.capacity * a.n_kv + kv;
-        uint4 kc[WORDS / 4]; uint32_t ks[BLOCKS];
-        // values: a piece is the tokens 8 ct .. of half `kb` and a word of features; lanes of a warp: ct, and four words
-        constexpr int PIECES = WORDS / 8;                   // of a thread (16 token groups x WORDS pieces over 128 threads)
-        uint32_t vc[PIECES][8]; uint32_t vs[PIECES][8];
-        const int ct = lane & 7;
-        auto piece = [&](int e, int &kb, int &w) { const int u = (warp + 4 * e) * 4 + (lane >> 3); kb = u / WORDS; w = u % WORDS; };
-        auto fetch_k = [&](int j) {
+        uint4 kc[WORDS / 4]; uint32_t ks;
+        auto fetch = [&](int j) {
             const size_t at = base + (size_t)min(tile_start(j) + n, tile_end(j) - 1) * a.n_kv;
 #pragma unroll
             for (int i = 0; i < WORDS / 4; ++i) kc[i] = reinterpret_cast<const uint4 *>(a.k_codes + at * (DH / 2))[i];
-            if constexpr (BLOCKS == 4) { const uint32_t x = *reinterpret_cast<const uint32_t *>(a.k_scales + at * 4); ks[0] = x & 255; ks[1] = (x >> 8) & 255; ks[2] = (x >> 16) & 255; ks[3] = x >> 24; }
-            else { const uint32_t x = *reinterpret_cast<const uint16_t *>(a.k_scales + at * 2); ks[0] = x & 255; ks[1] = x >> 8; }
+            if constexpr (BLOCKS == 4) ks = *reinterpret_cast<const uint32_t *>(a.k_scales + at * 4);
+            else ks = *reinterpret_cast<const uint16_t *>(a.k_scales + at * 2);
         };
-        auto fetch_v = [&](int j) {
+        if (n_tiles > 0) fetch(0);
+        for (int j = 0; j < n_tiles; ++j) {
+            const int s = j % kStages;
+            if (!tc::mbar_wait(bar_kempty + 8 * s, ((uint32_t)(j / kStages) & 1u) ^ 1u, &s_abort)) break;
+            const uint32_t sk = tc::smem_u32(sK) + s * K_BYTES + n * 128;
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w) {
+                const uint32_t x = w % 4 == 0 ? kc[w / 4].x : w % 4 == 1 ? kc[w / 4].y : w % 4 == 2 ? kc[w / 4].z : kc[w / 4].w;
+                const uint32_t f = factor_bits((ks >> (8 * (w / 4))) & 255u), ff = f | f << 16;
+                store_chunk(sk + (w / 8) * (KT * 128) + (((w % 8) ^ (n & 7)) * 16), mul_bf16x2(codes_as_bf16<0>(x), ff), mul_bf16x2(codes_as_bf16<1>(x), ff),
+                            mul_bf16x2(codes_as_bf16<2>(x), ff), mul_bf16x2(codes_as_bf16<3>(x), ff));
+            }
+            fence_async_shared();
+            tc::mbar_arrive(bar_kfull + 8 * s);
+            if (j + 1 < n_tiles) fetch(j + 1);
+        }
+    } else if (warp < 8) {
+        // ---------------- values, in pieces of eight tokens (8 ct .. of half kb of the tile) by a word of features, transposed
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
+        constexpr int PIECES = WORDS / 8;                   // of a thread (16 token groups x WORDS over 128 threads)
+        uint32_t vc[PIECES][8], vs[PIECES][4];              // codes, scales of two tokens
+        const int ct = lane & 7;                            // lanes of a warp: eight token groups, four words
+        auto piece = [&](int e, int &kb, int &w) { const int u = (warp - 4 + 4 * e) * 4 + (lane >> 3); kb = u / WORDS; w = u % WORDS; };
+        auto fetch = [&](int j) {
             const int j0 = tile_start(j), last = tile_end(j) - 1;
 #pragma unroll
             for (int e = 0; e < PIECES; ++e) {
@@ -185,27 +208,15 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
                 for (int i = 0; i < 8; ++i) {
                     const size_t at = base + (size_t)min(j0 + kb * 64 + ct * 8 + i, last) * a.n_kv;
                     vc[e][i] = *reinterpret_cast<const uint32_t *>(a.v_codes + at * (DH / 2) + w * 4);
-                    vs[e][i] = a.v_scales[at * BLOCKS + w / 4];
+                    const uint32_t c = a.v_scales[at * BLOCKS + w / 4];
+                    if (i & 1) vs[e][i / 2] |= c << 16; else vs[e][i / 2] = c;
                 }
             }
         };
-        if (n_tiles > 0) { fetch_k(0); fetch_v(0); }
+        if (n_tiles > 0) fetch(0);
         for (int j = 0; j < n_tiles; ++j) {
             const int s = j % kStages;
-            const uint32_t ph = (uint32_t)(j / kStages) & 1u;
-            if (!tc::mbar_wait(bar_kempty + 8 * s, ph ^ 1u, &s_abort)) break;
-            const uint32_t sk = tc::smem_u32(sK) + s * K_BYTES + n * 128;
-#pragma unroll
-            for (int w = 0; w < WORDS; ++w) {
-                const uint32_t x = w % 4 == 0 ? kc[w / 4].x : w % 4 == 1 ? kc[w / 4].y : w % 4 == 2 ? kc[w / 4].z : kc[w / 4].w;
-                const uint32_t f = factor_bits(ks[w / 4]), ff = f | f << 16;
-                store_chunk(sk + (w / 8) * (KT * 128) + (((w % 8) ^ (n & 7)) * 16), mul_bf16x2(codes_as_bf16<0>(x), ff), mul_bf16x2(codes_as_bf16<1>(x), ff),
-                            mul_bf16x2(codes_as_bf16<2>(x), ff), mul_bf16x2(codes_as_bf16<3>(x), ff));
-            }
-            fence_async_shared();
-            tc::mbar_arrive(bar_kfull + 8 * s);
-            if (j + 1 < n_tiles) fetch_k(j + 1);
-            if (!tc::mbar_wait(bar_vempty + 8 * s, ph ^ 1u, &s_abort)) break;
+            if (!tc::mbar_wait(bar_vempty + 8 * s, ((uint32_t)(j / kStages) & 1u) ^ 1u, &s_abort)) break;
 #pragma unroll
             for (int e = 0; e < PIECES; ++e) {
                 int kb, w;
@@ -213,11 +224,11 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
                 uint32_t f[4], lo4[4], hi4[4], bad = 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t c0 = vs[e][2 * i], c1 = vs[e][2 * i + 1];
                     // a NaN block counts as zeros here: it must not reach the rows that do not see its token
-                    if (c0 > mx4::kCacheHi) bad |= 1u << (2 * i);
-                    if (c1 > mx4::kCacheHi) bad |= 2u << (2 * i);
-                    f[i] = (c0 > mx4::kCacheHi ? 0u : (c0 + 62) << 7) | (c1 > mx4::kCacheHi ? 0u : (c1 + 62) << 23);
+                    const uint32_t c0 = vs[e][i] & 0xFFFFu, c1 = vs[e][i] >> 16;
+                    const bool bad0 = c0 > mx4::kCacheHi, bad1 = c1 > mx4::kCacheHi;
+                    bad |= (bad0 ? 1u : 0u) << (2 * i) | (bad1 ? 2u : 0u) << (2 * i);
+                    f[i] = (bad0 ? 0u : (c0 + 62) << 7) | (bad1 ? 0u : (c1 + 62) << 23);
                     lo4[i] = __byte_perm(vc[e][2 * i], vc[e][2 * i + 1], 0x5410);
                     hi4[i] = __byte_perm(vc[e][2 * i], vc[e][2 * i + 1], 0x7632);
                 }
@@ -235,9 +246,9 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
             }
             fence_async_shared();
             tc::mbar_arrive(bar_vfull + 8 * s);
-            if (j + 1 < n_tiles) fetch_v(j + 1);
+            if (j + 1 < n_tiles) fetch(j + 1);
         }
-    } else if (warp == 12) {
+    } else if (warp == kMmaWarp) {
         // ---------------- MMA issuer: the whole warp runs the loop with warp-uniform operands, one elected lane issues
         constexpr uint32_t idesc_s = tc::idesc_bf16_f32(QT, KT);
         constexpr uint32_t idesc_o = tc::idesc_bf16_f32(QT, DH);
@@ -285,7 +296,8 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
         __syncwarp();
     } else {
         // ---------------- online softmax, one thread per row, against a reference maximum that follows the true one lazily
-        const int w = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        const int w = (warp - 8) >> 2, row = (warp & 3) * 32 + lane;
         const int r = (PAIR ? w * QT : 0) + row;            // row of the CTA
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem_S + (uint32_t)(w * KT) + lane_off, to = tmem_O + (uint32_t)(w * DH) + lane_off;
@@ -489,7 +501,7 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (warp == 12) { tc::tc_fence_after(); tc::tmem_dealloc(tmem_base, TMEM_COLS); }
+    if (warp == kMmaWarp) { tc::tc_fence_after(); tc::tmem_dealloc(tmem_base, TMEM_COLS); }
     if (threadIdx.x == 0 && s_abort && a.err) atomicExch(a.err, SFS_ERR_TIMEOUT);
 }
 
@@ -501,6 +513,10 @@ int32_t launch(const Cache4Args &a, int splits, cudaStream_t stream)
     const long long row_tiles = ((long long)a.n_q * a.group + NQ * QT - 1) / (NQ * QT), ctas = (long long)a.batch * a.n_kv * row_tiles * splits;
     SFS_REQUIRE(ctas <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
     SFS_CUDA(allow_shared(attention_cache4_many_kernel<DH, PAIR>, shared));
+    // the softmax warps wait for registers that the launch must have brought: without them the kernel would not end
+    cudaFuncAttributes attr;
+    SFS_CUDA(cudaFuncGetAttributes(&attr, attention_cache4_many_kernel<DH, PAIR>));
+    SFS_REQUIRE(attr.numRegs >= kRegs, SFS_ERR_UNSUPPORTED, "attention_cache4: built with %d registers a thread, %d needed", attr.numRegs, kRegs);
     if (splits > 1) SFS_CUDA(launch_pdl_cluster(attention_cache4_many_kernel<DH, PAIR>, splits, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, splits, (int)row_tiles));
     else SFS_CUDA(launch_pdl(attention_cache4_many_kernel<DH, PAIR>, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, 1, (int)row_tiles));
     return SFS_OK;
