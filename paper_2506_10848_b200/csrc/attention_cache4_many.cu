@@ -4,8 +4,8 @@
 // A CTA has two streams of 128 rows x 128-key tiles, so that the tensor core works on one while the other is in its softmax: two row tiles
 // that share every decoded key and value tile (PAIR), or the even and the odd key tiles of one row tile.  A row is a (query, head) pair of
 // the key head's group.  Warps 0-3 decode keys: a thread takes one key's codes, whose words of 8 features become 16-byte chunks of the
-// 128-byte-swizzled K-major tile (the order of features within a word is that of the decoding, the same for queries), warps 4-7 take 8 x 8
-// pieces of values, which come out transposed, eight tokens of a feature to a chunk.  The codes of the next tile are in flight meanwhile.
+// 128-byte-swizzled K-major tile (the order of features within a word is that of the decoding, the same for queries), warps 4-7 take pieces
+// of eight tokens' values, which come out transposed, eight tokens of a feature to a chunk.  The codes of the next tile are in flight meanwhile.
 // Warps 8-15 are the softmax of the streams, one thread per row, warp 16 issues the MMAs.
 //
 // Decoded values are exact: bits moved into bf16 (times 2^-126), one product with 2^(c - 65), so a common factor of 2^-64 remains, which
@@ -167,17 +167,21 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
         // ---------------- keys: a thread decodes one key
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
         const int n = threadIdx.x;
-        uint4 kc[WORDS / 4]; uint32_t ks;
+        uint4 next[WORDS / 4], kc[WORDS / 4]; uint32_t next_s, ks;
         auto fetch = [&](int j) {
             const size_t at = base + (size_t)min(tile_start(j) + n, tile_end(j) - 1) * a.n_kv;
 #pragma unroll
-            for (int i = 0; i < WORDS / 4; ++i) kc[i] = reinterpret_cast<const uint4 *>(a.k_codes + at * (DH / 2))[i];
-            if constexpr (BLOCKS == 4) ks = *reinterpret_cast<const uint32_t *>(a.k_scales + at * 4);
-            else ks = *reinterpret_cast<const uint16_t *>(a.k_scales + at * 2);
+            for (int i = 0; i < WORDS / 4; ++i) next[i] = reinterpret_cast<const uint4 *>(a.k_codes + at * (DH / 2))[i];
+            if constexpr (BLOCKS == 4) next_s = *reinterpret_cast<const uint32_t *>(a.k_scales + at * 4);
+            else next_s = *reinterpret_cast<const uint16_t *>(a.k_scales + at * 2);
         };
         if (n_tiles > 0) fetch(0);
         for (int j = 0; j < n_tiles; ++j) {
             const int s = j % kStages;
+#pragma unroll
+            for (int i = 0; i < WORDS / 4; ++i) kc[i] = next[i];
+            ks = next_s;
+            if (j + 1 < n_tiles) fetch(j + 1);
             if (!tc::mbar_wait(bar_kempty + 8 * s, ((uint32_t)(j / kStages) & 1u) ^ 1u, &s_abort)) break;
             const uint32_t sk = tc::smem_u32(sK) + s * K_BYTES + n * 128;
 #pragma unroll
@@ -189,64 +193,63 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
             }
             fence_async_shared();
             tc::mbar_arrive(bar_kfull + 8 * s);
-            if (j + 1 < n_tiles) fetch(j + 1);
         }
     } else if (warp < 8) {
-        // ---------------- values, in pieces of eight tokens (8 ct .. of half kb of the tile) by a word of features, transposed
+        // ---------------- values, in pieces of eight tokens (8 ct .. of half kb of the tile) by 8 or 16 features, transposed
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
-        constexpr int PIECES = WORDS / 8;                   // of a thread (16 token groups x WORDS over 128 threads)
-        uint32_t vc[PIECES][8], vs[PIECES][4];              // codes, scales of two tokens
-        const int ct = lane & 7;                            // lanes of a warp: eight token groups, four words
-        auto piece = [&](int e, int &kb, int &w) { const int u = (warp - 4 + 4 * e) * 4 + (lane >> 3); kb = u / WORDS; w = u % WORDS; };
+        constexpr int PW = DH / 64;                         // words of a piece: 16 token groups x WORDS / PW pieces, one for each of 128 threads
+        uint32_t next[8][PW], vc[8][PW], next_s[8], vs[8];
+        const int ct = lane & 7, u = (warp - 4) * 4 + (lane >> 3), kb = u / (WORDS / PW), w0 = u % (WORDS / PW) * PW;
         auto fetch = [&](int j) {
-            const int j0 = tile_start(j), last = tile_end(j) - 1;
+            const int j0 = tile_start(j) + kb * 64 + ct * 8, last = tile_end(j) - 1;
 #pragma unroll
-            for (int e = 0; e < PIECES; ++e) {
-                int kb, w;
-                piece(e, kb, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const size_t at = base + (size_t)min(j0 + kb * 64 + ct * 8 + i, last) * a.n_kv;
-                    vc[e][i] = *reinterpret_cast<const uint32_t *>(a.v_codes + at * (DH / 2) + w * 4);
-                    const uint32_t c = a.v_scales[at * BLOCKS + w / 4];
-                    if (i & 1) vs[e][i / 2] |= c << 16; else vs[e][i / 2] = c;
-                }
+            for (int i = 0; i < 8; ++i) {
+                const size_t at = base + (size_t)min(j0 + i, last) * a.n_kv;
+                if constexpr (PW == 2) { const uint2 x = *reinterpret_cast<const uint2 *>(a.v_codes + at * (DH / 2) + w0 * 4); next[i][0] = x.x; next[i][PW - 1] = x.y; }
+                else next[i][0] = *reinterpret_cast<const uint32_t *>(a.v_codes + at * (DH / 2) + w0 * 4);
+                next_s[i] = a.v_scales[at * BLOCKS + w0 / 4];
             }
         };
         if (n_tiles > 0) fetch(0);
         for (int j = 0; j < n_tiles; ++j) {
             const int s = j % kStages;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int e = 0; e < PW; ++e) vc[i][e] = next[i][e];
+                vs[i] = next_s[i];
+            }
+            if (j + 1 < n_tiles) fetch(j + 1);
+            uint32_t f[4], bad = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // a NaN block counts as zeros here: it must not reach the rows that do not see its token
+                const bool bad0 = vs[2 * i] > mx4::kCacheHi, bad1 = vs[2 * i + 1] > mx4::kCacheHi;
+                bad |= (bad0 ? 1u : 0u) << (2 * i) | (bad1 ? 2u : 0u) << (2 * i);
+                f[i] = (bad0 ? 0u : (vs[2 * i] + 62) << 7) | (bad1 ? 0u : (vs[2 * i + 1] + 62) << 23);
+            }
             if (!tc::mbar_wait(bar_vempty + 8 * s, ((uint32_t)(j / kStages) & 1u) ^ 1u, &s_abort)) break;
+            if (w0 % 4 == 0) s_bad[j & 3][w0 / 4][kb * 8 + ct] = (uint8_t)bad;
+            if (bad) s_any_bad = 1;
 #pragma unroll
-            for (int e = 0; e < PIECES; ++e) {
-                int kb, w;
-                piece(e, kb, w);
-                uint32_t f[4], lo4[4], hi4[4], bad = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    // a NaN block counts as zeros here: it must not reach the rows that do not see its token
-                    const uint32_t c0 = vs[e][i] & 0xFFFFu, c1 = vs[e][i] >> 16;
-                    const bool bad0 = c0 > mx4::kCacheHi, bad1 = c1 > mx4::kCacheHi;
-                    bad |= (bad0 ? 1u : 0u) << (2 * i) | (bad1 ? 2u : 0u) << (2 * i);
-                    f[i] = (bad0 ? 0u : (c0 + 62) << 7) | (bad1 ? 0u : (c1 + 62) << 23);
-                    lo4[i] = __byte_perm(vc[e][2 * i], vc[e][2 * i + 1], 0x5410);
-                    hi4[i] = __byte_perm(vc[e][2 * i], vc[e][2 * i + 1], 0x7632);
-                }
-                if (w % 4 == 0) s_bad[j & 3][w / 4][kb * 8 + ct] = (uint8_t)bad;
-                if (bad) s_any_bad = 1;
-                const uint32_t sv = tc::smem_u32(sV) + s * V_BYTES + kb * (DH * 128) + w * 8 * 128;
-                auto feature = [&](auto J, const uint32_t *x, int d) {
+            for (int e = 0; e < PW; ++e) {
+                const uint32_t sv = tc::smem_u32(sV) + s * V_BYTES + kb * (DH * 128) + (w0 + e) * 8 * 128;
+                uint32_t x[4];
+                auto feature = [&](auto J, int d) {
                     store_chunk(sv + d * 128 + ((ct ^ d) * 16), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[0]), f[0]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[1]), f[1]),
                                 mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[2]), f[2]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[3]), f[3]));
                 };
-                feature(std::integral_constant<int, 0>(), lo4, 0); feature(std::integral_constant<int, 1>(), lo4, 1);
-                feature(std::integral_constant<int, 2>(), lo4, 2); feature(std::integral_constant<int, 3>(), lo4, 3);
-                feature(std::integral_constant<int, 0>(), hi4, 4); feature(std::integral_constant<int, 1>(), hi4, 5);
-                feature(std::integral_constant<int, 2>(), hi4, 6); feature(std::integral_constant<int, 3>(), hi4, 7);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = __byte_perm(vc[2 * i][e], vc[2 * i + 1][e], 0x5410);        // features 0-3 of both tokens
+                feature(std::integral_constant<int, 0>(), 0); feature(std::integral_constant<int, 1>(), 1);
+                feature(std::integral_constant<int, 2>(), 2); feature(std::integral_constant<int, 3>(), 3);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = __byte_perm(vc[2 * i][e], vc[2 * i + 1][e], 0x7632);        // features 4-7
+                feature(std::integral_constant<int, 0>(), 4); feature(std::integral_constant<int, 1>(), 5);
+                feature(std::integral_constant<int, 2>(), 6); feature(std::integral_constant<int, 3>(), 7);
             }
             fence_async_shared();
             tc::mbar_arrive(bar_vfull + 8 * s);
-            if (j + 1 < n_tiles) fetch(j + 1);
         }
     } else if (warp == kMmaWarp) {
         // ---------------- MMA issuer: the whole warp runs the loop with warp-uniform operands, one elected lane issues
