@@ -21,6 +21,10 @@
 namespace sfs {
 namespace {
 
+using mx4::cache_factor;
+using mx4::codes_as_bf16;
+using mx4::mul_bf16x2;
+
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kStep = 16;                                   // tokens of a warp's step
@@ -38,27 +42,11 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v)
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
-// the two codes at bits 4 j of each half of `w`, times 2^-126
-template <int J>
-__device__ __forceinline__ uint32_t codes_as_bf16(uint32_t w)
-{
-    const uint32_t s = J == 3 ? w : w << (12 - 4 * J);
-    const uint32_t m = J == 0 ? w << 6 : J == 1 ? w << 2 : J == 2 ? w >> 2 : w >> 6;
-    return (s & 0x80008000u) | (m & 0x01C001C0u);
-}
-// 2^(c - 65) as bf16 bits; scales above a cache's are NaN
-__device__ __forceinline__ uint32_t factor_bits(uint32_t c) { return c > mx4::kCacheHi ? 0x7FC0u : (c + 62) << 7; }
 
 __device__ __forceinline__ float load_remote(uint32_t cluster_addr)
 {
@@ -198,7 +186,7 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
             for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
         uint32_t f[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) { f[e] = factor_bits(cur.ks[e]); f[e] |= f[e] << 16; }
+        for (int e = 0; e < 2; ++e) { f[e] = cache_factor(cur.ks[e]); f[e] |= f[e] << 16; }
 #pragma unroll
         for (int w = 0; w < WORDS / 4; ++w) {
             const uint32_t x0 = word_k(cur, 0, w), x1 = word_k(cur, 1, w);

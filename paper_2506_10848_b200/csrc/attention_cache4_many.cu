@@ -21,6 +21,10 @@
 namespace sfs {
 namespace {
 
+using mx4::cache_factor;
+using mx4::codes_as_bf16;
+using mx4::mul_bf16x2;
+
 constexpr int kMmaWarp = 16;
 constexpr int kThreads = (kMmaWarp + 1) * 32;               // 4 warps that decode keys, 4 values, 2 x 4 softmax warps, the MMA warp
 constexpr int kDecoders = 128;                              // threads of either kind
@@ -34,20 +38,6 @@ constexpr int kBars = 4 * kStages + 7;                      // K full / empty, V
 constexpr float kLazy = 8.0f;
 constexpr float kUnscale = 18446744073709551616.0f;         // 2^64
 
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-template <int J>
-__device__ __forceinline__ uint32_t codes_as_bf16(uint32_t w)
-{
-    const uint32_t s = J == 3 ? w : w << (12 - 4 * J);
-    const uint32_t m = J == 0 ? w << 6 : J == 1 ? w << 2 : J == 2 ? w >> 2 : w >> 6;
-    return (s & 0x80008000u) | (m & 0x01C001C0u);
-}
-__device__ __forceinline__ uint32_t factor_bits(uint32_t c) { return c > mx4::kCacheHi ? 0x7FC0u : (c + 62) << 7; }
 __device__ __forceinline__ void store_chunk(uint32_t smem, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
@@ -187,7 +177,7 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
 #pragma unroll
             for (int w = 0; w < WORDS; ++w) {
                 const uint32_t x = w % 4 == 0 ? kc[w / 4].x : w % 4 == 1 ? kc[w / 4].y : w % 4 == 2 ? kc[w / 4].z : kc[w / 4].w;
-                const uint32_t f = factor_bits((ks >> (8 * (w / 4))) & 255u), ff = f | f << 16;
+                const uint32_t f = cache_factor((ks >> (8 * (w / 4))) & 255u), ff = f | f << 16;
                 store_chunk(sk + (w / 8) * (KT * 128) + (((w % 8) ^ (n & 7)) * 16), mul_bf16x2(codes_as_bf16<0>(x), ff), mul_bf16x2(codes_as_bf16<1>(x), ff),
                             mul_bf16x2(codes_as_bf16<2>(x), ff), mul_bf16x2(codes_as_bf16<3>(x), ff));
             }

@@ -11,155 +11,184 @@ namespace sfs {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnits = kThreads / 16;                       // half-warps of a CTA
+constexpr int kWarps = kThreads / 32;
 
-template <typename T> __device__ __forceinline__ float to_f32(T v);
-template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <typename T> __device__ __forceinline__ T from_f32(float v);
-template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-
-// eight values of a row from column `col` on, zeros behind the last column
-template <typename T>
-__device__ __forceinline__ void load8(const T *row, int col, int cols, bool wide, float *v)
-{
-    if (wide && col + 8 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 a = *reinterpret_cast<const float4 *>(row + col), b = *reinterpret_cast<const float4 *>(row + col + 4);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            const uint4 a = *reinterpret_cast<const uint4 *>(row + col);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+// Eight values of a row from column `col` on, zeros behind the last column; as they lie in memory, so that several loads can be in flight.
+template <typename T> struct Eight;
+template <> struct Eight<__nv_bfloat16> {
+    uint4 a;
+    __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const __nv_bfloat16 *at) { a = __ldcs(reinterpret_cast<const uint4 *>(at)); }
+    __device__ __forceinline__ void load_some(const __nv_bfloat16 *at, int n)
+    {
+        uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_bits_to_f32(w[i] & 0xFFFFu); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? to_f32<T>(row[col + i]) : 0.f;
+        for (int i = 0; i < 8; ++i) w[i] = i < n ? (uint32_t)__bfloat16_as_ushort(at[i]) : 0u;
+        a = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
     }
+    // bits of the largest magnitude as a float's; bit patterns of bf16 magnitudes are in order, NaN and infinity on top
+    __device__ __forceinline__ uint32_t largest() const
+    {
+        const uint32_t m = __vmaxu2(__vmaxu2(a.x & 0x7FFF7FFFu, a.y & 0x7FFF7FFFu), __vmaxu2(a.z & 0x7FFF7FFFu, a.w & 0x7FFF7FFFu));
+        return max(m & 0xFFFF0000u, m << 16);
+    }
+    __device__ __forceinline__ void get(float *v) const
+    {
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    }
+};
+template <> struct Eight<float> {
+    float4 a, b;
+    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void load(const float *at) { a = __ldcs(reinterpret_cast<const float4 *>(at)); b = __ldcs(reinterpret_cast<const float4 *>(at) + 1); }
+    __device__ __forceinline__ void load_some(const float *at, int n)
+    {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? at[i] : 0.f;
+        a = make_float4(v[0], v[1], v[2], v[3]); b = make_float4(v[4], v[5], v[6], v[7]);
+    }
+    __device__ __forceinline__ uint32_t largest() const
+    {
+        float v[8];
+        get(v);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+        return m;
+    }
+    __device__ __forceinline__ void get(float *v) const { v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w; }
+};
+// eight bf16 values to a row of T, n of them at a place that takes no wide store
+__device__ __forceinline__ void put(__nv_bfloat16 *at, const uint4 &v) { *reinterpret_cast<uint4 *>(at) = v; }
+__device__ __forceinline__ void put(float *at, const uint4 &v)
+{
+    reinterpret_cast<float4 *>(at)[0] = make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xFFFF0000u));
+    reinterpret_cast<float4 *>(at)[1] = make_float4(__uint_as_float(v.z << 16), __uint_as_float(v.z & 0xFFFF0000u), __uint_as_float(v.w << 16), __uint_as_float(v.w & 0xFFFF0000u));
 }
 template <typename T>
-__device__ __forceinline__ void store8(T *row, int col, int cols, bool wide, const float *v)
+__device__ __forceinline__ void put_some(T *at, const uint4 &v, int n)
 {
-    if (wide && col + 8 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4 *>(row + col) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4 *>(row + col + 4) = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            uint32_t w[4];
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t *>(&h); }
-            *reinterpret_cast<uint4 *>(row + col) = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 8; ++i)
+        if (i < n) {
+            const uint32_t h = (i & 1) ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu;
+            if constexpr (sizeof(T) == 4) at[i] = __uint_as_float(h << 16); else at[i] = __ushort_as_bfloat16((unsigned short)h);
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (col + i < cols) row[col + i] = from_f32<T>(v[i]);
-    }
 }
 
 // the four lanes of a block: its scale, and this lane's eight codes
-__device__ __forceinline__ uint32_t quantize8(float *v, int lo, int hi, int &c)
+template <typename T>
+__device__ __forceinline__ uint32_t quantize8(const Eight<T> &x, int lo, int hi, int &c)
 {
-    uint32_t a = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    uint32_t a = x.largest();
     a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
     a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
     c = mx4::scale_of(a, lo, hi);
     const float f = mx4::inverse_scale(c);
+    float v[8];
+    x.get(v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= f;
-    return c == 255 ? 0u : mx4::encode8(v);
-}
-__device__ __forceinline__ void dequantize8(uint32_t codes, int c, float *v)
-{
-    mx4::decode8(codes, v);
-    const float f = mx4::scale_value(c);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= f;
+    const uint32_t w = mx4::encode8(v);
+    return c == 255 ? 0u : w;
 }
 
 // where the four scale bytes of a row's blocks 4 q .. 4 q + 3 lie in a matrix's tiles
 __device__ __forceinline__ size_t scale_quad(int row, int q, int quads) { return ((size_t)(row >> 7) * quads + q) * 512 + (row & 31) * 16 + ((row & 127) >> 5) * 4; }
 
-// A half-warp's position, four blocks of a row, and the step to its next one without a division.
+// A warp's position, a segment of a row, and the step to its next one without a division.  A segment is 2 U quads: half-warp h takes
+// the quads h, h + 2, ..., so that a warp's loads are 512 consecutive bytes.
 struct Walk {
-    int row, quad, step_rows, step_quads, quads;
-    __device__ __forceinline__ Walk(long long first, int stride, int quads_) : quads(quads_)
+    int row, seg, step_rows, step_segs, segs;
+    __device__ __forceinline__ Walk(int first, int stride, int segs_) : segs(segs_)
     {
-        row = (int)(first / quads); quad = (int)(first - (long long)row * quads);
-        step_rows = stride / quads; step_quads = stride - step_rows * quads;
+        row = first / segs; seg = first - row * segs;
+        step_rows = stride / segs; step_segs = stride - step_rows * segs;
     }
-    __device__ __forceinline__ void next() { row += step_rows; quad += step_quads; if (quad >= quads) { quad -= quads; ++row; } }
+    __device__ __forceinline__ void next() { row += step_rows; seg += step_segs; if (seg >= segs) { seg -= segs; ++row; } }
 };
+__device__ __forceinline__ Walk warps_of_grid(int segs) { return Walk(blockIdx.x * kWarps + threadIdx.x / 32, gridDim.x * kWarps, segs); }
 
-template <typename T>
+template <typename T, int U>
 __global__ void __launch_bounds__(kThreads)
 quantize_kernel(const T *__restrict__ x, long long ldx, int rows, int cols, uint8_t *__restrict__ codes, long long ld_codes,
                 uint8_t *__restrict__ scales, int quads, int wide)
 {
     pdl_wait();
     pdl_trigger();
-    const int l = threadIdx.x & 15, blocks = (cols + 31) / 32, tile_rows = (rows + 127) / 128 * 128;
-    Walk at((long long)blockIdx.x * kUnits + threadIdx.x / 16, gridDim.x * kUnits, quads);
-    // (both halves of a warp run as long as either has work: the shuffles are the whole warp's)
-    while (__any_sync(0xffffffffu, at.row < tile_rows)) {
-        const int col = at.quad * 128 + l * 8;
-        float v[8];
-        if (at.row < rows) load8<T>(x + at.row * ldx, col, cols, wide != 0, v);
-        else { for (int i = 0; i < 8; ++i) v[i] = 0.f; }
-        int c;
-        const uint32_t word = quantize8(v, 0, 254, c);
-        const bool block_in = at.row < rows && at.quad * 4 + (l >> 2) < blocks;
-        if (block_in) *reinterpret_cast<uint32_t *>(codes + at.row * ld_codes + at.quad * 64 + l * 4) = word;
-        uint32_t s = (block_in ? (uint32_t)c : 0u) << ((l >> 2) * 8);         // the padding of the tiles holds zeros
-        s |= __shfl_xor_sync(0xffffffffu, s, 4);
-        s |= __shfl_xor_sync(0xffffffffu, s, 8);
-        if (l == 0 && at.row < tile_rows) *reinterpret_cast<uint32_t *>(scales + scale_quad(at.row, at.quad, quads)) = s;
-        at.next();
+    const int lane = threadIdx.x & 31, half = lane >> 4, l = lane & 15, tile_rows = (rows + 127) / 128 * 128, blocks = (cols + 31) / 32;
+    for (Walk at = warps_of_grid((quads + 2 * U - 1) / (2 * U)); at.row < tile_rows; at.next()) {
+        const int quad0 = at.seg * 2 * U + half, col0 = quad0 * 128 + l * 8;
+        const bool in = at.row < rows, full = in && wide && (at.seg + 1) * 2 * U * 128 <= cols;
+        const T *src = x + at.row * ldx + col0;
+        Eight<T> v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int left = cols - col0 - u * 256;
+            if (full || (in && wide && left >= 8)) v[u].load(src + u * 256);
+            else if (in && left > 0) v[u].load_some(src + u * 256, left);
+            else v[u].zero();
+        }
+        uint8_t *to = codes + at.row * ld_codes + quad0 * 64 + l * 4, *s = scales + scale_quad(at.row, quad0, quads) + (l >> 2);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            int c;
+            const uint32_t w = quantize8(v[u], 0, 254, c);
+            const bool block_in = full || (in && (quad0 + 2 * u) * 4 + (l >> 2) < blocks);
+            if (block_in) *reinterpret_cast<uint32_t *>(to + u * 128) = w;
+            if ((l & 3) == 0 && quad0 + 2 * u < quads) s[u * 1024] = block_in ? (uint8_t)c : (uint8_t)0;      // the padding of the tiles holds zeros
+        }
     }
 }
 
-template <typename T>
+template <typename T, int U>
 __global__ void __launch_bounds__(kThreads)
 dequantize_kernel(const uint8_t *__restrict__ codes, long long ld_codes, const uint8_t *__restrict__ scales, int rows, int cols, T *__restrict__ x,
                   long long ldx, int quads, int wide)
 {
     pdl_wait();
     pdl_trigger();
-    const int l = threadIdx.x & 15, blocks = (cols + 31) / 32;
-    Walk at((long long)blockIdx.x * kUnits + threadIdx.x / 16, gridDim.x * kUnits, quads);
-    while (at.row < rows) {
-        const int b = at.quad * 4 + (l >> 2);
-        if (b < blocks) {
-            float v[8];
-            dequantize8(*reinterpret_cast<const uint32_t *>(codes + at.row * ld_codes + at.quad * 64 + l * 4),
-                        scales[scale_quad(at.row, at.quad, quads) + (l >> 2)], v);
-            store8<T>(x + at.row * ldx, at.quad * 128 + l * 8, cols, wide != 0, v);
+    const int lane = threadIdx.x & 31, half = lane >> 4, l = lane & 15;
+    for (Walk at = warps_of_grid((quads + 2 * U - 1) / (2 * U)); at.row < rows; at.next()) {
+        const int quad0 = at.seg * 2 * U + half, col0 = quad0 * 128 + l * 8;
+        const uint8_t *from = codes + at.row * ld_codes + quad0 * 64 + l * 4, *s = scales + scale_quad(at.row, quad0, quads) + (l >> 2);
+        uint32_t w[U], c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            w[u] = c[u] = 0;
+            if (col0 + u * 256 < cols) { w[u] = __ldcs(reinterpret_cast<const uint32_t *>(from + u * 128)); c[u] = s[u * 1024]; }
         }
-        at.next();
+        T *to = x + at.row * ldx + col0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int left = cols - col0 - u * 256;
+            const uint4 v = mx4::decode8(w[u], c[u]);
+            if (wide && left >= 8) put(to + u * 256, v); else put_some(to + u * 256, v, left);
+        }
     }
 }
 
 // ---- the cache: a token's keys (or values) of all heads are one row of blocks, codes and scales each in one run of bytes ------------
 
-constexpr int kStoreRows = 8;                               // tokens of a CTA
+constexpr int kStoreRows = 8;                               // tokens of a CTA, at most
 
-template <typename T>
+template <typename T, int U>
 __global__ void __launch_bounds__(kThreads)
 cache_store_kernel(uint8_t *__restrict__ k_codes, uint8_t *__restrict__ k_scales, uint8_t *__restrict__ v_codes, uint8_t *__restrict__ v_scales,
                    int n_slots, int width, const T *__restrict__ k, long long ld_k, const T *__restrict__ v, long long ld_v, int wide_k, int wide_v,
-                   const int32_t *__restrict__ slots, int n_rows)
+                   const int32_t *__restrict__ slots, int n_rows, int cta_rows)
 {
     pdl_wait();
     pdl_trigger();
     __shared__ int s_slot[kStoreRows];
-    const int r0 = blockIdx.x * kStoreRows;
+    const int r0 = blockIdx.x * cta_rows;
     if (threadIdx.x < kStoreRows) {
         const int r = r0 + threadIdx.x;
-        const int slot = r < n_rows ? (slots ? slots[r] : r) : -1;
+        const int slot = r < n_rows && (int)threadIdx.x < cta_rows ? (slots ? slots[r] : r) : -1;
         s_slot[threadIdx.x] = (unsigned)slot < (unsigned)n_slots ? slot : -1;
     }
     __syncthreads();
@@ -181,25 +210,33 @@ cache_store_kernel(uint8_t *__restrict__ k_codes, uint8_t *__restrict__ k_scales
     const long long ld = keys ? ld_k : ld_v;
     const bool wide = keys ? wide_k : wide_v;
     uint8_t *codes = keys ? k_codes : v_codes, *scales = keys ? k_scales : v_scales;
-    const int blocks = width / 32, quads = (blocks + 3) / 4, l = threadIdx.x & 15;
-    Walk at(threadIdx.x / 16, kUnits, quads);
-    while (__any_sync(0xffffffffu, at.row < kStoreRows)) {
-        const int slot = at.row < kStoreRows ? s_slot[at.row] : -1, b = at.quad * 4 + (l >> 2);
-        const bool in = slot >= 0 && b < blocks;
-        float x[8];
-        if (in) load8<T>(src + (r0 + at.row) * ld, at.quad * 128 + l * 8, width, wide, x);
-        else { for (int i = 0; i < 8; ++i) x[i] = 0.f; }
-        int c;
-        const uint32_t word = quantize8(x, mx4::kCacheLo, mx4::kCacheHi, c);
-        if (in) {
-            *reinterpret_cast<uint32_t *>(codes + (size_t)slot * (width / 2) + at.quad * 64 + l * 4) = word;
-            if ((l & 3) == 0) scales[(size_t)slot * blocks + b] = (uint8_t)c;
+    const int lane = threadIdx.x & 31, half = lane >> 4, l = lane & 15, blocks = width / 32, quads = (blocks + 3) / 4;
+    for (Walk at(threadIdx.x / 32, kWarps, (quads + 2 * U - 1) / (2 * U)); at.row < cta_rows; at.next()) {
+        const int slot = s_slot[at.row];
+        if (slot < 0) continue;                             // (a warp works on one row)
+        const int quad0 = at.seg * 2 * U + half, col0 = quad0 * 128 + l * 8;
+        const T *from = src + (r0 + at.row) * ld + col0;
+        Eight<T> x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (col0 + u * 256 >= width) x[u].zero();       // (a width is whole blocks: eight values are in or out together)
+            else if (wide) x[u].load(from + u * 256);
+            else x[u].load_some(from + u * 256, 8);
         }
-        at.next();
+        uint8_t *to = codes + (size_t)slot * (width / 2) + quad0 * 64 + l * 4, *s = scales + (size_t)slot * blocks + quad0 * 4 + (l >> 2);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            int c;
+            const uint32_t w = quantize8(x[u], mx4::kCacheLo, mx4::kCacheHi, c);
+            if (col0 + u * 256 < width) {
+                *reinterpret_cast<uint32_t *>(to + u * 128) = w;
+                if ((l & 3) == 0) s[u * 8] = (uint8_t)c;
+            }
+        }
     }
 }
 
-template <typename T>
+template <typename T, int U>
 __global__ void __launch_bounds__(kThreads)
 cache_load_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restrict__ k_scales, const uint8_t *__restrict__ v_codes,
                   const uint8_t *__restrict__ v_scales, int n_slots, int width, T *__restrict__ k, long long ld_k, T *__restrict__ v, long long ld_v,
@@ -213,23 +250,72 @@ cache_load_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restrict
     const long long ld = keys ? ld_k : ld_v;
     const bool wide = keys ? wide_k : wide_v;
     const uint8_t *codes = keys ? k_codes : v_codes, *scales = keys ? k_scales : v_scales;
-    const int blocks = width / 32, quads = (blocks + 3) / 4, l = threadIdx.x & 15;
-    Walk at((long long)blockIdx.x * kUnits + threadIdx.x / 16, gridDim.x * kUnits, quads);
-    while (at.row < n_rows) {
-        const int slot = slots ? slots[at.row] : at.row, b = at.quad * 4 + (l >> 2);
-        if ((unsigned)slot < (unsigned)n_slots && b < blocks) {
-            float x[8];
-            const int c = scales[(size_t)slot * blocks + b];
-            dequantize8(*reinterpret_cast<const uint32_t *>(codes + (size_t)slot * (width / 2) + at.quad * 64 + l * 4), c > mx4::kCacheHi ? 255 : c, x);
-            store8<T>(dst + at.row * ld, at.quad * 128 + l * 8, width, wide, x);
+    const int lane = threadIdx.x & 31, half = lane >> 4, l = lane & 15, blocks = width / 32, quads = (blocks + 3) / 4;
+    for (Walk at = warps_of_grid((quads + 2 * U - 1) / (2 * U)); at.row < n_rows; at.next()) {
+        const int slot = slots ? slots[at.row] : at.row;
+        if ((unsigned)slot >= (unsigned)n_slots) continue;
+        const int quad0 = at.seg * 2 * U + half, col0 = quad0 * 128 + l * 8;
+        const uint8_t *from = codes + (size_t)slot * (width / 2) + quad0 * 64 + l * 4, *s = scales + (size_t)slot * blocks + quad0 * 4 + (l >> 2);
+        uint32_t w[U], c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            w[u] = c[u] = 0;
+            if (col0 + u * 256 < width) { w[u] = *reinterpret_cast<const uint32_t *>(from + u * 128); c[u] = s[u * 8]; }
         }
-        at.next();
+        T *to = dst + at.row * ld + col0;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (col0 + u * 256 < width) {
+                const uint4 x = mx4::decode8(w[u], c[u] > mx4::kCacheHi ? 255u : c[u]);
+                if (wide) put(to + u * 256, x); else put_some(to + u * 256, x, 8);
+            }
     }
 }
 
+// A segment of a row: 8 quads (1024 columns), four loads of a lane in flight, or 2 where rows are short.
+constexpr int kLong = 4;
+bool long_rows(int quads) { return quads > 4; }
+int segments(int quads) { return long_rows(quads) ? (quads + 2 * kLong - 1) / (2 * kLong) : (quads + 1) / 2; }
 bool wide_rows(const void *base, int64_t ld, size_t element) { return aligned_to(base, 16) && (ld * (int64_t)element) % 16 == 0; }
-// CTAs for `units` half-warps of work: up to eight on an SM, at least a few units each
-unsigned grid_for(long long units) { return (unsigned)std::max<long long>(1, std::min<long long>((units + kUnits - 1) / kUnits, (long long)gemm_num_sms() * 8)); }
+// CTAs for that many warps' segments: eight on an SM at most
+unsigned grid_for(long long segs) { return (unsigned)std::max<long long>(1, std::min<long long>((segs + kWarps - 1) / kWarps, (long long)gemm_num_sms() * 8)); }
+
+template <typename T>
+cudaError_t launch_quantize(const void *x, int64_t ldx, int rows, int cols, void *codes, int64_t ld_codes, void *scales, cudaStream_t stream)
+{
+    const int quads = (cols + 127) / 128;
+    const dim3 grid(grid_for((long long)((rows + 127) / 128 * 128) * segments(quads)));
+    return launch_pdl(long_rows(quads) ? quantize_kernel<T, kLong> : quantize_kernel<T, 1>, grid, dim3(kThreads), 0, stream, (const T *)x, (long long)ldx, rows, cols,
+                      (uint8_t *)codes, (long long)ld_codes, (uint8_t *)scales, quads, (int)wide_rows(x, ldx, sizeof(T)));
+}
+template <typename T>
+cudaError_t launch_dequantize(const void *codes, int64_t ld_codes, const void *scales, int rows, int cols, void *x, int64_t ldx, cudaStream_t stream)
+{
+    const int quads = (cols + 127) / 128;
+    const dim3 grid(grid_for((long long)rows * segments(quads)));
+    return launch_pdl(long_rows(quads) ? dequantize_kernel<T, kLong> : dequantize_kernel<T, 1>, grid, dim3(kThreads), 0, stream, (const uint8_t *)codes,
+                      (long long)ld_codes, (const uint8_t *)scales, rows, cols, (T *)x, (long long)ldx, quads, (int)wide_rows(x, ldx, sizeof(T)));
+}
+template <typename T>
+cudaError_t launch_store(const sfs_cache4 &c, const void *k, int64_t ld_k, const void *v, int64_t ld_v, const int32_t *slots, int n_rows, cudaStream_t stream)
+{
+    const int width = c.n_kv_heads * c.head_dim, quads = (width + 127) / 128;
+    // few rows: one or two for a CTA, so that they spread over the machine
+    const int cta_rows = std::min(kStoreRows, std::max(1, n_rows / gemm_num_sms()));
+    const dim3 grid((unsigned)((n_rows + cta_rows - 1) / cta_rows), 2);
+    return launch_pdl(long_rows(quads) ? cache_store_kernel<T, kLong> : cache_store_kernel<T, 1>, grid, dim3(kThreads), 0, stream, (uint8_t *)c.k_codes,
+                      (uint8_t *)c.k_scales, (uint8_t *)c.v_codes, (uint8_t *)c.v_scales, c.batch * c.capacity, width, (const T *)k, (long long)ld_k,
+                      (const T *)v, (long long)ld_v, (int)wide_rows(k, ld_k, sizeof(T)), (int)wide_rows(v, ld_v, sizeof(T)), slots, n_rows, cta_rows);
+}
+template <typename T>
+cudaError_t launch_load(const sfs_cache4 &c, const int32_t *slots, int n_rows, void *k, int64_t ld_k, void *v, int64_t ld_v, cudaStream_t stream)
+{
+    const int width = c.n_kv_heads * c.head_dim, quads = (width + 127) / 128;
+    const dim3 grid(grid_for((long long)n_rows * segments(quads)), 2);
+    return launch_pdl(long_rows(quads) ? cache_load_kernel<T, kLong> : cache_load_kernel<T, 1>, grid, dim3(kThreads), 0, stream, (const uint8_t *)c.k_codes,
+                      (const uint8_t *)c.k_scales, (const uint8_t *)c.v_codes, (const uint8_t *)c.v_scales, c.batch * c.capacity, width, (T *)k, (long long)ld_k,
+                      (T *)v, (long long)ld_v, (int)wide_rows(k, ld_k, sizeof(T)), (int)wide_rows(v, ld_v, sizeof(T)), slots, n_rows);
+}
 
 }  // namespace
 
@@ -277,16 +363,9 @@ int32_t sfs_mx4_quantize(const void *d_x, int64_t ldx, int32_t in_dtype, int32_t
 {
     const int32_t rc = check_matrix("mx4_quantize", d_x, ldx, in_dtype, rows, cols, d_codes, ld_codes, d_scales);
     if (rc != SFS_OK) return rc;
-    const int quads = (cols + 127) / 128;
-    const unsigned grid = grid_for((long long)((rows + 127) / 128 * 128) * quads);
-    const size_t element = in_dtype == SFS_LOGITS_BF16 ? 2 : 4;
-    const int wide = wide_rows(d_x, ldx, element);
-    if (in_dtype == SFS_LOGITS_BF16)
-        SFS_CUDA(launch_pdl(quantize_kernel<__nv_bfloat16>, dim3(grid), dim3(kThreads), 0, (cudaStream_t)stream, (const __nv_bfloat16 *)d_x, (long long)ldx,
-                            rows, cols, (uint8_t *)d_codes, (long long)ld_codes, (uint8_t *)d_scales, quads, wide));
-    else
-        SFS_CUDA(launch_pdl(quantize_kernel<float>, dim3(grid), dim3(kThreads), 0, (cudaStream_t)stream, (const float *)d_x, (long long)ldx,
-                            rows, cols, (uint8_t *)d_codes, (long long)ld_codes, (uint8_t *)d_scales, quads, wide));
+    SFS_REQUIRE((int64_t)rows * segments((cols + 127) / 128) < 0x7FFF0000, SFS_ERR_UNSUPPORTED, "mx4_quantize: matrix too large for one call");
+    if (in_dtype == SFS_LOGITS_BF16) SFS_CUDA(launch_quantize<__nv_bfloat16>(d_x, ldx, rows, cols, d_codes, ld_codes, d_scales, (cudaStream_t)stream));
+    else SFS_CUDA(launch_quantize<float>(d_x, ldx, rows, cols, d_codes, ld_codes, d_scales, (cudaStream_t)stream));
     return SFS_OK;
 }
 
@@ -295,16 +374,9 @@ int32_t sfs_mx4_dequantize(const void *d_codes, int64_t ld_codes, const void *d_
 {
     const int32_t rc = check_matrix("mx4_dequantize", d_x, ldx, out_dtype, rows, cols, d_codes, ld_codes, d_scales);
     if (rc != SFS_OK) return rc;
-    const int quads = (cols + 127) / 128;
-    const unsigned grid = grid_for((long long)rows * quads);
-    const size_t element = out_dtype == SFS_LOGITS_BF16 ? 2 : 4;
-    const int wide = wide_rows(d_x, ldx, element);
-    if (out_dtype == SFS_LOGITS_BF16)
-        SFS_CUDA(launch_pdl(dequantize_kernel<__nv_bfloat16>, dim3(grid), dim3(kThreads), 0, (cudaStream_t)stream, (const uint8_t *)d_codes, (long long)ld_codes,
-                            (const uint8_t *)d_scales, rows, cols, (__nv_bfloat16 *)d_x, (long long)ldx, quads, wide));
-    else
-        SFS_CUDA(launch_pdl(dequantize_kernel<float>, dim3(grid), dim3(kThreads), 0, (cudaStream_t)stream, (const uint8_t *)d_codes, (long long)ld_codes,
-                            (const uint8_t *)d_scales, rows, cols, (float *)d_x, (long long)ldx, quads, wide));
+    SFS_REQUIRE((int64_t)rows * segments((cols + 127) / 128) < 0x7FFF0000, SFS_ERR_UNSUPPORTED, "mx4_dequantize: matrix too large for one call");
+    if (out_dtype == SFS_LOGITS_BF16) SFS_CUDA(launch_dequantize<__nv_bfloat16>(d_codes, ld_codes, d_scales, rows, cols, d_x, ldx, (cudaStream_t)stream));
+    else SFS_CUDA(launch_dequantize<float>(d_codes, ld_codes, d_scales, rows, cols, d_x, ldx, (cudaStream_t)stream));
     return SFS_OK;
 }
 
@@ -319,17 +391,8 @@ int32_t sfs_cache4_store(const sfs_cache4 *cache, const void *d_k, int64_t ld_k,
     SFS_REQUIRE(aligned_to(d_slots, 4), SFS_ERR_INVALID_ARG, "cache4_store: misaligned slots");
     if ((rc = check_rows("cache4_store", cache, d_k, ld_k, in_dtype)) != SFS_OK || (rc = check_rows("cache4_store", cache, d_v, ld_v, in_dtype)) != SFS_OK) return rc;
     if (n_rows == 0) return SFS_OK;
-    const int n_slots = cache->batch * cache->capacity, width = cache->n_kv_heads * cache->head_dim;
-    const size_t element = in_dtype == SFS_LOGITS_BF16 ? 2 : 4;
-    const int wk = wide_rows(d_k, ld_k, element), wv = wide_rows(d_v, ld_v, element);
-    const dim3 grid((unsigned)((n_rows + kStoreRows - 1) / kStoreRows), 2);
-    uint8_t *kc = (uint8_t *)cache->k_codes, *ks = (uint8_t *)cache->k_scales, *vc = (uint8_t *)cache->v_codes, *vs = (uint8_t *)cache->v_scales;
-    if (in_dtype == SFS_LOGITS_BF16)
-        SFS_CUDA(launch_pdl(cache_store_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, (cudaStream_t)stream, kc, ks, vc, vs, n_slots, width,
-                            (const __nv_bfloat16 *)d_k, (long long)ld_k, (const __nv_bfloat16 *)d_v, (long long)ld_v, wk, wv, d_slots, n_rows));
-    else
-        SFS_CUDA(launch_pdl(cache_store_kernel<float>, grid, dim3(kThreads), 0, (cudaStream_t)stream, kc, ks, vc, vs, n_slots, width,
-                            (const float *)d_k, (long long)ld_k, (const float *)d_v, (long long)ld_v, wk, wv, d_slots, n_rows));
+    if (in_dtype == SFS_LOGITS_BF16) SFS_CUDA(launch_store<__nv_bfloat16>(*cache, d_k, ld_k, d_v, ld_v, d_slots, n_rows, (cudaStream_t)stream));
+    else SFS_CUDA(launch_store<float>(*cache, d_k, ld_k, d_v, ld_v, d_slots, n_rows, (cudaStream_t)stream));
     return SFS_OK;
 }
 
@@ -344,18 +407,8 @@ int32_t sfs_cache4_load(const sfs_cache4 *cache, const int32_t *d_slots, int32_t
     if (d_k && (rc = check_rows("cache4_load", cache, d_k, ld_k, out_dtype)) != SFS_OK) return rc;
     if (d_v && (rc = check_rows("cache4_load", cache, d_v, ld_v, out_dtype)) != SFS_OK) return rc;
     if (n_rows == 0 || (!d_k && !d_v)) return SFS_OK;
-    const int n_slots = cache->batch * cache->capacity, width = cache->n_kv_heads * cache->head_dim;
-    const size_t element = out_dtype == SFS_LOGITS_BF16 ? 2 : 4;
-    const int wk = wide_rows(d_k, ld_k, element), wv = wide_rows(d_v, ld_v, element);
-    const dim3 grid(grid_for((long long)n_rows * ((width + 127) / 128)), 2);
-    const uint8_t *kc = (const uint8_t *)cache->k_codes, *ks = (const uint8_t *)cache->k_scales;
-    const uint8_t *vc = (const uint8_t *)cache->v_codes, *vs = (const uint8_t *)cache->v_scales;
-    if (out_dtype == SFS_LOGITS_BF16)
-        SFS_CUDA(launch_pdl(cache_load_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, (cudaStream_t)stream, kc, ks, vc, vs, n_slots, width,
-                            (__nv_bfloat16 *)d_k, (long long)ld_k, (__nv_bfloat16 *)d_v, (long long)ld_v, wk, wv, d_slots, n_rows));
-    else
-        SFS_CUDA(launch_pdl(cache_load_kernel<float>, grid, dim3(kThreads), 0, (cudaStream_t)stream, kc, ks, vc, vs, n_slots, width,
-                            (float *)d_k, (long long)ld_k, (float *)d_v, (long long)ld_v, wk, wv, d_slots, n_rows));
+    if (out_dtype == SFS_LOGITS_BF16) SFS_CUDA(launch_load<__nv_bfloat16>(*cache, d_slots, n_rows, d_k, ld_k, d_v, ld_v, (cudaStream_t)stream));
+    else SFS_CUDA(launch_load<float>(*cache, d_slots, n_rows, d_k, ld_k, d_v, ld_v, (cudaStream_t)stream));
     return SFS_OK;
 }
 

@@ -1,7 +1,6 @@
 // Microscaled 4-bit numbers: blocks of 32 e2m1 codes with one scale byte c, which stands for 2^(c - 127).
 #pragma once
 #include "sfs_common.cuh"
-#include <cuda_fp16.h>
 
 namespace sfs {
 namespace mx4 {
@@ -18,8 +17,6 @@ __device__ __forceinline__ int scale_of(uint32_t amax_bits, int lo, int hi)
 }
 // 2^(127 - c): a normal number for every scale a finite block gets (c <= 252); 0 for the blocks that hold a NaN, whose codes are 0
 __device__ __forceinline__ float inverse_scale(int c) { return c == 255 ? 0.f : __uint_as_float((uint32_t)(254 - c) << 23); }
-// 2^(c - 127), NaN for 255
-__device__ __forceinline__ float scale_value(int c) { return __uint_as_float(c == 0 ? 0x00400000u : c == 255 ? 0x7FC00000u : (uint32_t)c << 23); }
 
 // eight values -> eight codes, the first in the lowest nibble; to nearest, ties to even, saturated at 6
 __device__ __forceinline__ uint32_t encode8(const float *y)
@@ -32,25 +29,34 @@ __device__ __forceinline__ uint32_t encode8(const float *y)
         : "=r"(r) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
     return r;
 }
-// The two codes at bits 4 j of each half of `w` as fp16 times 2^-14: sign to bit 15, the other three bits to the low end of the
+// The two codes at bits 4 j of each half of `w` as bf16 times 2^-126: the sign to bit 15, the other three bits to the low end of the
 // exponent and the high end of the mantissa, where 0.5 becomes a subnormal number of the right value.
 template <int J>
-__device__ __forceinline__ uint32_t codes_as_fp16(uint32_t w)
+__device__ __forceinline__ uint32_t codes_as_bf16(uint32_t w)
 {
     const uint32_t s = J == 3 ? w : w << (12 - 4 * J);
-    const uint32_t m = J == 0 ? w << 9 : J == 1 ? w << 5 : J == 2 ? w << 1 : w >> 3;
-    return (s & 0x80008000u) | (m & 0x0E000E00u);
+    const uint32_t m = J == 0 ? w << 6 : J == 1 ? w << 2 : J == 2 ? w >> 2 : w >> 6;
+    return (s & 0x80008000u) | (m & 0x01C001C0u);
 }
-// eight codes -> eight values without their scale
-__device__ __forceinline__ void decode8(uint32_t w, float *v)
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
 {
-    uint32_t h[4];
-    h[0] = codes_as_fp16<0>(w); h[1] = codes_as_fp16<1>(w); h[2] = codes_as_fp16<2>(w); h[3] = codes_as_fp16<3>(w);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[j]));
-        v[j] = f.x * 16384.f; v[j + 4] = f.y * 16384.f;
-    }
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// A cache's scale as the one factor that turns codes_as_bf16 into values times 2^-64: 2^(c - 65), NaN above a cache's range.
+__device__ __forceinline__ uint32_t cache_factor(uint32_t c) { return c > kCacheHi ? 0x7FC0u : (c + 62) << 7; }
+// Eight codes -> eight values as bf16, in order.  2^(c - 1) goes in as two factors that are normal numbers for every c; every value is
+// a bf16 number (the smallest, 2^-128, a subnormal one), so nothing is rounded.
+__device__ __forceinline__ uint4 decode8(uint32_t w, uint32_t c)
+{
+    const uint32_t e = c + 126;                             // c - 1 = (e >> 1) + (e - (e >> 1)) - 127
+    uint32_t f1 = ((e >> 1) + 63) << 7, f2 = (e - (e >> 1) + 64) << 7;
+    if (c == 255) f1 = 0x7FC0u;
+    f1 |= f1 << 16; f2 |= f2 << 16;
+    const uint32_t h0 = mul_bf16x2(mul_bf16x2(codes_as_bf16<0>(w), f1), f2), h1 = mul_bf16x2(mul_bf16x2(codes_as_bf16<1>(w), f1), f2);
+    const uint32_t h2 = mul_bf16x2(mul_bf16x2(codes_as_bf16<2>(w), f1), f2), h3 = mul_bf16x2(mul_bf16x2(codes_as_bf16<3>(w), f1), f2);
+    return make_uint4(__byte_perm(h0, h1, 0x5410), __byte_perm(h2, h3, 0x5410), __byte_perm(h0, h1, 0x7632), __byte_perm(h2, h3, 0x7632));
 }
 #endif
 
