@@ -29,14 +29,15 @@ __device__ __forceinline__ uint32_t encode8(const float *y)
         : "=r"(r) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
     return r;
 }
-// The two codes at bits 4 j of each half of `w` as bf16 times 2^-126: the sign to bit 15, the other three bits to the low end of the
-// exponent and the high end of the mantissa, where 0.5 becomes a subnormal number of the right value.
+// The two codes at bits 4 j of each half of `w` as bf16 times 2^-126: the sign goes to bit 15, the other three bits to the low end of the
+// exponent and the high end of the mantissa, where 0.5 becomes a subnormal number of the right value.  One multiplication puts a copy at
+// each place, a mask keeps the bits wanted: logic runs at half the rate of issue, and with two shifts instead of the multiplication (the
+// other pipe's work) it was what bounded the decoding (single tokens of four sequences of 65536: 105 us).
 template <int J>
 __device__ __forceinline__ uint32_t codes_as_bf16(uint32_t w)
 {
-    const uint32_t s = J == 3 ? w : w << (12 - 4 * J);
-    const uint32_t m = J == 0 ? w << 6 : J == 1 ? w << 2 : J == 2 ? w >> 2 : w >> 6;
-    return (s & 0x80008000u) | (m & 0x01C001C0u);
+    const uint32_t x = J >= 2 ? w >> 8 : w;                 // (shared by both of its codes)
+    return ((J & 1) ? (x & 0x00F000F0u) * 0x0104u : (x & 0x000F000Fu) * 0x1040u) & 0x81C081C0u;
 }
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
 {
