@@ -27,6 +27,7 @@ using mx4::mul_bf16x2;
 
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
+constexpr int kMaxSplits = 16;                            // CTAs of a cluster
 constexpr int kStep = 16;                                   // tokens of a warp's step
 constexpr float kLazy = 8.0f;                               // the reference maximum may lag by 2^8
 constexpr float kUnscale = 18446744073709551616.0f;         // 2^64
@@ -48,17 +49,27 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-__device__ __forceinline__ float load_remote(uint32_t cluster_addr)
+__device__ __forceinline__ void store_remote2(uint32_t cluster_addr, float x, float y)
 {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
-    return v;
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(cluster_addr), "f"(x), "f"(y) : "memory");
 }
 
-// what a warp reads of 16 tokens: raw codes and scale bytes of its lanes
-template <int DH> struct Raw;
-template <> struct Raw<128> { uint4 k[2]; uint2 v[4]; uint32_t ks[2], vs[4]; };
-template <> struct Raw<64> { uint2 k[2]; uint32_t v[4]; uint32_t ks[2], vs[4]; };
+// A warp's ring in shared memory: codes of 16 tokens a stage, copied asynchronously kDepth - 1 steps ahead.
+constexpr int kDepth = 4;
+template <int DH> struct Ring { static constexpr int kPart = kStep * DH / 2, kStage = 2 * kPart, kWarp = kDepth * kStage; };
+__device__ __forceinline__ void copy16(uint32_t smem, const void *global) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory"); }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// Row i of a tile holds token token_of(i): the four tokens whose values a quarter of the lanes read together then lie in different banks
+// (with the chunks of a token's values rotated, see fetch).
+__device__ __forceinline__ int token_of(int i) { return (i & 8) | ((i & 3) << 1) | ((i >> 2) & 1); }
+__device__ __forceinline__ int row_of(int j) { return (j & 8) | ((j >> 1) & 3) | ((j & 1) << 2); }
+
+// shared memory: the rings, in whose place the warps' partial outputs are joined
+template <int DH, int NT> struct Few {
+    static constexpr int kPartials = kWarps * 8 * NT * (DH + 4) * 4;
+    static constexpr int kWork = kPartials > kWarps * Ring<DH>::kWarp ? kPartials : kWarps * Ring<DH>::kWarp;
+};
 
 template <int DH, int NT>                                   // NT tiles of 8 query rows
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
@@ -67,12 +78,13 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
     constexpr int ROWS = 8 * NT, KS = DH / 16, WORDS = DH / 8, BLOCKS = DH / 32;
     constexpr int MT = DH / 16;                             // feature tiles of O^T
     constexpr int PITCH = DH + 4;
-    extern __shared__ float s_mem[];
+    extern __shared__ __align__(16) float s_mem[];
     float *s_part = s_mem;                                  // [kWarps][ROWS][PITCH]
-    float *s_out = s_mem + kWarps * ROWS * PITCH;           // [ROWS][DH], unnormalised, of this CTA
+    float2 *s_in = reinterpret_cast<float2 *>(s_mem + Few<DH, NT>::kWork / 4);      // [splits][per], what the ranks send
     __shared__ float s_m[kWarps][ROWS], s_l[kWarps][ROWS];  // reference maximum and denominator
     __shared__ float s_cm[ROWS], s_cl[ROWS];                // of this CTA
-    __shared__ float s_f[16][ROWS], s_inv[ROWS];
+    __shared__ float2 s_ml[kMaxSplits][ROWS];               // of all ranks: maximum (then factor) and denominator
+    __shared__ float s_inv[ROWS];
     __shared__ int s_lo[ROWS], s_hi[ROWS], s_first[ROWS], s_live[ROWS];
 
     pdl_wait();
@@ -83,8 +95,23 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
     const int row_tile = item % row_tiles; item /= row_tiles;
     const int kv = item % a.n_kv, b = item / a.n_kv;
     const int rows = min(ROWS, a.n_q * a.group - row_tile * ROWS);          // rows of this tile, query by query, the group's heads together
+    if (splits > 1) tc::cluster_arrive_relaxed();           // (waited for before anything is sent)
     const int length = cache4_length(a, b);
-
+    // the queries, as the second operand of S^T: lane (g, t) holds row g, the features of its words in pairs (j, j + 4)
+    uint32_t q[NT][KS][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = n * 8 + g;
+        const int i = (row_tile * ROWS + r) / a.group, head = kv * a.group + (row_tile * ROWS + r) % a.group;
+        const __nv_bfloat16 *src = a.q + ((long long)b * a.n_q + i) * a.ld_q + (long long)head * DH + t * (DH / 4);
+#pragma unroll
+        for (int w = 0; w < WORDS / 4; ++w) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (r < rows) x = *reinterpret_cast<const uint4 *>(src + w * 8);
+            q[n][2 * w][0] = __byte_perm(x.x, x.z, 0x5410); q[n][2 * w][1] = __byte_perm(x.x, x.z, 0x7632);
+            q[n][2 * w + 1][0] = __byte_perm(x.y, x.w, 0x5410); q[n][2 * w + 1][1] = __byte_perm(x.y, x.w, 0x7632);
+        }
+    }
     if (threadIdx.x < ROWS) {
         Seen s = {0, 0, 0};
         int live = 0;
@@ -112,21 +139,6 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
         if (s < n_first) { j0 = s * kStep; end = first; } else { j0 = lo + (s - n_first) * kStep; end = hi; }
     };
 
-    // the queries, as the second operand of S^T: lane (g, t) holds row g, the features of its words in pairs (j, j + 4)
-    uint32_t q[NT][KS][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int r = n * 8 + g;
-        const int i = (row_tile * ROWS + r) / a.group, head = kv * a.group + (row_tile * ROWS + r) % a.group;
-        const __nv_bfloat16 *src = a.q + ((long long)b * a.n_q + i) * a.ld_q + (long long)head * DH + t * (DH / 4);
-#pragma unroll
-        for (int w = 0; w < WORDS / 4; ++w) {
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (r < rows) x = *reinterpret_cast<const uint4 *>(src + w * 8);
-            q[n][2 * w][0] = __byte_perm(x.x, x.z, 0x5410); q[n][2 * w][1] = __byte_perm(x.x, x.z, 0x7632);
-            q[n][2 * w + 1][0] = __byte_perm(x.y, x.w, 0x5410); q[n][2 * w + 1][1] = __byte_perm(x.y, x.w, 0x7632);
-        }
-    }
     int r_lo[NT][2], r_hi[NT][2], r_first[NT][2];           // of rows 2 t and 2 t + 1
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -145,51 +157,72 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
     }
     const float c = a.scale_log2 * kUnscale;
 
-    // tokens of a lane: keys j0 + g and j0 + g + 8; values j0 + 2 t, + 1, + 8, + 9
+    // ---- a step's codes: lane -> token lane / chunks (and + 8 with 128 features), 16-byte chunk; its scales: lane -> token lane % 16, keys' or values'
+    constexpr int CHUNKS = DH / 32;                         // of a token
+    const uint32_t ring = tc::smem_u32(s_mem) + warp * Ring<DH>::kWarp;
     const size_t base = (size_t)b * a.capacity * a.n_kv + kv;
-    auto fetch = [&](int s, Raw<DH> &raw) {
-        int j0, end;
-        tokens_of(s, j0, end);
+    uint32_t next_scales = 0;
+    auto fetch_codes = [&](int s, int stage) {
+        if (s < my_last) {
+            int j0, end;
+            tokens_of(s, j0, end);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const size_t at = base + (size_t)min(j0 + g + 8 * e, end - 1) * a.n_kv;
-            if constexpr (DH == 128) raw.k[e] = *reinterpret_cast<const uint4 *>(a.k_codes + at * 64 + t * 16);
-            else raw.k[e] = *reinterpret_cast<const uint2 *>(a.k_codes + at * 32 + t * 8);
-            raw.ks[e] = a.k_scales[at * BLOCKS + t * BLOCKS / 4];
+            for (int e = 0; e < DH / 64; ++e) {
+                const int j = lane / CHUNKS + e * (32 / CHUNKS), chunk = lane % CHUNKS;
+                const size_t at = (base + (size_t)min(j0 + j, end - 1) * a.n_kv) * (DH / 2) + chunk * 16;
+                const uint32_t to = ring + stage * Ring<DH>::kStage;
+                copy16(to + row_of(j) * (DH / 2) + chunk * 16, a.k_codes + at);
+                copy16(to + Ring<DH>::kPart + j * (DH / 2) + (chunk ^ ((j >> 1) & (CHUNKS - 1))) * 16, a.v_codes + at);
+            }
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const size_t at = base + (size_t)min(j0 + 2 * t + (e & 1) + 8 * (e >> 1), end - 1) * a.n_kv;
-            if constexpr (DH == 128) raw.v[e] = *reinterpret_cast<const uint2 *>(a.v_codes + at * 64 + g * 8);
-            else raw.v[e] = *reinterpret_cast<const uint32_t *>(a.v_codes + at * 32 + g * 4);
-            raw.vs[e] = a.v_scales[at * BLOCKS + g * BLOCKS / 8];
-        }
+        copies_commit();
     };
-    auto word_k = [](const Raw<DH> &raw, int e, int w) -> uint32_t {
-        if constexpr (DH == 128) return w == 0 ? raw.k[e].x : w == 1 ? raw.k[e].y : w == 2 ? raw.k[e].z : raw.k[e].w;
-        else return w == 0 ? raw.k[e].x : raw.k[e].y;
+    auto fetch_scales = [&](int s) {
+        if (s < my_last) {
+            int j0, end;
+            tokens_of(s, j0, end);
+            const size_t at = base + (size_t)min(j0 + (lane & 15), end - 1) * a.n_kv;
+            const uint8_t *from = (lane < 16 ? a.k_scales : a.v_scales) + at * BLOCKS;
+            if constexpr (BLOCKS == 4) next_scales = *reinterpret_cast<const uint32_t *>(from);
+            else next_scales = *reinterpret_cast<const uint16_t *>(from);
+        }
     };
 
-    Raw<DH> raw;
     int s = my_first + warp;
-    if (s < my_last) fetch(s, raw);
-    for (; s < my_last; s += kWarps) {
-        Raw<DH> cur = raw;
-        if (s + kWarps < my_last) fetch(s + kWarps, raw);
+    fetch_scales(s);
+#pragma unroll
+    for (int d = 0; d < kDepth - 1; ++d) fetch_codes(s + d * kWarps, d);
+    for (int stage = 0; s < my_last; s += kWarps, stage = stage + 1 == kDepth ? 0 : stage + 1) {
         int j0, end;
         tokens_of(s, j0, end);
+        const uint32_t scales = next_scales;
+        copies_wait<kDepth - 2>();
+        __syncwarp();
+        fetch_codes(s + (kDepth - 1) * kWarps, stage == 0 ? kDepth - 1 : stage - 1);
+        fetch_scales(s + kWarps);
+        const uint32_t from = ring + stage * Ring<DH>::kStage;
+        uint32_t kc[2][WORDS / 4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t at = from + (g + 8 * e) * (DH / 2) + t * (DH / 8);
+            if constexpr (DH == 128) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(kc[e][0]), "=r"(kc[e][1]), "=r"(kc[e][2]), "=r"(kc[e][WORDS / 4 - 1]) : "r"(at));
+            else asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(kc[e][0]), "=r"(kc[e][WORDS / 4 - 1]) : "r"(at));
+        }
         // ---- scores
-        float sc[NT][4];
+        float sc[NT][4], sd[NT][4];                         // two chains of products
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
+            for (int e = 0; e < 4; ++e) sc[n][e] = sd[n][e] = 0.f;
         uint32_t f[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) { f[e] = cache_factor(cur.ks[e]); f[e] |= f[e] << 16; }
+        for (int e = 0; e < 2; ++e) {
+            f[e] = cache_factor((__shfl_sync(0xffffffffu, scales, token_of(g + 8 * e)) >> (8 * (t * BLOCKS / 4))) & 255u);
+            f[e] |= f[e] << 16;
+        }
 #pragma unroll
         for (int w = 0; w < WORDS / 4; ++w) {
-            const uint32_t x0 = word_k(cur, 0, w), x1 = word_k(cur, 1, w);
+            const uint32_t x0 = kc[0][w], x1 = kc[1][w];
             uint32_t A[4];
             A[0] = mul_bf16x2(codes_as_bf16<0>(x0), f[0]); A[1] = mul_bf16x2(codes_as_bf16<0>(x1), f[1]);
             A[2] = mul_bf16x2(codes_as_bf16<1>(x0), f[0]); A[3] = mul_bf16x2(codes_as_bf16<1>(x1), f[1]);
@@ -198,8 +231,12 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
             A[0] = mul_bf16x2(codes_as_bf16<2>(x0), f[0]); A[1] = mul_bf16x2(codes_as_bf16<2>(x1), f[1]);
             A[2] = mul_bf16x2(codes_as_bf16<3>(x0), f[0]); A[3] = mul_bf16x2(codes_as_bf16<3>(x1), f[1]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma_bf16(sc[n], A, q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
+            for (int n = 0; n < NT; ++n) mma_bf16(sd[n], A, q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
         }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[n][e] += sd[n][e];
         // ---- what the rows do not see
         const bool whole = j0 >= all_lo && j0 + kStep <= min(end, all_hi);
         if (!whole) {
@@ -207,7 +244,7 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int j = j0 + g + 8 * (e >> 1);
+                    const int j = j0 + token_of(g + 8 * (e >> 1));
                     const bool in = j < end && (j < r_first[n][e & 1] || (j >= r_lo[n][e & 1] && j < r_hi[n][e & 1]));
                     if (!in) sc[n][e] = -INFINITY;
                 }
@@ -241,23 +278,27 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
 #pragma unroll
         for (int n = 0; n < NT; ++n) { pb[n][0] = transpose8(pack_bf16(p[n][0], p[n][1])); pb[n][1] = transpose8(pack_bf16(p[n][2], p[n][3])); }
         // ---- values
-        uint32_t fv[2];
-        uint32_t bad = 0;
+        // rows 2 t, 2 t + 1, 2 t + 8 and 2 t + 9 of the tile
+        uint32_t fv[2], bad = 0, lo4[2][2], hi4[2][2];      // [token pair][word]: the low and the high four codes of both tokens
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const uint32_t c0 = cur.vs[2 * e], c1 = cur.vs[2 * e + 1];
+            const int j = token_of(2 * t + 8 * e), j1 = token_of(2 * t + 1 + 8 * e);
+            const uint32_t c0 = (__shfl_sync(0xffffffffu, scales, 16 + j) >> (8 * (g * BLOCKS / 8))) & 255u, c1 = (__shfl_sync(0xffffffffu, scales, 16 + j1) >> (8 * (g * BLOCKS / 8))) & 255u;
             if (c0 > mx4::kCacheHi) bad |= 1u << (2 * e);
             if (c1 > mx4::kCacheHi) bad |= 2u << (2 * e);
             fv[e] = (c0 > mx4::kCacheHi ? 0u : (c0 + 62) << 7) | (c1 > mx4::kCacheHi ? 0u : (c1 + 62) << 23);
-        }
-        uint32_t lo4[2][2], hi4[2][2];                      // [token pair][word]: the low and the high four codes of both tokens
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
+            const uint32_t at = from + Ring<DH>::kPart;
             if constexpr (DH == 128) {
-                lo4[e][0] = __byte_perm(cur.v[2 * e].x, cur.v[2 * e + 1].x, 0x5410); hi4[e][0] = __byte_perm(cur.v[2 * e].x, cur.v[2 * e + 1].x, 0x7632);
-                lo4[e][1] = __byte_perm(cur.v[2 * e].y, cur.v[2 * e + 1].y, 0x5410); hi4[e][1] = __byte_perm(cur.v[2 * e].y, cur.v[2 * e + 1].y, 0x7632);
+                uint32_t x, y, x1, y1;
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(at + j * 64 + (((g >> 1) ^ ((j >> 1) & 3)) * 16) + (g & 1) * 8));
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x1), "=r"(y1) : "r"(at + j1 * 64 + (((g >> 1) ^ ((j1 >> 1) & 3)) * 16) + (g & 1) * 8));
+                lo4[e][0] = __byte_perm(x, x1, 0x5410); hi4[e][0] = __byte_perm(x, x1, 0x7632);
+                lo4[e][1] = __byte_perm(y, y1, 0x5410); hi4[e][1] = __byte_perm(y, y1, 0x7632);
             } else {                                        // one word: its low codes are the tile's first eight features, its high codes the others
-                lo4[e][0] = __byte_perm(cur.v[2 * e], cur.v[2 * e + 1], 0x5410); lo4[e][1] = __byte_perm(cur.v[2 * e], cur.v[2 * e + 1], 0x7632);
+                uint32_t x, x1;
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(at + j * 32 + (((g >> 2) ^ ((j >> 1) & 1)) * 16) + (g & 3) * 4));
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x1) : "r"(at + j1 * 32 + (((g >> 2) ^ ((j1 >> 1) & 1)) * 16) + (g & 3) * 4));
+                lo4[e][0] = __byte_perm(x, x1, 0x5410); lo4[e][1] = __byte_perm(x, x1, 0x7632);
             }
         }
         auto product = [&](auto J, int j, const uint32_t (&x)[2][2]) {
@@ -285,7 +326,7 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
                 float in[4], count[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int j = j0 + g + 8 * (e >> 1);
+                    const int j = j0 + token_of(g + 8 * (e >> 1));
                     in[e] = j < end && (j < r_first[n][e & 1] || (j >= r_lo[n][e & 1] && j < r_hi[n][e & 1])) ? 1.f : 0.f;
                 }
                 mma_bf16(count, A, transpose8(pack_bf16(in[0], in[1])), transpose8(pack_bf16(in[2], in[3])));
@@ -298,7 +339,9 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
         }
     }
 
-    // ---- join the warps
+    // ---- join the warps (their rings make room)
+    copies_wait<0>();
+    __syncthreads();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -309,72 +352,87 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
             if (g == 0) { s_m[warp][n * 8 + 2 * t + e] = m[n][e]; s_l[warp][n * 8 + 2 * t + e] = x; }
         }
 #pragma unroll
-        for (int j = 0; j < MT; ++j)
+        for (int e = 0; e < 4; ++e) {                       // rows 2 t + (e & 1); features of the lane's first or second word (or half word)
+            const int r = n * 8 + 2 * t + (e & 1);
+            if (r < rows)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)                     // rows 2 t + (e & 1); features of the lane's first or second word (or half word)
-                s_part[(warp * ROWS + n * 8 + 2 * t + (e & 1)) * PITCH + g * (DH / 8) + (e >> 1) * (DH / 16) + j] = o[n][j][e];
+                for (int j = 0; j < MT; ++j) s_part[(warp * ROWS + r) * PITCH + g * (DH / 8) + (e >> 1) * (DH / 16) + j] = o[n][j][e];
+        }
     }
     __syncthreads();
-    if (threadIdx.x < ROWS) {
+    if ((int)threadIdx.x < rows) {
         float M = -INFINITY, L = 0.f;
+#pragma unroll
         for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w][threadIdx.x]);
+#pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             const float mw = s_m[w][threadIdx.x], fw = mw == -INFINITY ? 0.f : tc::ex2_approx(mw - M);
             L += fw * s_l[w][threadIdx.x];
             s_m[w][threadIdx.x] = fw;
         }
         s_cm[threadIdx.x] = M; s_cl[threadIdx.x] = L;
+        if (splits == 1) s_inv[threadIdx.x] = L == 0.f ? 0.f : kUnscale / L;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < ROWS * DH; i += kThreads) {
-        const int r = i / DH, d = i % DH;
-        float x = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) x += s_m[w][r] * s_part[(w * ROWS + r) * PITCH + d];
-        s_out[i] = x;
-    }
-    // ---- join the CTAs: each writes a share of the outputs
-    if (splits > 1) tc::cluster_sync(); else __syncthreads();
-    if (threadIdx.x < ROWS) {
-        float M = -INFINITY, L = 0.f;
-        for (int k = 0; k < splits; ++k) { s_f[k][threadIdx.x] = splits > 1 ? load_remote(tc::mapa(tc::smem_u32(&s_cm[threadIdx.x]), (uint32_t)k)) : s_cm[threadIdx.x]; M = fmaxf(M, s_f[k][threadIdx.x]); }
-        for (int k = 0; k < splits; ++k) {
-            const float mk = s_f[k][threadIdx.x], fk = mk == -INFINITY ? 0.f : tc::ex2_approx(mk - M);
-            L += fk * (splits > 1 ? load_remote(tc::mapa(tc::smem_u32(&s_cl[threadIdx.x]), (uint32_t)k)) : s_cl[threadIdx.x]);
-            s_f[k][threadIdx.x] = fk;
-        }
-        s_inv[threadIdx.x] = L == 0.f ? 0.f : kUnscale / L;
-    }
-    __syncthreads();
-    const int pairs = rows * DH / 2;
-    for (int i = rank * kThreads + threadIdx.x; i < pairs; i += splits * kThreads) {
+    // ---- join the CTAs: rank k finishes the pairs of features [k per, (k + 1) per) of the tile's rows; the others send it theirs
+    const int pairs = rows * DH / 2, per = (pairs + splits - 1) / splits;
+    auto finish = [&](int i, float x, float y) {
         const int r = 2 * i / DH, d = 2 * i % DH;
-        if (!s_live[r]) continue;
-        float x = 0.f, y = 0.f;
-        for (int k = 0; k < splits; ++k) {
-            const float fk = s_f[k][r];
-            if (splits > 1) {
-                const uint32_t from = tc::mapa(tc::smem_u32(&s_out[2 * i]), (uint32_t)k);
-                x += fk * load_remote(from); y += fk * load_remote(from + 4);
-            } else { x += fk * s_out[2 * i]; y += fk * s_out[2 * i + 1]; }
-        }
+        if (!s_live[r]) return;
         const int qi = (row_tile * ROWS + r) / a.group, head = kv * a.group + (row_tile * ROWS + r) % a.group;
         *reinterpret_cast<uint32_t *>(a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + d) = pack_bf16(x * s_inv[r], y * s_inv[r]);
+    };
+    if (splits > 1) {
+        tc::cluster_wait();                                 // every rank has started: its shared memory is there
+        for (int i = threadIdx.x; i < rows * splits; i += kThreads) {
+            const int r = i % rows;
+            store_remote2(tc::mapa(tc::smem_u32(&s_ml[rank][r]), (uint32_t)(i / rows)), s_cm[r], s_cl[r]);
+        }
     }
-    if (splits > 1) tc::cluster_sync();                     // shared memory stays until every rank has read it
+    for (int i = threadIdx.x; i < pairs; i += kThreads) {
+        const int r = 2 * i / DH, d = 2 * i % DH;
+        float x = 0.f, y = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float2 v = *reinterpret_cast<const float2 *>(&s_part[(w * ROWS + r) * PITCH + d]);
+            x += s_m[w][r] * v.x; y += s_m[w][r] * v.y;
+        }
+        if (splits > 1) store_remote2(tc::mapa(tc::smem_u32(&s_in[rank * per + i % per]), (uint32_t)(i / per)), x, y);
+        else finish(i, x, y);
+    }
+    if (splits > 1) {
+        tc::cluster_sync();
+        if ((int)threadIdx.x < rows) {
+            float M = -INFINITY, L = 0.f;
+            for (int k = 0; k < splits; ++k) M = fmaxf(M, s_ml[k][threadIdx.x].x);
+            for (int k = 0; k < splits; ++k) {
+                const float mk = s_ml[k][threadIdx.x].x, fk = mk == -INFINITY ? 0.f : tc::ex2_approx(mk - M);
+                L += fk * s_ml[k][threadIdx.x].y;
+                s_ml[k][threadIdx.x].x = fk;
+            }
+            s_inv[threadIdx.x] = L == 0.f ? 0.f : kUnscale / L;
+        }
+        __syncthreads();
+        for (int p = threadIdx.x; p < per && rank * per + p < pairs; p += kThreads) {
+            const int i = rank * per + p, r = 2 * i / DH;
+            float x = 0.f, y = 0.f;
+            for (int k = 0; k < splits; ++k) { const float2 v = s_in[k * per + p]; x += s_ml[k][r].x * v.x; y += s_ml[k][r].x * v.y; }
+            finish(i, x, y);
+        }
+    }
 }
 
 template <int DH, int NT>
 int32_t launch_few(const Cache4Args &a, cudaStream_t stream)
 {
     constexpr int ROWS = 8 * NT;
-    constexpr size_t shared = (size_t)(kWarps * ROWS * (DH + 4) + ROWS * DH) * 4;
+    constexpr size_t shared = Few<DH, NT>::kWork + (size_t)(ROWS * DH + 2 * kMaxSplits) * 4;
     const int row_tiles = (int)(((long long)a.n_q * a.group + ROWS - 1) / ROWS);
     const long long items = (long long)a.batch * a.n_kv * row_tiles;
     // as many CTAs as the machine holds at a time, but no fewer than two steps of 16 tokens for every warp
     const int slots = gemm_num_sms() * (NT == 1 ? 2 : 1);
     int splits = 1;
-    while (splits < 16 && items * splits * 2 <= slots && a.capacity > splits * kWarps * kStep * 2) splits *= 2;
+    while (splits < kMaxSplits && items * splits * 2 <= slots && a.capacity > splits * kWarps * kStep * 2) splits *= 2;
     SFS_REQUIRE(items * splits <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
     SFS_CUDA(allow_shared(attention_cache4_few<DH, NT>, shared));
     if (splits > 8) SFS_CUDA(cudaFuncSetAttribute(attention_cache4_few<DH, NT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
