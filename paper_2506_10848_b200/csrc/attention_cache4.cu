@@ -21,14 +21,13 @@
 namespace sfs {
 namespace {
 
-using mx4::cache_factor;
 using mx4::codes_as_bf16;
 using mx4::mul_bf16x2;
 
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kMaxSplits = 16;                            // CTAs of a cluster
-constexpr int kStep = 16;                                   // tokens of a warp's step
+constexpr int kStep = 32;                                   // tokens of a warp's step, two tiles of 16
 constexpr float kLazy = 8.0f;                               // the reference maximum may lag by 2^8
 constexpr float kUnscale = 18446744073709551616.0f;         // 2^64
 
@@ -49,80 +48,78 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-__device__ __forceinline__ void store_remote2(uint32_t cluster_addr, float x, float y)
+__device__ __forceinline__ void store_remote4(uint32_t cluster_addr, float x, float y, float z, float w)
 {
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(cluster_addr), "f"(x), "f"(y) : "memory");
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "f"(x), "f"(y), "f"(z), "f"(w) : "memory");
 }
 
-// A warp's ring in shared memory: codes of 16 tokens a stage, copied asynchronously kDepth - 1 steps ahead.
-constexpr int kDepth = 4;
-template <int DH> struct Ring { static constexpr int kPart = kStep * DH / 2, kStage = 2 * kPart, kWarp = kDepth * kStage; };
+// A warp's two stages in shared memory: codes and scales of a step's tokens, the next step's copied while the present one is worked on.
+// Behind them the present step's scales as factors, keys' as a pair of equal bf16 numbers per block, values' as one.
+template <int DH> struct Ring {
+    static constexpr int kPart = kStep * DH / 2, kScales = 2 * kPart, kStage = kScales + 2 * kStep * 4, kBlocks = DH / 32;
+    static constexpr int kKeyFactors = 2 * kStage, kValueFactors = kKeyFactors + kStep * kBlocks * 4, kWarp = kValueFactors + kStep * kBlocks * 2;
+};
 __device__ __forceinline__ void copy16(uint32_t smem, const void *global) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory"); }
+// four bytes, of which the first `bytes` are read and the others 0
+__device__ __forceinline__ void copy4(uint32_t smem, const void *global, int bytes) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem), "l"(global), "r"(bytes) : "memory"); }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// Row i of a tile holds token token_of(i): the four tokens whose values a quarter of the lanes read together then lie in different banks
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+// Row i of a tile of 16 holds token token_of(i): the four tokens whose values a quarter of the lanes read together then lie in different banks
 // (with the chunks of a token's values rotated, see fetch).
 __device__ __forceinline__ int token_of(int i) { return (i & 8) | ((i & 3) << 1) | ((i >> 2) & 1); }
 __device__ __forceinline__ int row_of(int j) { return (j & 8) | ((j >> 1) & 3) | ((j & 1) << 2); }
 
 // shared memory: the rings, in whose place the warps' partial outputs are joined
 template <int DH, int NT> struct Few {
+    static constexpr int kPerSm = 2;                        // CTAs
     static constexpr int kPartials = kWarps * 8 * NT * (DH + 4) * 4;
     static constexpr int kWork = kPartials > kWarps * Ring<DH>::kWarp ? kPartials : kWarps * Ring<DH>::kWarp;
 };
 
 template <int DH, int NT>                                   // NT tiles of 8 query rows
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
-attention_cache4_few(Cache4Args a, int splits, int row_tiles)
+__global__ void __launch_bounds__(kThreads, Few<DH, NT>::kPerSm)
+attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
 {
-    constexpr int ROWS = 8 * NT, KS = DH / 16, WORDS = DH / 8, BLOCKS = DH / 32;
+    constexpr int ROWS = 8 * NT, WORDS = DH / 8, BLOCKS = DH / 32;
     constexpr int MT = DH / 16;                             // feature tiles of O^T
     constexpr int PITCH = DH + 4;
     extern __shared__ __align__(16) float s_mem[];
     float *s_part = s_mem;                                  // [kWarps][ROWS][PITCH]
-    float2 *s_in = reinterpret_cast<float2 *>(s_mem + Few<DH, NT>::kWork / 4);      // [splits][per], what the ranks send
-    __shared__ float s_m[kWarps][ROWS], s_l[kWarps][ROWS];  // reference maximum and denominator
-    __shared__ float s_cm[ROWS], s_cl[ROWS];                // of this CTA
-    __shared__ float2 s_ml[kMaxSplits][ROWS];               // of all ranks: maximum (then factor) and denominator
-    __shared__ float s_inv[ROWS];
+    float4 *s_in = reinterpret_cast<float4 *>(s_mem + Few<DH, NT>::kWork / 4);      // [splits][ROWS][DH / 2 / splits], what the ranks send
+    __shared__ float2 s_ml[kWarps][ROWS];                   // reference maximum and denominator
     __shared__ int s_lo[ROWS], s_hi[ROWS], s_first[ROWS], s_live[ROWS];
+    __shared__ uint4 s_q[NT][WORDS / 4][32];
 
-    pdl_wait();
-    pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int rank = blockIdx.x % splits;
-    int item = blockIdx.x / splits;
+    const int splits = 1 << log_splits, rank = blockIdx.x & (splits - 1);
+    int item = blockIdx.x >> log_splits;
     const int row_tile = item % row_tiles; item /= row_tiles;
     const int kv = item % a.n_kv, b = item / a.n_kv;
     const int rows = min(ROWS, a.n_q * a.group - row_tile * ROWS);          // rows of this tile, query by query, the group's heads together
     if (splits > 1) tc::cluster_arrive_relaxed();           // (waited for before anything is sent)
-    const int length = cache4_length(a, b);
+    pdl_wait();
+    pdl_trigger();
     // the queries, as the second operand of S^T: lane (g, t) holds row g, the features of its words in pairs (j, j + 4)
-    uint32_t q[NT][KS][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int r = n * 8 + g;
+    if (warp < NT) {
+        const int r = warp * 8 + g;
         const int i = (row_tile * ROWS + r) / a.group, head = kv * a.group + (row_tile * ROWS + r) % a.group;
         const __nv_bfloat16 *src = a.q + ((long long)b * a.n_q + i) * a.ld_q + (long long)head * DH + t * (DH / 4);
+        uint4 x[WORDS / 4];
 #pragma unroll
-        for (int w = 0; w < WORDS / 4; ++w) {
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (r < rows) x = *reinterpret_cast<const uint4 *>(src + w * 8);
-            q[n][2 * w][0] = __byte_perm(x.x, x.z, 0x5410); q[n][2 * w][1] = __byte_perm(x.x, x.z, 0x7632);
-            q[n][2 * w + 1][0] = __byte_perm(x.y, x.w, 0x5410); q[n][2 * w + 1][1] = __byte_perm(x.y, x.w, 0x7632);
-        }
-    }
-    if (threadIdx.x < ROWS) {
+        for (int w = 0; w < WORDS / 4; ++w) x[w] = r < rows ? *reinterpret_cast<const uint4 *>(src + w * 8) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int w = 0; w < WORDS / 4; ++w)
+            s_q[warp][w][lane] = make_uint4(__byte_perm(x[w].x, x[w].z, 0x5410), __byte_perm(x[w].x, x[w].z, 0x7632), __byte_perm(x[w].y, x[w].w, 0x5410), __byte_perm(x[w].y, x[w].w, 0x7632));
+    } else if (warp == NT && lane < ROWS) {                 // meanwhile, what the rows see
         Seen s = {0, 0, 0};
         int live = 0;
-        if ((int)threadIdx.x < rows) {
-            const int i = (row_tile * ROWS + threadIdx.x) / a.group;
-            long long p = (long long)length - a.n_q + i;
-            live = 1;
-            if (a.positions) { p = a.positions[(long long)b * a.n_q + i]; live = p >= 0; }
-            if (live) s = cache4_seen(a, length, p);
+        if (lane < rows) {
+            const int i = (row_tile * ROWS + lane) / a.group;
+            const int given = a.positions ? a.positions[(long long)b * a.n_q + i] : 0, length = cache4_length(a, b);
+            live = given >= 0;
+            if (live) s = cache4_seen(a, length, a.positions ? (long long)given : (long long)length - a.n_q + i);
         }
-        s_first[threadIdx.x] = s.first; s_lo[threadIdx.x] = s.lo; s_hi[threadIdx.x] = s.hi; s_live[threadIdx.x] = live;
+        s_first[lane] = s.first; s_lo[lane] = s.lo; s_hi[lane] = s.hi; s_live[lane] = live;
     }
     __syncthreads();
     // what any row sees: [0, first) and [lo, hi); what all rows see: [all_lo, all_hi)
@@ -134,7 +131,7 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
     lo = min(lo, hi);
     first = min(first, lo);                                 // (one row's first tokens may lie in another row's window)
     const int n_first = (first + kStep - 1) / kStep, n_steps = n_first + (hi - lo + kStep - 1) / kStep;
-    const int my_first = (int)((long long)n_steps * rank / splits), my_last = (int)((long long)n_steps * (rank + 1) / splits);
+    const int my_first = (int)(((long long)n_steps * rank) >> log_splits), my_last = (int)(((long long)n_steps * (rank + 1)) >> log_splits);
     auto tokens_of = [&](int s, int &j0, int &end) {
         if (s < n_first) { j0 = s * kStep; end = first; } else { j0 = lo + (s - n_first) * kStep; end = hi; }
     };
@@ -157,103 +154,143 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
     }
     const float c = a.scale_log2 * kUnscale;
 
-    // ---- a step's codes: lane -> token lane / chunks (and + 8 with 128 features), 16-byte chunk; its scales: lane -> token lane % 16, keys' or values'
-    constexpr int CHUNKS = DH / 32;                         // of a token
-    const uint32_t ring = tc::smem_u32(s_mem) + warp * Ring<DH>::kWarp;
+    // ---- a step's codes: lane -> token lane / chunks (+ 32 / chunks a copy), 16-byte chunk; its scales: lane -> token
+    constexpr int CHUNKS = DH / 32, COPIES = DH / 32, HOP = 32 / CHUNKS;
+    uint8_t *ring = reinterpret_cast<uint8_t *>(s_mem) + warp * Ring<DH>::kWarp;
     const size_t base = (size_t)b * a.capacity * a.n_kv + kv;
-    uint32_t next_scales = 0;
-    auto fetch_codes = [&](int s, int stage) {
+    const int my_token = lane / CHUNKS, my_chunk = lane % CHUNKS;
+    const uint32_t token_bytes = (uint32_t)a.n_kv * (DH / 2), token_scales = (uint32_t)a.n_kv * BLOCKS;
+    const uint8_t *k_from = a.k_codes + base * (DH / 2) + my_chunk * 16, *v_from = a.v_codes + base * (DH / 2) + my_chunk * 16;
+    const uint32_t ring_at = tc::smem_u32(ring);
+    const uint32_t k_to = ring_at + row_of(my_token) * (DH / 2) + my_chunk * 16, v_to = ring_at + Ring<DH>::kPart + my_token * (DH / 2) + (my_chunk ^ ((my_token >> 1) & (CHUNKS - 1))) * 16;
+    const size_t all_scales = (size_t)a.batch * a.capacity * a.n_kv * BLOCKS;
+    const int last_token = a.capacity - 1;
+    auto fetch = [&](int s, uint32_t stage) {               // tokens behind the sequence are read too, but none behind the cache
         if (s < my_last) {
             int j0, end;
             tokens_of(s, j0, end);
 #pragma unroll
-            for (int e = 0; e < DH / 64; ++e) {
-                const int j = lane / CHUNKS + e * (32 / CHUNKS), chunk = lane % CHUNKS;
-                const size_t at = (base + (size_t)min(j0 + j, end - 1) * a.n_kv) * (DH / 2) + chunk * 16;
-                const uint32_t to = ring + stage * Ring<DH>::kStage;
-                copy16(to + row_of(j) * (DH / 2) + chunk * 16, a.k_codes + at);
-                copy16(to + Ring<DH>::kPart + j * (DH / 2) + (chunk ^ ((j >> 1) & (CHUNKS - 1))) * 16, a.v_codes + at);
+            for (int e = 0; e < COPIES; ++e) {
+                const size_t at = (size_t)(uint32_t)min(j0 + my_token + e * HOP, last_token) * token_bytes;
+                copy16(k_to + stage + e * HOP * (DH / 2), k_from + at);
+                copy16(v_to + stage + e * HOP * (DH / 2), v_from + at);
+            }
+            const size_t at = base * BLOCKS + (size_t)(uint32_t)min(j0 + lane, last_token) * token_scales;
+            const uint32_t to = ring_at + stage + Ring<DH>::kScales + lane * 4;
+            if constexpr (BLOCKS == 4) { copy4(to, a.k_scales + at, 4); copy4(to + kStep * 4, a.v_scales + at, 4); }
+            else {                                          // four bytes are two tokens' scales: ours are one half
+                const size_t at4 = at & ~(size_t)3;
+                const int bytes = (int)min((size_t)4, all_scales - at4);
+                copy4(to, a.k_scales + at4, bytes); copy4(to + kStep * 4, a.v_scales + at4, bytes);
             }
         }
         copies_commit();
     };
-    auto fetch_scales = [&](int s) {
-        if (s < my_last) {
-            int j0, end;
-            tokens_of(s, j0, end);
-            const size_t at = base + (size_t)min(j0 + (lane & 15), end - 1) * a.n_kv;
-            const uint8_t *from = (lane < 16 ? a.k_scales : a.v_scales) + at * BLOCKS;
-            if constexpr (BLOCKS == 4) next_scales = *reinterpret_cast<const uint32_t *>(from);
-            else next_scales = *reinterpret_cast<const uint16_t *>(from);
-        }
-    };
 
     int s = my_first + warp;
-    fetch_scales(s);
-#pragma unroll
-    for (int d = 0; d < kDepth - 1; ++d) fetch_codes(s + d * kWarps, d);
-    for (int stage = 0; s < my_last; s += kWarps, stage = stage + 1 == kDepth ? 0 : stage + 1) {
+    uint32_t stage = 0;
+    fetch(s, 0);
+    for (; s < my_last; s += kWarps, stage = Ring<DH>::kStage - stage) {
         int j0, end;
         tokens_of(s, j0, end);
-        const uint32_t scales = next_scales;
-        copies_wait<kDepth - 2>();
+        const uint8_t *from = ring + stage;
+        copies_wait();
+        // Scales of this lane's token as factors 2^(c - 65), two of 16 bits from one multiplication.  Where a byte is above 192, a key's
+        // factor is NaN, a value's 0, so that it does not reach the rows that do not see its token (see below).
+        uint32_t scales[2], above[2], f01[2], f23[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            scales[e] = *reinterpret_cast<const volatile uint32_t *>(from + Ring<DH>::kScales + e * kStep * 4 + lane * 4);     // this lane's own copy
+            if constexpr (BLOCKS == 2) {
+                if (((uint32_t)base + (uint32_t)min(j0 + lane, last_token) * (uint32_t)a.n_kv) & 1) scales[e] >>= 16;
+                scales[e] &= 0xFFFFu;
+            }
+            above[e] = ((scales[e] & 0x7F7F7F7Fu) + 0x3F3F3F3Fu) & scales[e] & 0x80808080u;
+            f01[e] = (__byte_perm(scales[e], 0, 0x4140) + 0x003E003Eu) * 128u;
+            f23[e] = (__byte_perm(scales[e], 0, 0x4342) + 0x003E003Eu) * 128u;
+        }
+        const bool any_above = __any_sync(0xffffffffu, (above[0] | above[1]) != 0);     // (and every lane has left the step before)
+        if (any_above)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t instead = e == 0 ? 0x7FC0u : 0u;
+                if (above[e] & 0x80u) f01[e] = (f01[e] & 0xFFFF0000u) | instead;
+                if (above[e] & 0x8000u) f01[e] = (f01[e] & 0xFFFFu) | instead << 16;
+                if (above[e] & 0x800000u) f23[e] = (f23[e] & 0xFFFF0000u) | instead;
+                if (above[e] & 0x80000000u) f23[e] = (f23[e] & 0xFFFFu) | instead << 16;
+            }
         __syncwarp();
-        fetch_codes(s + (kDepth - 1) * kWarps, stage == 0 ? kDepth - 1 : stage - 1);
-        fetch_scales(s + kWarps);
-        const uint32_t from = ring + stage * Ring<DH>::kStage;
-        uint32_t kc[2][WORDS / 4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t at = from + (g + 8 * e) * (DH / 2) + t * (DH / 8);
-            if constexpr (DH == 128) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(kc[e][0]), "=r"(kc[e][1]), "=r"(kc[e][2]), "=r"(kc[e][WORDS / 4 - 1]) : "r"(at));
-            else asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(kc[e][0]), "=r"(kc[e][WORDS / 4 - 1]) : "r"(at));
+        {
+            uint8_t *kf = ring + Ring<DH>::kKeyFactors + ((lane & 16) | row_of(lane & 15)) * BLOCKS * 4, *vf = ring + Ring<DH>::kValueFactors + lane * BLOCKS * 2;
+            const uint32_t a0 = __byte_perm(f01[0], 0, 0x1010), a1 = __byte_perm(f01[0], 0, 0x3232);
+            if constexpr (BLOCKS == 4) {
+                *reinterpret_cast<uint4 *>(kf) = make_uint4(a0, a1, __byte_perm(f23[0], 0, 0x1010), __byte_perm(f23[0], 0, 0x3232));
+                *reinterpret_cast<uint2 *>(vf) = make_uint2(f01[1], f23[1]);
+            } else {
+                *reinterpret_cast<uint2 *>(kf) = make_uint2(a0, a1);
+                *reinterpret_cast<uint32_t *>(vf) = f01[1];
+            }
         }
-        // ---- scores
-        float sc[NT][4], sd[NT][4];                         // two chains of products
+        __syncwarp();                                       // codes and factors of all lanes are there
+        fetch(s + kWarps, Ring<DH>::kStage - stage);
+        // ---- scores of both tiles
+        uint32_t kc[2][2][WORDS / 4], f[2][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[n][e] = sd[n][e] = 0.f;
-        uint32_t f[2];
+            for (int e = 0; e < 2; ++e) {
+                const int r = 16 * h + g + 8 * e;
+                const uint8_t *at = from + r * (DH / 2) + t * (DH / 8);
+                if constexpr (DH == 128) { const uint4 x = *reinterpret_cast<const uint4 *>(at); kc[h][e][0] = x.x; kc[h][e][1] = x.y; kc[h][e][WORDS / 4 - 2] = x.z; kc[h][e][WORDS / 4 - 1] = x.w; }
+                else { const uint2 x = *reinterpret_cast<const uint2 *>(at); kc[h][e][0] = x.x; kc[h][e][1] = x.y; }
+                f[h][e] = *reinterpret_cast<const uint32_t *>(ring + Ring<DH>::kKeyFactors + (r * BLOCKS + t * BLOCKS / 4) * 4);
+            }
+        float sc[2][NT][4];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            f[e] = cache_factor((__shfl_sync(0xffffffffu, scales, token_of(g + 8 * e)) >> (8 * (t * BLOCKS / 4))) & 255u);
-            f[e] |= f[e] << 16;
-        }
-#pragma unroll
-        for (int w = 0; w < WORDS / 4; ++w) {
-            const uint32_t x0 = kc[0][w], x1 = kc[1][w];
-            uint32_t A[4];
-            A[0] = mul_bf16x2(codes_as_bf16<0>(x0), f[0]); A[1] = mul_bf16x2(codes_as_bf16<0>(x1), f[1]);
-            A[2] = mul_bf16x2(codes_as_bf16<1>(x0), f[0]); A[3] = mul_bf16x2(codes_as_bf16<1>(x1), f[1]);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma_bf16(sc[n], A, q[n][2 * w][0], q[n][2 * w][1]);
-            A[0] = mul_bf16x2(codes_as_bf16<2>(x0), f[0]); A[1] = mul_bf16x2(codes_as_bf16<2>(x1), f[1]);
-            A[2] = mul_bf16x2(codes_as_bf16<3>(x0), f[0]); A[3] = mul_bf16x2(codes_as_bf16<3>(x1), f[1]);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma_bf16(sd[n], A, q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sc[n][e] += sd[n][e];
-        // ---- what the rows do not see
-        const bool whole = j0 >= all_lo && j0 + kStep <= min(end, all_hi);
-        if (!whole) {
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = j0 + token_of(g + 8 * (e >> 1));
-                    const bool in = j < end && (j < r_first[n][e & 1] || (j >= r_lo[n][e & 1] && j < r_hi[n][e & 1]));
-                    if (!in) sc[n][e] = -INFINITY;
-                }
+                for (int e = 0; e < 4; ++e) sc[h][n][e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < WORDS / 4; ++w) {
+            uint4 q[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) q[n] = s_q[n][w][lane];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t x0 = kc[h][0][w], x1 = kc[h][1][w];
+                uint32_t A[4];
+                A[0] = mul_bf16x2(codes_as_bf16<0>(x0), f[h][0]); A[1] = mul_bf16x2(codes_as_bf16<0>(x1), f[h][1]);
+                A[2] = mul_bf16x2(codes_as_bf16<1>(x0), f[h][0]); A[3] = mul_bf16x2(codes_as_bf16<1>(x1), f[h][1]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma_bf16(sc[h][n], A, q[n].x, q[n].y);
+                A[0] = mul_bf16x2(codes_as_bf16<2>(x0), f[h][0]); A[1] = mul_bf16x2(codes_as_bf16<2>(x1), f[h][1]);
+                A[2] = mul_bf16x2(codes_as_bf16<3>(x0), f[h][0]); A[3] = mul_bf16x2(codes_as_bf16<3>(x1), f[h][1]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma_bf16(sc[h][n], A, q[n].z, q[n].w);
+            }
+        }
+        // ---- what the rows do not see
+        auto sees = [&](int n, int h, int e) {
+            const int j = j0 + 16 * h + token_of(g + 8 * (e >> 1));
+            return j < end && (j < r_first[n][e & 1] || (j >= r_lo[n][e & 1] && j < r_hi[n][e & 1]));
+        };
+        if (!(j0 >= all_lo && j0 + kStep <= min(end, all_hi))) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!sees(n, h, e)) sc[h][n][e] = -INFINITY;
         }
         // ---- softmax against a reference that follows the maximum lazily
-        float p[NT][4];
+        uint32_t pb[2][NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const float x0 = fmaxf(sc[n][0], sc[n][2]) * c, x1 = fmaxf(sc[n][1], sc[n][3]) * c;
+            const float x0 = fmaxf(fmaxf(sc[0][n][0], sc[0][n][2]), fmaxf(sc[1][n][0], sc[1][n][2])) * c;
+            const float x1 = fmaxf(fmaxf(sc[0][n][1], sc[0][n][3]), fmaxf(sc[1][n][1], sc[1][n][3])) * c;
             if (__any_sync(0xffffffffu, x0 > m[n][0] + kLazy || x1 > m[n][1] + kLazy)) {
                 float y[2] = {x0, x1};
 #pragma unroll
@@ -267,80 +304,83 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
                     for (int j = 0; j < MT; ++j) { o[n][j][e] *= alpha; o[n][j][2 + e] *= alpha; }
                 }
             }
+            float ref[2];                                   // probabilities times 2^64
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float ref = m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1] - 64.f;       // probabilities times 2^64
-                p[n][e] = tc::ex2_approx(fmaf(sc[n][e], c, -ref));
+            for (int e = 0; e < 2; ++e) ref[e] = m[n][e] == -INFINITY ? 0.f : 64.f - m[n][e];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = tc::ex2_approx(fmaf(sc[h][n][e], c, ref[e & 1]));
+                l[n][0] += p[0] + p[2]; l[n][1] += p[1] + p[3];
+                pb[h][n][0] = transpose8(pack_bf16(p[0], p[1])); pb[h][n][1] = transpose8(pack_bf16(p[2], p[3]));
             }
-            l[n][0] += p[n][0] + p[n][2]; l[n][1] += p[n][1] + p[n][3];
         }
-        uint32_t pb[NT][2];
+        // ---- values: rows 2 t, 2 t + 1, 2 t + 8 and 2 t + 9 of either tile
 #pragma unroll
-        for (int n = 0; n < NT; ++n) { pb[n][0] = transpose8(pack_bf16(p[n][0], p[n][1])); pb[n][1] = transpose8(pack_bf16(p[n][2], p[n][3])); }
-        // ---- values
-        // rows 2 t, 2 t + 1, 2 t + 8 and 2 t + 9 of the tile
-        uint32_t fv[2], bad = 0, lo4[2][2], hi4[2][2];      // [token pair][word]: the low and the high four codes of both tokens
+        for (int h = 0; h < 2; ++h) {
+            uint32_t fv[2], lo4[2][2], hi4[2][2];           // [token pair][word]: the low and the high four codes of both tokens
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int j = token_of(2 * t + 8 * e), j1 = token_of(2 * t + 1 + 8 * e);
-            const uint32_t c0 = (__shfl_sync(0xffffffffu, scales, 16 + j) >> (8 * (g * BLOCKS / 8))) & 255u, c1 = (__shfl_sync(0xffffffffu, scales, 16 + j1) >> (8 * (g * BLOCKS / 8))) & 255u;
-            if (c0 > mx4::kCacheHi) bad |= 1u << (2 * e);
-            if (c1 > mx4::kCacheHi) bad |= 2u << (2 * e);
-            fv[e] = (c0 > mx4::kCacheHi ? 0u : (c0 + 62) << 7) | (c1 > mx4::kCacheHi ? 0u : (c1 + 62) << 23);
-            const uint32_t at = from + Ring<DH>::kPart;
+            for (int e = 0; e < 2; ++e) {
+                const int j = 16 * h + token_of(2 * t + 8 * e), j1 = 16 * h + token_of(2 * t + 1 + 8 * e);
+                const uint8_t *at_f = ring + Ring<DH>::kValueFactors + (g * BLOCKS / 8) * 2, *at = from + Ring<DH>::kPart;
+                fv[e] = (uint32_t)*reinterpret_cast<const uint16_t *>(at_f + j * BLOCKS * 2) | (uint32_t)*reinterpret_cast<const uint16_t *>(at_f + j1 * BLOCKS * 2) << 16;
+                if constexpr (DH == 128) {
+                    const uint2 x = *reinterpret_cast<const uint2 *>(at + j * 64 + (((g >> 1) ^ ((j >> 1) & 3)) * 16) + (g & 1) * 8);
+                    const uint2 y = *reinterpret_cast<const uint2 *>(at + j1 * 64 + (((g >> 1) ^ ((j1 >> 1) & 3)) * 16) + (g & 1) * 8);
+                    lo4[e][0] = __byte_perm(x.x, y.x, 0x5410); hi4[e][0] = __byte_perm(x.x, y.x, 0x7632);
+                    lo4[e][1] = __byte_perm(x.y, y.y, 0x5410); hi4[e][1] = __byte_perm(x.y, y.y, 0x7632);
+                } else {                                    // one word: its low codes are the tile's first eight features, its high codes the others
+                    const uint32_t x = *reinterpret_cast<const uint32_t *>(at + j * 32 + (((g >> 2) ^ ((j >> 1) & 1)) * 16) + (g & 3) * 4);
+                    const uint32_t y = *reinterpret_cast<const uint32_t *>(at + j1 * 32 + (((g >> 2) ^ ((j1 >> 1) & 1)) * 16) + (g & 3) * 4);
+                    lo4[e][0] = __byte_perm(x, y, 0x5410); lo4[e][1] = __byte_perm(x, y, 0x7632);
+                }
+            }
+            auto product = [&](auto J, int j, const uint32_t (&x)[2][2]) {
+                uint32_t A[4];
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) A[2 * e + w] = mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[e][w]), fv[e]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma_bf16(o[n][j], A, pb[h][n][0], pb[h][n][1]);
+            };
+            product(std::integral_constant<int, 0>(), 0, lo4); product(std::integral_constant<int, 1>(), 1, lo4);
+            product(std::integral_constant<int, 2>(), 2, lo4); product(std::integral_constant<int, 3>(), 3, lo4);
             if constexpr (DH == 128) {
-                uint32_t x, y, x1, y1;
-                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(at + j * 64 + (((g >> 1) ^ ((j >> 1) & 3)) * 16) + (g & 1) * 8));
-                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x1), "=r"(y1) : "r"(at + j1 * 64 + (((g >> 1) ^ ((j1 >> 1) & 3)) * 16) + (g & 1) * 8));
-                lo4[e][0] = __byte_perm(x, x1, 0x5410); hi4[e][0] = __byte_perm(x, x1, 0x7632);
-                lo4[e][1] = __byte_perm(y, y1, 0x5410); hi4[e][1] = __byte_perm(y, y1, 0x7632);
-            } else {                                        // one word: its low codes are the tile's first eight features, its high codes the others
-                uint32_t x, x1;
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(at + j * 32 + (((g >> 2) ^ ((j >> 1) & 1)) * 16) + (g & 3) * 4));
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x1) : "r"(at + j1 * 32 + (((g >> 2) ^ ((j1 >> 1) & 1)) * 16) + (g & 3) * 4));
-                lo4[e][0] = __byte_perm(x, x1, 0x5410); lo4[e][1] = __byte_perm(x, x1, 0x7632);
+                product(std::integral_constant<int, 0>(), 4, hi4); product(std::integral_constant<int, 1>(), 5, hi4);
+                product(std::integral_constant<int, 2>(), 6, hi4); product(std::integral_constant<int, 3>(), 7, hi4);
             }
-        }
-        auto product = [&](auto J, int j, const uint32_t (&x)[2][2]) {
-            uint32_t A[4];
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int w = 0; w < 2; ++w) A[2 * e + w] = mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[e][w]), fv[e]);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma_bf16(o[n][j], A, pb[n][0], pb[n][1]);
-        };
-        product(std::integral_constant<int, 0>(), 0, lo4); product(std::integral_constant<int, 1>(), 1, lo4);
-        product(std::integral_constant<int, 2>(), 2, lo4); product(std::integral_constant<int, 3>(), 3, lo4);
-        if constexpr (DH == 128) {
-            product(std::integral_constant<int, 0>(), 4, hi4); product(std::integral_constant<int, 1>(), 5, hi4);
-            product(std::integral_constant<int, 2>(), 6, hi4); product(std::integral_constant<int, 3>(), 7, hi4);
         }
         // ---- NaN blocks reach the rows that see them, and no others: how many of them a row sees, by one more product
-        if (__any_sync(0xffffffffu, bad != 0)) {
-            uint32_t A[4];
+        if (any_above) {
+            const uint32_t bit = 0x80u << (8 * (g * BLOCKS / 8));
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                uint32_t A[4];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) A[2 * e] = A[2 * e + 1] = ((bad >> (2 * e)) & 1u ? 0x3F80u : 0u) | ((bad >> (2 * e)) & 2u ? 0x3F800000u : 0u);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float in[4], count[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = j0 + token_of(g + 8 * (e >> 1));
-                    in[e] = j < end && (j < r_first[n][e & 1] || (j >= r_lo[n][e & 1] && j < r_hi[n][e & 1])) ? 1.f : 0.f;
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t b0 = __shfl_sync(0xffffffffu, above[1], 16 * h + token_of(2 * t + 8 * e)) & bit, b1 = __shfl_sync(0xffffffffu, above[1], 16 * h + token_of(2 * t + 1 + 8 * e)) & bit;
+                    A[2 * e] = A[2 * e + 1] = (b0 ? 0x3F80u : 0u) | (b1 ? 0x3F800000u : 0u);
                 }
-                mma_bf16(count, A, transpose8(pack_bf16(in[0], in[1])), transpose8(pack_bf16(in[2], in[3])));
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (count[e] != 0.f)
+                for (int n = 0; n < NT; ++n) {
+                    float in[4], count[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int j = 0; j < MT; ++j) o[n][j][e] = __uint_as_float(0x7FC00000u);
+                    for (int e = 0; e < 4; ++e) in[e] = sees(n, h, e) ? 1.f : 0.f;
+                    mma_bf16(count, A, transpose8(pack_bf16(in[0], in[1])), transpose8(pack_bf16(in[2], in[3])));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (count[e] != 0.f)
+#pragma unroll
+                            for (int j = 0; j < MT; ++j) o[n][j][e] = __uint_as_float(0x7FC00000u);
+                }
             }
         }
     }
 
     // ---- join the warps (their rings make room)
-    copies_wait<0>();
+    copies_wait();
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -349,7 +389,7 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
             float x = l[n][e];
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-            if (g == 0) { s_m[warp][n * 8 + 2 * t + e] = m[n][e]; s_l[warp][n * 8 + 2 * t + e] = x; }
+            if (g == 0) s_ml[warp][n * 8 + 2 * t + e] = make_float2(m[n][e], x);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {                       // rows 2 t + (e & 1); features of the lane's first or second word (or half word)
@@ -360,64 +400,45 @@ attention_cache4_few(Cache4Args a, int splits, int row_tiles)
         }
     }
     __syncthreads();
-    if ((int)threadIdx.x < rows) {
-        float M = -INFINITY, L = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w][threadIdx.x]);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float mw = s_m[w][threadIdx.x], fw = mw == -INFINITY ? 0.f : tc::ex2_approx(mw - M);
-            L += fw * s_l[w][threadIdx.x];
-            s_m[w][threadIdx.x] = fw;
-        }
-        s_cm[threadIdx.x] = M; s_cl[threadIdx.x] = L;
-        if (splits == 1) s_inv[threadIdx.x] = L == 0.f ? 0.f : kUnscale / L;
-    }
-    __syncthreads();
-    // ---- join the CTAs: rank k finishes the pairs of features [k per, (k + 1) per) of the tile's rows; the others send it theirs
-    const int pairs = rows * DH / 2, per = (pairs + splits - 1) / splits;
-    auto finish = [&](int i, float x, float y) {
-        const int r = 2 * i / DH, d = 2 * i % DH;
+    auto finish = [&](int r, int pair, float x, float y, float den) {
         if (!s_live[r]) return;
+        const float inv = den == 0.f ? 0.f : kUnscale / den;
         const int qi = (row_tile * ROWS + r) / a.group, head = kv * a.group + (row_tile * ROWS + r) % a.group;
-        *reinterpret_cast<uint32_t *>(a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + d) = pack_bf16(x * s_inv[r], y * s_inv[r]);
+        *reinterpret_cast<uint32_t *>(a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + 2 * pair) = pack_bf16(x * inv, y * inv);
     };
-    if (splits > 1) {
-        tc::cluster_wait();                                 // every rank has started: its shared memory is there
-        for (int i = threadIdx.x; i < rows * splits; i += kThreads) {
-            const int r = i % rows;
-            store_remote2(tc::mapa(tc::smem_u32(&s_ml[rank][r]), (uint32_t)(i / rows)), s_cm[r], s_cl[r]);
-        }
-    }
-    for (int i = threadIdx.x; i < pairs; i += kThreads) {
-        const int r = 2 * i / DH, d = 2 * i % DH;
-        float x = 0.f, y = 0.f;
+    constexpr int PAIRS = DH / 2;                           // of a row
+    if (splits > 1) tc::cluster_wait();                     // every rank has started: its shared memory is there
+    // rank k finishes the pairs [k PAIRS / splits, (k + 1) PAIRS / splits) of every row: the others send it theirs, with maximum and denominator
+    for (int i = threadIdx.x; i < rows * PAIRS; i += kThreads) {
+        const int r = i / PAIRS, pair = i % PAIRS;
+        float mw[kWarps], M = -INFINITY, L = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) { mw[w] = s_ml[w][r].x; M = fmaxf(M, mw[w]); }
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            const float2 v = *reinterpret_cast<const float2 *>(&s_part[(w * ROWS + r) * PITCH + d]);
-            x += s_m[w][r] * v.x; y += s_m[w][r] * v.y;
+            const float f = mw[w] == -INFINITY ? 0.f : tc::ex2_approx(mw[w] - M);
+            const float2 v = *reinterpret_cast<const float2 *>(&s_part[(w * ROWS + r) * PITCH + 2 * pair]);
+            L += f * s_ml[w][r].y; x += f * v.x; y += f * v.y;
         }
-        if (splits > 1) store_remote2(tc::mapa(tc::smem_u32(&s_in[rank * per + i % per]), (uint32_t)(i / per)), x, y);
-        else finish(i, x, y);
+        if (splits == 1) { finish(r, pair, x, y, L); continue; }
+        const int to = (pair << log_splits) / PAIRS, width = PAIRS >> log_splits;
+        store_remote4(tc::mapa(tc::smem_u32(&s_in[(rank * ROWS + r) * width + (pair & (width - 1))]), (uint32_t)to), x, y, M, L);
     }
     if (splits > 1) {
         tc::cluster_sync();
-        if ((int)threadIdx.x < rows) {
-            float M = -INFINITY, L = 0.f;
-            for (int k = 0; k < splits; ++k) M = fmaxf(M, s_ml[k][threadIdx.x].x);
+        const int width = PAIRS >> log_splits;
+        for (int i = threadIdx.x; i < rows * width; i += kThreads) {
+            const int r = i / width, p = i & (width - 1);
+            float M = -INFINITY, L = 0.f, x = 0.f, y = 0.f;
+#pragma unroll 8
+            for (int k = 0; k < splits; ++k) M = fmaxf(M, s_in[(k * ROWS + r) * width + p].z);
+#pragma unroll 8
             for (int k = 0; k < splits; ++k) {
-                const float mk = s_ml[k][threadIdx.x].x, fk = mk == -INFINITY ? 0.f : tc::ex2_approx(mk - M);
-                L += fk * s_ml[k][threadIdx.x].y;
-                s_ml[k][threadIdx.x].x = fk;
+                const float4 v = s_in[(k * ROWS + r) * width + p];
+                const float f = v.z == -INFINITY ? 0.f : tc::ex2_approx(v.z - M);
+                L += f * v.w; x += f * v.x; y += f * v.y;
             }
-            s_inv[threadIdx.x] = L == 0.f ? 0.f : kUnscale / L;
-        }
-        __syncthreads();
-        for (int p = threadIdx.x; p < per && rank * per + p < pairs; p += kThreads) {
-            const int i = rank * per + p, r = 2 * i / DH;
-            float x = 0.f, y = 0.f;
-            for (int k = 0; k < splits; ++k) { const float2 v = s_in[k * per + p]; x += s_ml[k][r].x * v.x; y += s_ml[k][r].x * v.y; }
-            finish(i, x, y);
+            finish(r, rank * width + p, x, y, L);
         }
     }
 }
@@ -426,18 +447,18 @@ template <int DH, int NT>
 int32_t launch_few(const Cache4Args &a, cudaStream_t stream)
 {
     constexpr int ROWS = 8 * NT;
-    constexpr size_t shared = Few<DH, NT>::kWork + (size_t)(ROWS * DH + 2 * kMaxSplits) * 4;
+    constexpr size_t shared = Few<DH, NT>::kWork + (size_t)ROWS * (DH / 2) * 16;
     const int row_tiles = (int)(((long long)a.n_q * a.group + ROWS - 1) / ROWS);
     const long long items = (long long)a.batch * a.n_kv * row_tiles;
-    // as many CTAs as the machine holds at a time, but no fewer than two steps of 16 tokens for every warp
-    const int slots = gemm_num_sms() * (NT == 1 ? 2 : 1);
-    int splits = 1;
-    while (splits < kMaxSplits && items * splits * 2 <= slots && a.capacity > splits * kWarps * kStep * 2) splits *= 2;
+    const int slots = gemm_num_sms() * Few<DH, NT>::kPerSm;
+    int log_splits = 0;                                     // one wave of CTAs, whole steps for every warp
+    while ((1 << log_splits) < kMaxSplits && (items << (log_splits + 1)) <= slots && a.capacity >= (kWarps * kStep) << (log_splits + 1)) ++log_splits;
+    const int splits = 1 << log_splits;
     SFS_REQUIRE(items * splits <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
     SFS_CUDA(allow_shared(attention_cache4_few<DH, NT>, shared));
     if (splits > 8) SFS_CUDA(cudaFuncSetAttribute(attention_cache4_few<DH, NT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    if (splits > 1) SFS_CUDA(launch_pdl_cluster(attention_cache4_few<DH, NT>, splits, dim3((unsigned)(items * splits)), dim3(kThreads), shared, stream, a, splits, row_tiles));
-    else SFS_CUDA(launch_pdl(attention_cache4_few<DH, NT>, dim3((unsigned)items), dim3(kThreads), shared, stream, a, splits, row_tiles));
+    if (splits > 1) SFS_CUDA(launch_pdl_cluster(attention_cache4_few<DH, NT>, splits, dim3((unsigned)(items * splits)), dim3(kThreads), shared, stream, a, log_splits, row_tiles));
+    else SFS_CUDA(launch_pdl(attention_cache4_few<DH, NT>, dim3((unsigned)items), dim3(kThreads), shared, stream, a, log_splits, row_tiles));
     return SFS_OK;
 }
 
