@@ -3,9 +3,9 @@
 //
 // A CTA has two streams of 128 rows x 128-key tiles, so that the tensor core works on one while the other is in its softmax: two row tiles
 // that share every decoded key and value tile (PAIR), or the even and the odd key tiles of one row tile.  A row is a (query, head) pair of
-// the key head's group.  Warps 0-3 decode keys: a thread takes one key's codes, whose words of 8 features become 16-byte chunks of the
-// 128-byte-swizzled K-major tile (the order of features within a word is that of the decoding, the same for queries), warps 4-7 take pieces
-// of eight tokens' values, which come out transposed, eight tokens of a feature to a chunk.  The codes of the next tile are in flight meanwhile.
+// the key head's group.  Warps 0-7 decode: half of a key's codes per thread, whose words of 8 features become 16-byte chunks of the
+// 128-byte-swizzled K-major tile (the order of features within a word is that of the decoding, the same for queries), then a piece of eight
+// tokens' values, which comes out transposed, eight tokens of a feature to a chunk.  The codes of the next tile are in flight meanwhile.
 // Warps 8-15 are the softmax of the streams, one thread per row, warp 16 issues the MMAs.
 //
 // Decoded values are exact: bits moved into bf16 (times 2^-126), one product with 2^(c - 65), so a common factor of 2^-64 remains, which
@@ -26,15 +26,15 @@ using mx4::codes_as_bf16;
 using mx4::mul_bf16x2;
 
 constexpr int kMmaWarp = 16;
-constexpr int kThreads = (kMmaWarp + 1) * 32;               // 4 warps that decode keys, 4 values, 2 x 4 softmax warps, the MMA warp
-constexpr int kDecoders = 128;                              // threads of either kind
+constexpr int kThreads = (kMmaWarp + 1) * 32;               // 8 decoding warps, 2 x 4 softmax warps, the MMA warp
+constexpr int kDecoders = 256;
 // Registers: the launch's share is what five warps of a quarter of the SM can have; the decoders give some to the softmax.
 constexpr int kRegs = 96, kDecodeRegs = 64, kSoftmaxRegs = 128;
-static_assert(2 * kDecoders * kDecodeRegs + 256 * kSoftmaxRegs + 32 * kRegs <= kThreads * kRegs, "what is taken was given or is free");
+static_assert(kDecoders * kDecodeRegs + 256 * kSoftmaxRegs + 32 * kRegs <= kThreads * kRegs, "what is taken was given or is free");
 constexpr int QT = 128;                                     // rows of a stream
 constexpr int KT = 128;                                     // keys of a tile
 constexpr int kStages = 2;
-constexpr int kBars = 4 * kStages + 7;                      // K full / empty, V full / empty, S (two), P (two halves of two), exchange
+constexpr int kBars = 4 * kStages + 8;                      // K full / empty, V full / empty, S (two), P (two halves of two), exchange, Q
 constexpr float kLazy = 8.0f;
 constexpr float kUnscale = 18446744073709551616.0f;         // 2^64
 
@@ -43,17 +43,13 @@ __device__ __forceinline__ void store_chunk(uint32_t smem, uint32_t x, uint32_t 
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ float load_remote(uint32_t cluster_addr)
+__device__ __forceinline__ void store_remote4(uint32_t cluster_addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
 {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
-    return v;
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
-__device__ __forceinline__ float4 load_remote4(uint32_t cluster_addr)
+__device__ __forceinline__ void store_remote2(uint32_t cluster_addr, float x, float y)
 {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
-    return v;
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(cluster_addr), "f"(x), "f"(y) : "memory");
 }
 // bits k of [0, 64) with from <= k < to
 __device__ __forceinline__ unsigned long long bit_range(int from, int to)
@@ -71,6 +67,7 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
     constexpr int KB = DH / 64, WORDS = DH / 8, BLOCKS = DH / 32;
     constexpr int Q_BYTES = QT * DH * 2, K_BYTES = KT * DH * 2, V_BYTES = DH * KT * 2;
     constexpr int ROWS = NQ * QT;
+    constexpr int V_WARPS = DH / 16;                        // decoding warps that have values (16 token groups x WORDS pieces)
     constexpr uint32_t TMEM_COLS = 512;                     // S / P and O of each stream: 2 x (128 + DH) columns
 
     extern __shared__ uint8_t smem_raw[];
@@ -78,12 +75,12 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
     uint8_t *sQ = smem, *sK = smem + NQ * Q_BYTES, *sV = sK + kStages * K_BYTES;
     uint64_t *bars = reinterpret_cast<uint64_t *>(sV + kStages * V_BYTES);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + kBars);
-    float *s_o = reinterpret_cast<float *>(sK);             // [QT][DH], this CTA's partial output once all MMAs are done
+    float4 *s_o = reinterpret_cast<float4 *>(sK);           // [splits][QT / splits][DH / 4], what the ranks send once all MMAs are done
     __shared__ int s_abort, s_any_bad, s_range[3];          // first, lo, hi over the CTA's rows
     __shared__ int s_lo[ROWS], s_hi[ROWS], s_first[ROWS];
     __shared__ uint8_t s_bad[4][BLOCKS][KT / 8];            // tokens whose values are NaN, by tile (four in turn) and block of features
     __shared__ float s_max[2][QT], s_den[2][QT];
-    __shared__ float s_cm[QT], s_cl[QT];
+    __shared__ float2 s_ml[QT];                             // [splits][QT / splits], their maxima and denominators
     __shared__ uint32_t s_nan[2][QT];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -95,14 +92,14 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
 
     const uint32_t bar_kfull = tc::smem_u32(bars), bar_kempty = bar_kfull + 8 * kStages;
     const uint32_t bar_vfull = bar_kempty + 8 * kStages, bar_vempty = bar_vfull + 8 * kStages;
-    const uint32_t bar_s = bar_vempty + 8 * kStages /* two */, bar_p = bar_s + 16 /* + 16 w + 8 half */, bar_x = bar_s + 48;
+    const uint32_t bar_s = bar_vempty + 8 * kStages /* two */, bar_p = bar_s + 16 /* + 16 w + 8 half */, bar_x = bar_s + 48, bar_q = bar_s + 56;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             tc::mbar_init(bar_kfull + 8 * s, kDecoders); tc::mbar_init(bar_kempty + 8 * s, 1);
-            tc::mbar_init(bar_vfull + 8 * s, kDecoders); tc::mbar_init(bar_vempty + 8 * s, 1);
+            tc::mbar_init(bar_vfull + 8 * s, V_WARPS * 32); tc::mbar_init(bar_vempty + 8 * s, 1);
         }
         for (int w = 0; w < 2; ++w) { tc::mbar_init(bar_s + 8 * w, 1); tc::mbar_init(bar_p + 16 * w, QT); tc::mbar_init(bar_p + 16 * w + 8, QT); }
-        tc::mbar_init(bar_x, 2 * QT);
+        tc::mbar_init(bar_x, 2 * QT); tc::mbar_init(bar_q, 2 * QT);
         s_abort = 0; s_any_bad = 0;
         s_range[0] = 0; s_range[1] = 0x7FFFFFFF; s_range[2] = 0;
         tc::mbar_init_fence();
@@ -116,100 +113,84 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
 
     pdl_wait();
     pdl_trigger();
-    const int length = cache4_length(a, b);
-    for (int r = threadIdx.x; r < ROWS; r += kThreads) {
+    if (warp < ROWS / 32) {
+        const int r = threadIdx.x;
         Seen s = {0, 0, 0};
         bool live = r < n_rows;
         if (live) {
             const int i = (row0 + r) / a.group;
-            long long p = (long long)length - a.n_q + i;
-            if (a.positions) { p = a.positions[(long long)b * a.n_q + i]; live = p >= 0; }
-            if (live) s = cache4_seen(a, length, p);
+            const int given = a.positions ? a.positions[(long long)b * a.n_q + i] : 0, length = cache4_length(a, b);
+            live = given >= 0;
+            if (live) s = cache4_seen(a, length, a.positions ? (long long)given : (long long)length - a.n_q + i);
         }
         s_lo[r] = s.lo; s_hi[r] = s.hi; s_first[r] = live ? s.first : -1;      // -1: a row that is left as it was
-        if (s.hi > s.lo || s.first > 0) { atomicMax(&s_range[0], s.first); atomicMin(&s_range[1], s.lo); atomicMax(&s_range[2], s.hi); }
+        const bool some = s.hi > s.lo || s.first > 0;
+        const int f = warp_max_i32(s.first), l = warp_min_i32(some ? s.lo : 0x7FFFFFFF), h = warp_max_i32(s.hi);
+        if (lane == 0) { atomicMax(&s_range[0], f); atomicMin(&s_range[1], l); atomicMax(&s_range[2], h); }
     }
-    // queries, in the features' order of a decoded word: (0, 4), (1, 5), (2, 6), (3, 7)
-    for (int x = threadIdx.x; x < ROWS * WORDS; x += kThreads) {
-        const int r = x / WORDS, w = x % WORDS;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (r < n_rows) {
-            const int i = (row0 + r) / a.group, head = kv * a.group + (row0 + r) % a.group;
-            v = *reinterpret_cast<const uint4 *>(a.q + ((long long)b * a.n_q + i) * a.ld_q + (long long)head * DH + w * 8);
-        }
-        const int tile = r / QT, rr = r % QT;
-        store_chunk(tc::smem_u32(sQ) + tile * Q_BYTES + (w / 8) * (QT * 128) + rr * 128 + (((w % 8) ^ (rr & 7)) * 16),
-                    __byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-    }
-    fence_async_shared();
     __syncthreads();
-    const int hi = s_range[2], lo = min(s_range[1], hi), first = min(s_range[0], lo);
-    const int n_first = (first + KT - 1) / KT, n_all = n_first + (hi - lo + KT - 1) / KT;
+    // The tokens that some row sees, in one sequence without the gap behind the first ones: v stands for token v below `first`, for
+    // v + gap from there on.  (A row's first tokens beyond another row's window start: then lo = first, and there is no gap.)
+    const int hi = s_range[2], lo = min(s_range[1], hi), first = min(s_range[0], lo), gap = lo - first, n_seen = hi - gap;
+    const int n_all = (n_seen + KT - 1) / KT;
     const int tile0 = (int)((long long)n_all * rank / splits), n_tiles = (int)((long long)n_all * (rank + 1) / splits) - tile0;
-    auto tile_start = [&](int j) { j += tile0; return j < n_first ? j * KT : lo + (j - n_first) * KT; };
-    auto tile_end = [&](int j) { return j + tile0 < n_first ? first : hi; };
+    auto tile_start = [&](int j) { return (j + tile0) * KT; };
+    auto token = [&](int v) { v = min(v, n_seen - 1); return v < first ? v : v + gap; };
+    const int share = QT / splits;                          // rows of a rank's part of the join
     const int n_streams = PAIR ? (n_tiles == 0 ? 0 : n_rows > QT ? 2 : 1) : min(n_tiles, 2);
     auto tiles_of = [&](int w) { return w >= n_streams ? 0 : (PAIR ? n_tiles : (n_tiles - w + 1) / 2); };
     auto key_tile = [&](int w, int i) { return PAIR ? i : 2 * i + w; };
 
     const size_t base = (size_t)b * a.capacity * a.n_kv + kv;
-    if (warp < 4) {
-        // ---------------- keys: a thread decodes one key
+    if (warp < kDecoders / 32) {
+        // ---------------- decoding, the codes of the next tile in flight.  Keys: a thread has half of a key's words.  Values: a piece of
+        // eight tokens (8 ct .. of half kb of the tile) by a word of features, which comes out transposed.
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
-        const int n = threadIdx.x;
-        uint4 next[WORDS / 4], kc[WORDS / 4]; uint32_t next_s, ks;
-        auto fetch = [&](int j) {
-            const size_t at = base + (size_t)min(tile_start(j) + n, tile_end(j) - 1) * a.n_kv;
+        constexpr int KW = WORDS / 2;
+        const int n = threadIdx.x & (KT - 1), half = threadIdx.x / KT;
+        const int ct = lane & 7, u = warp * 4 + (lane >> 3), kb = u / WORDS, w0 = u % WORDS;
+        const bool has_values = warp < V_WARPS;
+        uint4 k_next[KW / 4], kc[KW / 4]; uint32_t ks_next, ks, v_next[8], vc[8], vs_next[8], vs[8];
+        auto fetch_k = [&](int j) {
+            const size_t at = base + (size_t)token(tile_start(j) + n) * a.n_kv;
 #pragma unroll
-            for (int i = 0; i < WORDS / 4; ++i) next[i] = reinterpret_cast<const uint4 *>(a.k_codes + at * (DH / 2))[i];
-            if constexpr (BLOCKS == 4) next_s = *reinterpret_cast<const uint32_t *>(a.k_scales + at * 4);
-            else next_s = *reinterpret_cast<const uint16_t *>(a.k_scales + at * 2);
+            for (int i = 0; i < KW / 4; ++i) k_next[i] = reinterpret_cast<const uint4 *>(a.k_codes + at * (DH / 2) + half * (DH / 4))[i];
+            if constexpr (BLOCKS == 4) ks_next = *reinterpret_cast<const uint16_t *>(a.k_scales + at * 4 + half * 2);
+            else ks_next = a.k_scales[at * 2 + half];
         };
-        if (n_tiles > 0) fetch(0);
+        auto fetch_v = [&](int j) {
+            const int v0 = tile_start(j) + kb * 64 + ct * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const size_t at = base + (size_t)token(v0 + i) * a.n_kv;
+                v_next[i] = *reinterpret_cast<const uint32_t *>(a.v_codes + at * (DH / 2) + w0 * 4);
+                vs_next[i] = a.v_scales[at * BLOCKS + w0 / 4];
+            }
+        };
+        if (n_tiles > 0) { fetch_k(0); if (has_values) fetch_v(0); }
         for (int j = 0; j < n_tiles; ++j) {
             const int s = j % kStages;
+            const uint32_t free_phase = ((uint32_t)(j / kStages) & 1u) ^ 1u;
 #pragma unroll
-            for (int i = 0; i < WORDS / 4; ++i) kc[i] = next[i];
-            ks = next_s;
-            if (j + 1 < n_tiles) fetch(j + 1);
-            if (!tc::mbar_wait(bar_kempty + 8 * s, ((uint32_t)(j / kStages) & 1u) ^ 1u, &s_abort)) break;
+            for (int i = 0; i < KW / 4; ++i) kc[i] = k_next[i];
+            ks = ks_next;
+            if (j + 1 < n_tiles) fetch_k(j + 1);
+            if (!tc::mbar_wait(bar_kempty + 8 * s, free_phase, &s_abort)) break;
             const uint32_t sk = tc::smem_u32(sK) + s * K_BYTES + n * 128;
 #pragma unroll
-            for (int w = 0; w < WORDS; ++w) {
-                const uint32_t x = w % 4 == 0 ? kc[w / 4].x : w % 4 == 1 ? kc[w / 4].y : w % 4 == 2 ? kc[w / 4].z : kc[w / 4].w;
-                const uint32_t f = cache_factor((ks >> (8 * (w / 4))) & 255u), ff = f | f << 16;
+            for (int i = 0; i < KW; ++i) {
+                const uint32_t x = i % 4 == 0 ? kc[i / 4].x : i % 4 == 1 ? kc[i / 4].y : i % 4 == 2 ? kc[i / 4].z : kc[i / 4].w;
+                const uint32_t f = cache_factor((ks >> (8 * (i / 4))) & 255u), ff = f | f << 16;
+                const int w = half * KW + i;
                 store_chunk(sk + (w / 8) * (KT * 128) + (((w % 8) ^ (n & 7)) * 16), mul_bf16x2(codes_as_bf16<0>(x), ff), mul_bf16x2(codes_as_bf16<1>(x), ff),
                             mul_bf16x2(codes_as_bf16<2>(x), ff), mul_bf16x2(codes_as_bf16<3>(x), ff));
             }
             fence_async_shared();
             tc::mbar_arrive(bar_kfull + 8 * s);
-        }
-    } else if (warp < 8) {
-        // ---------------- values, in pieces of eight tokens (8 ct .. of half kb of the tile) by 8 or 16 features, transposed
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
-        constexpr int PW = DH / 64;                         // words of a piece: 16 token groups x WORDS / PW pieces, one for each of 128 threads
-        uint32_t next[8][PW], vc[8][PW], next_s[8], vs[8];
-        const int ct = lane & 7, u = (warp - 4) * 4 + (lane >> 3), kb = u / (WORDS / PW), w0 = u % (WORDS / PW) * PW;
-        auto fetch = [&](int j) {
-            const int j0 = tile_start(j) + kb * 64 + ct * 8, last = tile_end(j) - 1;
+            if (!has_values) continue;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const size_t at = base + (size_t)min(j0 + i, last) * a.n_kv;
-                if constexpr (PW == 2) { const uint2 x = *reinterpret_cast<const uint2 *>(a.v_codes + at * (DH / 2) + w0 * 4); next[i][0] = x.x; next[i][PW - 1] = x.y; }
-                else next[i][0] = *reinterpret_cast<const uint32_t *>(a.v_codes + at * (DH / 2) + w0 * 4);
-                next_s[i] = a.v_scales[at * BLOCKS + w0 / 4];
-            }
-        };
-        if (n_tiles > 0) fetch(0);
-        for (int j = 0; j < n_tiles; ++j) {
-            const int s = j % kStages;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-#pragma unroll
-                for (int e = 0; e < PW; ++e) vc[i][e] = next[i][e];
-                vs[i] = next_s[i];
-            }
-            if (j + 1 < n_tiles) fetch(j + 1);
+            for (int i = 0; i < 8; ++i) { vc[i] = v_next[i]; vs[i] = vs_next[i]; }
+            if (j + 1 < n_tiles) fetch_v(j + 1);
             uint32_t f[4], bad = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -218,29 +199,27 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
                 bad |= (bad0 ? 1u : 0u) << (2 * i) | (bad1 ? 2u : 0u) << (2 * i);
                 f[i] = (bad0 ? 0u : (vs[2 * i] + 62) << 7) | (bad1 ? 0u : (vs[2 * i + 1] + 62) << 23);
             }
-            if (!tc::mbar_wait(bar_vempty + 8 * s, ((uint32_t)(j / kStages) & 1u) ^ 1u, &s_abort)) break;
+            if (!tc::mbar_wait(bar_vempty + 8 * s, free_phase, &s_abort)) break;
             if (w0 % 4 == 0) s_bad[j & 3][w0 / 4][kb * 8 + ct] = (uint8_t)bad;
             if (bad) s_any_bad = 1;
+            const uint32_t sv = tc::smem_u32(sV) + s * V_BYTES + kb * (DH * 128) + w0 * 8 * 128;
+            uint32_t x[4];
+            auto feature = [&](auto J, int d) {
+                store_chunk(sv + d * 128 + ((ct ^ d) * 16), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[0]), f[0]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[1]), f[1]),
+                            mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[2]), f[2]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[3]), f[3]));
+            };
 #pragma unroll
-            for (int e = 0; e < PW; ++e) {
-                const uint32_t sv = tc::smem_u32(sV) + s * V_BYTES + kb * (DH * 128) + (w0 + e) * 8 * 128;
-                uint32_t x[4];
-                auto feature = [&](auto J, int d) {
-                    store_chunk(sv + d * 128 + ((ct ^ d) * 16), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[0]), f[0]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[1]), f[1]),
-                                mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[2]), f[2]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[3]), f[3]));
-                };
+            for (int i = 0; i < 4; ++i) x[i] = __byte_perm(vc[2 * i], vc[2 * i + 1], 0x5410);              // features 0-3 of both tokens
+            feature(std::integral_constant<int, 0>(), 0); feature(std::integral_constant<int, 1>(), 1);
+            feature(std::integral_constant<int, 2>(), 2); feature(std::integral_constant<int, 3>(), 3);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = __byte_perm(vc[2 * i][e], vc[2 * i + 1][e], 0x5410);        // features 0-3 of both tokens
-                feature(std::integral_constant<int, 0>(), 0); feature(std::integral_constant<int, 1>(), 1);
-                feature(std::integral_constant<int, 2>(), 2); feature(std::integral_constant<int, 3>(), 3);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = __byte_perm(vc[2 * i][e], vc[2 * i + 1][e], 0x7632);        // features 4-7
-                feature(std::integral_constant<int, 0>(), 4); feature(std::integral_constant<int, 1>(), 5);
-                feature(std::integral_constant<int, 2>(), 6); feature(std::integral_constant<int, 3>(), 7);
-            }
+            for (int i = 0; i < 4; ++i) x[i] = __byte_perm(vc[2 * i], vc[2 * i + 1], 0x7632);              // features 4-7
+            feature(std::integral_constant<int, 0>(), 4); feature(std::integral_constant<int, 1>(), 5);
+            feature(std::integral_constant<int, 2>(), 6); feature(std::integral_constant<int, 3>(), 7);
             fence_async_shared();
             tc::mbar_arrive(bar_vfull + 8 * s);
         }
+        __syncwarp();
     } else if (warp == kMmaWarp) {
         // ---------------- MMA issuer: the whole warp runs the loop with warp-uniform operands, one elected lane issues
         constexpr uint32_t idesc_s = tc::idesc_bf16_f32(QT, KT);
@@ -261,7 +240,7 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
             if (!PAIR || w == last) tc::mma_commit_elect(bar_kempty + 8 * s);
             return true;
         };
-        bool ok = true;
+        bool ok = __all_sync(0xffffffffu, tc::mbar_wait(bar_q, 0, &s_abort));
         for (int w = 0; w < n_streams && ok; ++w) ok = issue_S(w, key_tile(w, 0));
         const int n0 = tiles_of(0);
         for (int i = 0; i < n0 && ok; ++i) {
@@ -291,18 +270,39 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
         // ---------------- online softmax, one thread per row, against a reference maximum that follows the true one lazily
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int w = (warp - 8) >> 2, row = (warp & 3) * 32 + lane;
+        {
+            // queries, in the features' order of a decoded word: (0, 4), (1, 5), (2, 6), (3, 7); a thread has a row, or half of one
+            constexpr int PART = WORDS * NQ / 2, BATCH = PART < 8 ? PART : 8;
+            const int x = threadIdx.x - kDecoders, rq = x % ROWS, c0 = x / ROWS * PART, tile = rq / QT, rr = rq % QT;
+            const int i = (row0 + rq) / a.group, head = kv * a.group + (row0 + rq) % a.group;
+            const __nv_bfloat16 *src = a.q + ((long long)b * a.n_q + i) * a.ld_q + (long long)head * DH;
+#pragma unroll
+            for (int c = 0; c < PART; c += BATCH) {
+                uint4 v[BATCH];
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) v[k] = rq < n_rows ? *reinterpret_cast<const uint4 *>(src + (c0 + c + k) * 8) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) {
+                    const int wd = c0 + c + k;
+                    store_chunk(tc::smem_u32(sQ) + tile * Q_BYTES + (wd / 8) * (QT * 128) + rr * 128 + (((wd % 8) ^ (rr & 7)) * 16),
+                                __byte_perm(v[k].x, v[k].z, 0x5410), __byte_perm(v[k].x, v[k].z, 0x7632), __byte_perm(v[k].y, v[k].w, 0x5410), __byte_perm(v[k].y, v[k].w, 0x7632));
+                }
+            }
+            fence_async_shared();
+            tc::mbar_arrive(bar_q);
+        }
         const int r = (PAIR ? w * QT : 0) + row;            // row of the CTA
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem_S + (uint32_t)(w * KT) + lane_off, to = tmem_O + (uint32_t)(w * DH) + lane_off;
         const float c = a.scale_log2 * kUnscale;
         const int n_mine = tiles_of(w);
-        const int r_lo = s_lo[r], r_hi = s_hi[r], r_first = s_first[r];
+        const int r_lo = s_lo[r] - gap, r_hi = s_hi[r] - gap, r_first = s_first[r];             // (in the sequence without the gap)
         float m = -INFINITY, l = 0.f;                       // reference maximum, denominator (times 2^64)
         uint32_t nan_blocks = 0;
         bool ok = true;
         auto seen64 = [&](int j, int q) {                   // which of 64 keys of tile j the row sees
-            const int j0 = tile_start(j) + q * 64, end = tile_end(j);
-            return bit_range(r_lo - j0, min(r_hi, end) - j0) | bit_range(0, min(r_first, end) - j0);
+            const int v0 = tile_start(j) + q * 64;
+            return bit_range(r_lo - v0, r_hi - v0) | bit_range(0, r_first - v0);
         };
         auto nan_of = [&](int j) {                          // blocks of features in which the row sees a NaN of tile j
             for (int blk = 0; blk < BLOCKS; ++blk)
@@ -316,9 +316,9 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
             ok = tc::mbar_wait(bar_s + 8 * w, (uint32_t)i & 1u, &s_abort);      // (P V of the tile before has finished too)
             if (!ok) break;
             tc::tc_fence_after();
-            const int j = key_tile(w, i), j0 = tile_start(j);
+            const int j = key_tile(w, i), v0 = tile_start(j);
             if (i > 0 && *reinterpret_cast<volatile int *>(&s_any_bad)) nan_of(key_tile(w, i - 1));      // its values were decoded by then
-            const bool whole = j0 >= r_lo && j0 + KT <= min(r_hi, tile_end(j));
+            const bool whole = v0 >= r_lo && v0 + KT <= r_hi;
             uint32_t v[64], pk[32];
             auto load = [&](int q) {                        // 64 scores, those of keys that the row does not see -inf
                 tc::tmem_ld32(ts + q * 64, v); tc::tmem_ld32(ts + q * 64 + 32, v + 32);
@@ -418,14 +418,19 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
             if (splits == 1) {
                 const float inv = den == 0.f ? 0.f : kUnscale / den;
                 f0 *= inv; f1 *= inv;
-            } else if (w == 0) { s_cm[row] = mm; s_cl[row] = den; }
+            } else {
+                // every rank is done with its ring: what it sends, rank k = row / share joins
+                tc::cluster_sync();
+                if (w == 0) store_remote2(tc::mapa(tc::smem_u32(&s_ml[rank * share + row % share]), (uint32_t)(row / share)), mm, den);
+            }
         }
         if (__all_sync(0xffffffffu, write)) {
             tc::tc_fence_after();
-            const bool in = r < n_rows && r_first >= 0;
             const uint32_t t0 = tmem_O + lane_off + (uint32_t)(PAIR ? w * DH : col0);
-            const int qi = (row0 + r) / a.group, head = kv * a.group + (row0 + r) % a.group;
-            __nv_bfloat16 *dst = a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + col0;
+            // the rows' outputs pass through the queries' place, so that a row leaves in whole lines; 16-byte chunks rotated by the row
+            constexpr int CH = COLS / 8, TURN = CH < 8 ? CH - 1 : 7;
+            const uint32_t park = tc::smem_u32(sQ) + (PAIR ? w * Q_BYTES : w * (QT * COLS * 2)) + (warp & 3) * 32 * COLS * 2;
+            auto place = [&](int rr, int chunk) { return park + rr * (COLS * 2) + ((chunk ^ ((CH < 8 ? rr >> 1 : rr) & TURN)) * 16); };
 #pragma unroll
             for (int q = 0; q < COLS / 32; ++q) {
                 uint32_t o[32], o1[32];
@@ -441,13 +446,12 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
                     o[k] = nan ? 0x7FC00000u : __float_as_uint(x);
                 }
                 if (!PAIR && splits > 1) {
-                    // rows are 16-byte chunks in turn, rotated by the row so that a warp's stores spread over the banks
+                    // rotated by the row, so that a warp's stores spread over the banks
+                    const uint32_t row_at = tc::smem_u32(s_o + (rank * share + row % share) * (DH / 4));
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int chunk = (col0 / 4 + q * 8 + i + row) % (DH / 4);
-                        store_chunk(tc::smem_u32(s_o + row * DH + chunk * 4), o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-                    }
-                } else if (in) {
+                    for (int i = 0; i < 8; ++i)
+                        store_remote4(tc::mapa(row_at + ((col0 / 4 + q * 8 + i + row) % (DH / 4)) * 16, (uint32_t)(row / share)), o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         uint32_t wd[4];
@@ -456,32 +460,45 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
                             __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[8 * i + 2 * t]), __uint_as_float(o[8 * i + 2 * t + 1]));
                             wd[t] = *reinterpret_cast<uint32_t *>(&hh);
                         }
-                        reinterpret_cast<uint4 *>(dst)[q * 4 + i] = make_uint4(wd[0], wd[1], wd[2], wd[3]);
+                        store_chunk(place(lane, q * 4 + i), wd[0], wd[1], wd[2], wd[3]);
                     }
+                }
+            }
+            if (PAIR || splits == 1) {
+                __syncwarp();
+                constexpr int AT_ONCE = 32 / CH;            // rows of a warp's store
+#pragma unroll 4
+                for (int rr = lane / CH; rr < 32; rr += AT_ONCE) {
+                    const int rg = (PAIR ? w * QT : 0) + (warp & 3) * 32 + rr;
+                    if (rg >= n_rows || s_first[rg] < 0) continue;
+                    const int qi = (row0 + rg) / a.group, head = kv * a.group + (row0 + rg) % a.group;
+                    uint4 v;
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(place(rr, lane % CH)) : "memory");
+                    *reinterpret_cast<uint4 *>(a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + col0 + lane % CH * 8) = v;
                 }
             }
         }
     }
     if (!PAIR && splits > 1) {
         // ---------------- join the ranks: each writes its share of the rows
+        if (warp < 8 || warp == kMmaWarp) tc::cluster_sync();                   // (the softmax warps have passed theirs)
         tc::cluster_sync();
         if (!s_abort) {
-            const int share = QT / splits;
             for (int x = threadIdx.x; x < share * (DH / 4); x += kThreads) {
-                const int row = rank * share + x / (DH / 4), col = x % (DH / 4);
+                const int local = x / (DH / 4), col = x % (DH / 4), row = rank * share + local;
                 if (row >= n_rows || s_first[row] < 0) continue;
-                float mk[8], M = -INFINITY, L = 0.f;
+                float M = -INFINITY, L = 0.f;
                 float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                float2 ml[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) { mk[k] = k < splits ? load_remote(tc::mapa(tc::smem_u32(&s_cm[row]), (uint32_t)k)) : -INFINITY; M = fmaxf(M, mk[k]); }
-                const uint32_t at = tc::smem_u32(s_o + row * DH + ((col + row) % (DH / 4)) * 4);
+                for (int k = 0; k < 8; ++k) { ml[k] = k < splits ? s_ml[k * share + local] : make_float2(-INFINITY, 0.f); M = fmaxf(M, ml[k].x); }
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     if (k < splits) {
-                        const float fk = mk[k] == -INFINITY ? 0.f : tc::ex2_approx((mk[k] - M) * (a.scale_log2 * kUnscale));
-                        const float4 o = load_remote4(tc::mapa(at, (uint32_t)k));
-                        L += fk * load_remote(tc::mapa(tc::smem_u32(&s_cl[row]), (uint32_t)k));
-                        sum.x += fk * o.x; sum.y += fk * o.y; sum.z += fk * o.z; sum.w += fk * o.w;
+                        const float f = ml[k].x == -INFINITY ? 0.f : tc::ex2_approx((ml[k].x - M) * (a.scale_log2 * kUnscale));
+                        const float4 o = s_o[(k * share + local) * (DH / 4) + (col + row) % (DH / 4)];
+                        L += f * ml[k].y;
+                        sum.x += f * o.x; sum.y += f * o.y; sum.z += f * o.z; sum.w += f * o.w;
                     }
                 const float inv = L == 0.f ? 0.f : kUnscale / L;
                 const int qi = (row0 + row) / a.group, head = kv * a.group + (row0 + row) % a.group;
@@ -490,7 +507,6 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
                     make_uint2(*reinterpret_cast<const uint32_t *>(&x0), *reinterpret_cast<const uint32_t *>(&x1));
             }
         }
-        tc::cluster_sync();                                 // shared memory stays until every rank has read it
     }
     tc::tc_fence_before();
     __syncthreads();
