@@ -3,7 +3,7 @@
 //
 // A CTA has two streams of 128 rows x 128-key tiles, so that the tensor core works on one while the other is in its softmax: two row tiles
 // that share every decoded key and value tile (PAIR), or the even and the odd key tiles of one row tile.  A row is a (query, head) pair of
-// the key head's group.  Warps 0-7 decode: half of a key's codes per thread, whose words of 8 features become 16-byte chunks of the
+// the key head's group.  Warps 0-7 decode: blocks of keys' codes, whose words of 8 features become 16-byte chunks of the
 // 128-byte-swizzled K-major tile (the order of features within a word is that of the decoding, the same for queries), then a piece of eight
 // tokens' values, which comes out transposed, eight tokens of a feature to a chunk.  The codes of the next tile are in flight meanwhile.
 // Warps 8-15 are the softmax of the streams, one thread per row, warp 16 issues the MMAs.
@@ -61,7 +61,7 @@ __device__ __forceinline__ unsigned long long bit_range(int from, int to)
 
 template <int DH, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
-attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
+attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
 {
     constexpr int NQ = PAIR ? 2 : 1;
     constexpr int KB = DH / 64, WORDS = DH / 8, BLOCKS = DH / 32;
@@ -77,15 +77,15 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + kBars);
     float4 *s_o = reinterpret_cast<float4 *>(sK);           // [splits][QT / splits][DH / 4], what the ranks send once all MMAs are done
     __shared__ int s_abort, s_any_bad, s_range[3];          // first, lo, hi over the CTA's rows
-    __shared__ int s_lo[ROWS], s_hi[ROWS], s_first[ROWS];
+    __shared__ int s_lo[ROWS], s_hi[ROWS], s_first[ROWS], s_query[ROWS];          // s_query: a row's query; its head in the group is what is left
     __shared__ uint8_t s_bad[4][BLOCKS][KT / 8];            // tokens whose values are NaN, by tile (four in turn) and block of features
     __shared__ float s_max[2][QT], s_den[2][QT];
     __shared__ float2 s_ml[QT];                             // [splits][QT / splits], their maxima and denominators
     __shared__ uint32_t s_nan[2][QT];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = blockIdx.x % splits;
-    int item = blockIdx.x / splits;
+    const int splits = 1 << log_splits, rank = blockIdx.x & (splits - 1);
+    int item = blockIdx.x >> log_splits;
     const int row0 = (item % row_tiles) * ROWS; item /= row_tiles;
     const int kv = item % a.n_kv, b = item / a.n_kv;
     const int n_rows = a.n_q * a.group - row0;              // rows from this CTA's first on
@@ -117,8 +117,9 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
         const int r = threadIdx.x;
         Seen s = {0, 0, 0};
         bool live = r < n_rows;
+        const int i = (row0 + r) / a.group;
+        s_query[r] = i;
         if (live) {
-            const int i = (row0 + r) / a.group;
             const int given = a.positions ? a.positions[(long long)b * a.n_q + i] : 0, length = cache4_length(a, b);
             live = given >= 0;
             if (live) s = cache4_seen(a, length, a.positions ? (long long)given : (long long)length - a.n_q + i);
@@ -133,30 +134,33 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
     // v + gap from there on.  (A row's first tokens beyond another row's window start: then lo = first, and there is no gap.)
     const int hi = s_range[2], lo = min(s_range[1], hi), first = min(s_range[0], lo), gap = lo - first, n_seen = hi - gap;
     const int n_all = (n_seen + KT - 1) / KT;
-    const int tile0 = (int)((long long)n_all * rank / splits), n_tiles = (int)((long long)n_all * (rank + 1) / splits) - tile0;
+    const int tile0 = (n_all * rank) >> log_splits, n_tiles = ((n_all * (rank + 1)) >> log_splits) - tile0;         // (at most 2^24 tiles)
     auto tile_start = [&](int j) { return (j + tile0) * KT; };
+    // where a row's query and output lie, without the head dimension's offset
+    auto row_of = [&](int r, long long ld) { const int i = s_query[r]; return ((long long)b * a.n_q + i) * ld + (long long)(kv * a.group + row0 + r - i * a.group) * DH; };
     auto token = [&](int v) { v = min(v, n_seen - 1); return v < first ? v : v + gap; };
-    const int share = QT / splits;                          // rows of a rank's part of the join
+    const int share = QT >> log_splits;                          // rows of a rank's part of the join
     const int n_streams = PAIR ? (n_tiles == 0 ? 0 : n_rows > QT ? 2 : 1) : min(n_tiles, 2);
     auto tiles_of = [&](int w) { return w >= n_streams ? 0 : (PAIR ? n_tiles : (n_tiles - w + 1) / 2); };
     auto key_tile = [&](int w, int i) { return PAIR ? i : 2 * i + w; };
 
     const size_t base = (size_t)b * a.capacity * a.n_kv + kv;
     if (warp < kDecoders / 32) {
-        // ---------------- decoding, the codes of the next tile in flight.  Keys: a thread has half of a key's words.  Values: a piece of
+        // ---------------- decoding, the codes of the next tile in flight.  Keys: a thread has a block of one or two keys.  Values: a piece of
         // eight tokens (8 ct .. of half kb of the tile) by a word of features, which comes out transposed.
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
-        constexpr int KW = WORDS / 2;
-        const int n = threadIdx.x & (KT - 1), half = threadIdx.x / KT;
+        constexpr int LANES = BLOCKS, KEYS = KT * LANES / kDecoders;         // lanes of a key, one block of features each, and keys of a thread
+        const int n0 = threadIdx.x / LANES, kt = threadIdx.x % LANES;
         const int ct = lane & 7, u = warp * 4 + (lane >> 3), kb = u / WORDS, w0 = u % WORDS;
         const bool has_values = warp < V_WARPS;
-        uint4 k_next[KW / 4], kc[KW / 4]; uint32_t ks_next, ks, v_next[8], vc[8], vs_next[8], vs[8];
+        uint4 k_next[KEYS], kc[KEYS]; uint32_t ks_next[KEYS], ks[KEYS], v_next[8], vc[8], vs_next[8], vs[8];
         auto fetch_k = [&](int j) {
-            const size_t at = base + (size_t)token(tile_start(j) + n) * a.n_kv;
 #pragma unroll
-            for (int i = 0; i < KW / 4; ++i) k_next[i] = reinterpret_cast<const uint4 *>(a.k_codes + at * (DH / 2) + half * (DH / 4))[i];
-            if constexpr (BLOCKS == 4) ks_next = *reinterpret_cast<const uint16_t *>(a.k_scales + at * 4 + half * 2);
-            else ks_next = a.k_scales[at * 2 + half];
+            for (int e = 0; e < KEYS; ++e) {
+                const size_t at = base + (size_t)token(tile_start(j) + n0 + e * (KT / KEYS)) * a.n_kv;
+                k_next[e] = *reinterpret_cast<const uint4 *>(a.k_codes + at * (DH / 2) + kt * 16);
+                ks_next[e] = a.k_scales[at * BLOCKS + kt];
+            }
         };
         auto fetch_v = [&](int j) {
             const int v0 = tile_start(j) + kb * 64 + ct * 8;
@@ -171,19 +175,26 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
         for (int j = 0; j < n_tiles; ++j) {
             const int s = j % kStages;
             const uint32_t free_phase = ((uint32_t)(j / kStages) & 1u) ^ 1u;
+            // lanes of the second half of the features take their words in another order, so that a warp's stores spread over the banks
+            const int turn = kt & 2;
 #pragma unroll
-            for (int i = 0; i < KW / 4; ++i) kc[i] = k_next[i];
-            ks = ks_next;
+            for (int e = 0; e < KEYS; ++e) {
+                kc[e] = turn ? make_uint4(k_next[e].z, k_next[e].w, k_next[e].x, k_next[e].y) : k_next[e];
+                ks[e] = ks_next[e];
+            }
             if (j + 1 < n_tiles) fetch_k(j + 1);
             if (!tc::mbar_wait(bar_kempty + 8 * s, free_phase, &s_abort)) break;
-            const uint32_t sk = tc::smem_u32(sK) + s * K_BYTES + n * 128;
 #pragma unroll
-            for (int i = 0; i < KW; ++i) {
-                const uint32_t x = i % 4 == 0 ? kc[i / 4].x : i % 4 == 1 ? kc[i / 4].y : i % 4 == 2 ? kc[i / 4].z : kc[i / 4].w;
-                const uint32_t f = cache_factor((ks >> (8 * (i / 4))) & 255u), ff = f | f << 16;
-                const int w = half * KW + i;
-                store_chunk(sk + (w / 8) * (KT * 128) + (((w % 8) ^ (n & 7)) * 16), mul_bf16x2(codes_as_bf16<0>(x), ff), mul_bf16x2(codes_as_bf16<1>(x), ff),
-                            mul_bf16x2(codes_as_bf16<2>(x), ff), mul_bf16x2(codes_as_bf16<3>(x), ff));
+            for (int e = 0; e < KEYS; ++e) {
+                const int n = n0 + e * (KT / KEYS);
+                const uint32_t sk = tc::smem_u32(sK) + s * K_BYTES + (kt / 2) * (KT * 128) + n * 128;
+                const uint32_t f = cache_factor(ks[e]), ff = f | f << 16;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t x = i == 0 ? kc[e].x : i == 1 ? kc[e].y : i == 2 ? kc[e].z : kc[e].w;
+                    store_chunk(sk + ((((kt & 1) * 4 + (i ^ turn)) ^ (n & 7)) * 16), mul_bf16x2(codes_as_bf16<0>(x), ff), mul_bf16x2(codes_as_bf16<1>(x), ff),
+                                mul_bf16x2(codes_as_bf16<2>(x), ff), mul_bf16x2(codes_as_bf16<3>(x), ff));
+                }
             }
             fence_async_shared();
             tc::mbar_arrive(bar_kfull + 8 * s);
@@ -271,21 +282,23 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int w = (warp - 8) >> 2, row = (warp & 3) * 32 + lane;
         {
-            // queries, in the features' order of a decoded word: (0, 4), (1, 5), (2, 6), (3, 7); a thread has a row, or half of one
-            constexpr int PART = WORDS * NQ / 2, BATCH = PART < 8 ? PART : 8;
-            const int x = threadIdx.x - kDecoders, rq = x % ROWS, c0 = x / ROWS * PART, tile = rq / QT, rr = rq % QT;
-            const int i = (row0 + rq) / a.group, head = kv * a.group + (row0 + rq) % a.group;
-            const __nv_bfloat16 *src = a.q + ((long long)b * a.n_q + i) * a.ld_q + (long long)head * DH;
+            // queries, in the features' order of a decoded word: (0, 4), (1, 5), (2, 6), (3, 7); neighbouring lanes have a row's words
+            constexpr int ROWS_AT_ONCE = 2 * QT / WORDS, BATCH = 8;
+            const int wd = (threadIdx.x - kDecoders) % WORDS, first_row = (threadIdx.x - kDecoders) / WORDS;
 #pragma unroll
-            for (int c = 0; c < PART; c += BATCH) {
+            for (int c = 0; c < ROWS; c += BATCH * ROWS_AT_ONCE) {
                 uint4 v[BATCH];
 #pragma unroll
-                for (int k = 0; k < BATCH; ++k) v[k] = rq < n_rows ? *reinterpret_cast<const uint4 *>(src + (c0 + c + k) * 8) : make_uint4(0, 0, 0, 0);
+                for (int k = 0; k < BATCH; ++k) {
+                    const int rq = first_row + c + k * ROWS_AT_ONCE;
+                    v[k] = rq < min(n_rows, ROWS) ? *reinterpret_cast<const uint4 *>(a.q + row_of(rq, a.ld_q) + wd * 8) : make_uint4(0, 0, 0, 0);
+                }
 #pragma unroll
                 for (int k = 0; k < BATCH; ++k) {
-                    const int wd = c0 + c + k;
-                    store_chunk(tc::smem_u32(sQ) + tile * Q_BYTES + (wd / 8) * (QT * 128) + rr * 128 + (((wd % 8) ^ (rr & 7)) * 16),
-                                __byte_perm(v[k].x, v[k].z, 0x5410), __byte_perm(v[k].x, v[k].z, 0x7632), __byte_perm(v[k].y, v[k].w, 0x5410), __byte_perm(v[k].y, v[k].w, 0x7632));
+                    const int rq = first_row + c + k * ROWS_AT_ONCE, tile = rq / QT, rr = rq % QT;
+                    if (rq < ROWS)
+                        store_chunk(tc::smem_u32(sQ) + tile * Q_BYTES + (wd / 8) * (QT * 128) + rr * 128 + (((wd % 8) ^ (rr & 7)) * 16),
+                                    __byte_perm(v[k].x, v[k].z, 0x5410), __byte_perm(v[k].x, v[k].z, 0x7632), __byte_perm(v[k].y, v[k].w, 0x5410), __byte_perm(v[k].y, v[k].w, 0x7632));
                 }
             }
             fence_async_shared();
@@ -471,10 +484,9 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
                 for (int rr = lane / CH; rr < 32; rr += AT_ONCE) {
                     const int rg = (PAIR ? w * QT : 0) + (warp & 3) * 32 + rr;
                     if (rg >= n_rows || s_first[rg] < 0) continue;
-                    const int qi = (row0 + rg) / a.group, head = kv * a.group + (row0 + rg) % a.group;
                     uint4 v;
                     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(place(rr, lane % CH)) : "memory");
-                    *reinterpret_cast<uint4 *>(a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + col0 + lane % CH * 8) = v;
+                    *reinterpret_cast<uint4 *>(a.out + row_of(rg, a.ld_out) + col0 + lane % CH * 8) = v;
                 }
             }
         }
@@ -501,9 +513,8 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
                         sum.x += f * o.x; sum.y += f * o.y; sum.z += f * o.z; sum.w += f * o.w;
                     }
                 const float inv = L == 0.f ? 0.f : kUnscale / L;
-                const int qi = (row0 + row) / a.group, head = kv * a.group + (row0 + row) % a.group;
                 const __nv_bfloat162 x0 = __floats2bfloat162_rn(sum.x * inv, sum.y * inv), x1 = __floats2bfloat162_rn(sum.z * inv, sum.w * inv);
-                *reinterpret_cast<uint2 *>(a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + col * 4) =
+                *reinterpret_cast<uint2 *>(a.out + row_of(row, a.ld_out) + col * 4) =
                     make_uint2(*reinterpret_cast<const uint32_t *>(&x0), *reinterpret_cast<const uint32_t *>(&x1));
             }
         }
@@ -515,19 +526,19 @@ attention_cache4_many_kernel(Cache4Args a, int splits, int row_tiles)
 }
 
 template <int DH, bool PAIR>
-int32_t launch(const Cache4Args &a, int splits, cudaStream_t stream)
+int32_t launch(const Cache4Args &a, int log_splits, cudaStream_t stream)
 {
     constexpr int NQ = PAIR ? 2 : 1;
     constexpr size_t shared = 1024 + (size_t)NQ * QT * DH * 2 + (size_t)kStages * 2 * KT * DH * 2 + kBars * 8 + 16;
-    const long long row_tiles = ((long long)a.n_q * a.group + NQ * QT - 1) / (NQ * QT), ctas = (long long)a.batch * a.n_kv * row_tiles * splits;
+    const long long row_tiles = ((long long)a.n_q * a.group + NQ * QT - 1) / (NQ * QT), ctas = ((long long)a.batch * a.n_kv * row_tiles) << log_splits;
     SFS_REQUIRE(ctas <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
     SFS_CUDA(allow_shared(attention_cache4_many_kernel<DH, PAIR>, shared));
     // the softmax warps wait for registers that the launch must have brought: without them the kernel would not end
     cudaFuncAttributes attr;
     SFS_CUDA(cudaFuncGetAttributes(&attr, attention_cache4_many_kernel<DH, PAIR>));
     SFS_REQUIRE(attr.numRegs >= kRegs, SFS_ERR_UNSUPPORTED, "attention_cache4: built with %d registers a thread, %d needed", attr.numRegs, kRegs);
-    if (splits > 1) SFS_CUDA(launch_pdl_cluster(attention_cache4_many_kernel<DH, PAIR>, splits, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, splits, (int)row_tiles));
-    else SFS_CUDA(launch_pdl(attention_cache4_many_kernel<DH, PAIR>, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, 1, (int)row_tiles));
+    if (log_splits > 0) SFS_CUDA(launch_pdl_cluster(attention_cache4_many_kernel<DH, PAIR>, 1 << log_splits, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, log_splits, (int)row_tiles));
+    else SFS_CUDA(launch_pdl(attention_cache4_many_kernel<DH, PAIR>, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, 0, (int)row_tiles));
     return SFS_OK;
 }
 
@@ -537,10 +548,10 @@ int32_t attention_cache4_many(const Cache4Args &a, int head_dim, cudaStream_t st
 {
     const long long row_tiles = ((long long)a.n_q * a.group + QT - 1) / QT, heads = (long long)a.batch * a.n_kv, sms = gemm_num_sms();
     if (row_tiles > 1 && heads * ((row_tiles + 1) / 2) >= sms)               // pairs of row tiles fill the machine
-        return head_dim == 128 ? launch<128, true>(a, 1, stream) : launch<64, true>(a, 1, stream);
-    int splits = 1;                                         // up to one wave of CTAs, two key tiles for each
-    while (splits < 8 && heads * row_tiles * splits * 2 <= sms && a.capacity > splits * 2 * KT) splits *= 2;
-    return head_dim == 128 ? launch<128, false>(a, splits, stream) : launch<64, false>(a, splits, stream);
+        return head_dim == 128 ? launch<128, true>(a, 0, stream) : launch<64, true>(a, 0, stream);
+    int log_splits = 0;                                     // up to one wave of CTAs, two key tiles for each
+    while (log_splits < 3 && (heads * row_tiles << (log_splits + 1)) <= sms && a.capacity > (2 * KT) << log_splits) ++log_splits;
+    return head_dim == 128 ? launch<128, false>(a, log_splits, stream) : launch<64, false>(a, log_splits, stream);
 }
 
 }  // namespace sfs
