@@ -26,6 +26,8 @@ using mx4::mul_bf16x2;
 
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
+constexpr int kRows = 8;                                    // query rows of a CTA
+constexpr int kPerSm = 2;                                   // CTAs
 constexpr int kMaxSplits = 16;                            // CTAs of a cluster
 constexpr int kStep = 32;                                   // tokens of a warp's step, two tiles of 16
 constexpr float kLazy = 8.0f;                               // the reference maximum may lag by 2^8
@@ -70,25 +72,24 @@ __device__ __forceinline__ int token_of(int i) { return (i & 8) | ((i & 3) << 1)
 __device__ __forceinline__ int row_of(int j) { return (j & 8) | ((j >> 1) & 3) | ((j & 1) << 2); }
 
 // shared memory: the rings, in whose place the warps' partial outputs are joined
-template <int DH, int NT> struct Few {
-    static constexpr int kPerSm = 2;                        // CTAs
-    static constexpr int kPartials = kWarps * 8 * NT * (DH + 4) * 4;
+template <int DH> struct Few {
+    static constexpr int kPartials = kWarps * kRows * (DH + 4) * 4;
     static constexpr int kWork = kPartials > kWarps * Ring<DH>::kWarp ? kPartials : kWarps * Ring<DH>::kWarp;
 };
 
-template <int DH, int NT>                                   // NT tiles of 8 query rows
-__global__ void __launch_bounds__(kThreads, Few<DH, NT>::kPerSm)
+template <int DH>
+__global__ void __launch_bounds__(kThreads, kPerSm)
 attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
 {
-    constexpr int ROWS = 8 * NT, WORDS = DH / 8, BLOCKS = DH / 32;
+    constexpr int ROWS = kRows, WORDS = DH / 8, BLOCKS = DH / 32;
     constexpr int MT = DH / 16;                             // feature tiles of O^T
     constexpr int PITCH = DH + 4;
     extern __shared__ __align__(16) float s_mem[];
     float *s_part = s_mem;                                  // [kWarps][ROWS][PITCH]
-    float4 *s_in = reinterpret_cast<float4 *>(s_mem + Few<DH, NT>::kWork / 4);      // [splits][ROWS][DH / 2 / splits], what the ranks send
+    float4 *s_in = reinterpret_cast<float4 *>(s_mem + Few<DH>::kWork / 4);      // [splits][ROWS][DH / 2 / splits], what the ranks send
     __shared__ float2 s_ml[kWarps][ROWS];                   // reference maximum and denominator
     __shared__ int s_lo[ROWS], s_hi[ROWS], s_first[ROWS], s_live[ROWS];
-    __shared__ uint4 s_q[NT][WORDS / 4][32];
+    __shared__ uint4 s_q[WORDS / 4][32];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int splits = 1 << log_splits, rank = blockIdx.x & (splits - 1);
@@ -100,8 +101,8 @@ attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
     pdl_wait();
     pdl_trigger();
     // the queries, as the second operand of S^T: lane (g, t) holds row g, the features of its words in pairs (j, j + 4)
-    if (warp < NT) {
-        const int r = warp * 8 + g;
+    if (warp == 0) {
+        const int r = g;
         const int i = (row_tile * ROWS + r) / a.group, head = kv * a.group + (row_tile * ROWS + r) % a.group;
         const __nv_bfloat16 *src = a.q + ((long long)b * a.n_q + i) * a.ld_q + (long long)head * DH + t * (DH / 4);
         uint4 x[WORDS / 4];
@@ -109,8 +110,8 @@ attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
         for (int w = 0; w < WORDS / 4; ++w) x[w] = r < rows ? *reinterpret_cast<const uint4 *>(src + w * 8) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int w = 0; w < WORDS / 4; ++w)
-            s_q[warp][w][lane] = make_uint4(__byte_perm(x[w].x, x[w].z, 0x5410), __byte_perm(x[w].x, x[w].z, 0x7632), __byte_perm(x[w].y, x[w].w, 0x5410), __byte_perm(x[w].y, x[w].w, 0x7632));
-    } else if (warp == NT && lane < ROWS) {                 // meanwhile, what the rows see
+            s_q[w][lane] = make_uint4(__byte_perm(x[w].x, x[w].z, 0x5410), __byte_perm(x[w].x, x[w].z, 0x7632), __byte_perm(x[w].y, x[w].w, 0x5410), __byte_perm(x[w].y, x[w].w, 0x7632));
+    } else if (warp == 1 && lane < ROWS) {                 // meanwhile, what the rows see
         Seen s = {0, 0, 0};
         int live = 0;
         if (lane < rows) {
@@ -136,22 +137,17 @@ attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
         if (s < n_first) { j0 = s * kStep; end = first; } else { j0 = lo + (s - n_first) * kStep; end = hi; }
     };
 
-    int r_lo[NT][2], r_hi[NT][2], r_first[NT][2];           // of rows 2 t and 2 t + 1
+    int r_lo[2], r_hi[2], r_first[2];                       // of rows 2 t and 2 t + 1
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) { const int r = n * 8 + 2 * t + e; r_lo[n][e] = s_lo[r]; r_hi[n][e] = s_hi[r]; r_first[n][e] = s_first[r]; }
+    for (int e = 0; e < 2; ++e) { const int r = 2 * t + e; r_lo[e] = s_lo[r]; r_hi[e] = s_hi[r]; r_first[e] = s_first[r]; }
 
-    float o[NT][MT][4], m[NT][2], l[NT][2];
+    float o[MT][4], m[2], l[2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int e = 0; e < 2; ++e) { m[e] = -INFINITY; l[e] = 0.f; }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.f; }
+    for (int j = 0; j < MT; ++j)
 #pragma unroll
-        for (int j = 0; j < MT; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[n][j][e] = 0.f;
-    }
+        for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
     const float c = a.scale_log2 * kUnscale;
 
     // ---- a step's codes: lane -> token lane / chunks (+ 32 / chunks a copy), 16-byte chunk; its scales: lane -> token
@@ -245,75 +241,66 @@ attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
                 else { const uint2 x = *reinterpret_cast<const uint2 *>(at); kc[h][e][0] = x.x; kc[h][e][1] = x.y; }
                 f[h][e] = *reinterpret_cast<const uint32_t *>(ring + Ring<DH>::kKeyFactors + (r * BLOCKS + t * BLOCKS / 4) * 4);
             }
-        float sc[2][NT][4];
+        float sc[2][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sc[h][n][e] = 0.f;
+            for (int e = 0; e < 4; ++e) sc[h][e] = 0.f;
 #pragma unroll
         for (int w = 0; w < WORDS / 4; ++w) {
-            uint4 q[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) q[n] = s_q[n][w][lane];
+            const uint4 q = s_q[w][lane];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const uint32_t x0 = kc[h][0][w], x1 = kc[h][1][w];
                 uint32_t A[4];
                 A[0] = mul_bf16x2(codes_as_bf16<0>(x0), f[h][0]); A[1] = mul_bf16x2(codes_as_bf16<0>(x1), f[h][1]);
                 A[2] = mul_bf16x2(codes_as_bf16<1>(x0), f[h][0]); A[3] = mul_bf16x2(codes_as_bf16<1>(x1), f[h][1]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) mma_bf16(sc[h][n], A, q[n].x, q[n].y);
+                mma_bf16(sc[h], A, q.x, q.y);
                 A[0] = mul_bf16x2(codes_as_bf16<2>(x0), f[h][0]); A[1] = mul_bf16x2(codes_as_bf16<2>(x1), f[h][1]);
                 A[2] = mul_bf16x2(codes_as_bf16<3>(x0), f[h][0]); A[3] = mul_bf16x2(codes_as_bf16<3>(x1), f[h][1]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) mma_bf16(sc[h][n], A, q[n].z, q[n].w);
+                mma_bf16(sc[h], A, q.z, q.w);
             }
         }
         // ---- what the rows do not see
-        auto sees = [&](int n, int h, int e) {
+        auto sees = [&](int h, int e) {
             const int j = j0 + 16 * h + token_of(g + 8 * (e >> 1));
-            return j < end && (j < r_first[n][e & 1] || (j >= r_lo[n][e & 1] && j < r_hi[n][e & 1]));
+            return j < end && (j < r_first[e & 1] || (j >= r_lo[e & 1] && j < r_hi[e & 1]));
         };
         if (!(j0 >= all_lo && j0 + kStep <= min(end, all_hi))) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!sees(n, h, e)) sc[h][n][e] = -INFINITY;
+                for (int e = 0; e < 4; ++e)
+                    if (!sees(h, e)) sc[h][e] = -INFINITY;
         }
         // ---- softmax against a reference that follows the maximum lazily
-        uint32_t pb[2][NT][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const float x0 = fmaxf(fmaxf(sc[0][n][0], sc[0][n][2]), fmaxf(sc[1][n][0], sc[1][n][2])) * c;
-            const float x1 = fmaxf(fmaxf(sc[0][n][1], sc[0][n][3]), fmaxf(sc[1][n][1], sc[1][n][3])) * c;
-            if (__any_sync(0xffffffffu, x0 > m[n][0] + kLazy || x1 > m[n][1] + kLazy)) {
+        uint32_t pb[2][2];
+        {
+            const float x0 = fmaxf(fmaxf(sc[0][0], sc[0][2]), fmaxf(sc[1][0], sc[1][2])) * c;
+            const float x1 = fmaxf(fmaxf(sc[0][1], sc[0][3]), fmaxf(sc[1][1], sc[1][3])) * c;
+            if (__any_sync(0xffffffffu, x0 > m[0] + kLazy || x1 > m[1] + kLazy)) {
                 float y[2] = {x0, x1};
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) y[e] = fmaxf(y[e], __shfl_xor_sync(0xffffffffu, y[e], d));
-                    const float to = fmaxf(m[n][e], y[e]), alpha = to == -INFINITY ? 1.f : tc::ex2_approx(m[n][e] - to);
-                    m[n][e] = to;
-                    l[n][e] *= alpha;
+                    const float to = fmaxf(m[e], y[e]), alpha = to == -INFINITY ? 1.f : tc::ex2_approx(m[e] - to);
+                    m[e] = to;
+                    l[e] *= alpha;
 #pragma unroll
-                    for (int j = 0; j < MT; ++j) { o[n][j][e] *= alpha; o[n][j][2 + e] *= alpha; }
+                    for (int j = 0; j < MT; ++j) { o[j][e] *= alpha; o[j][2 + e] *= alpha; }
                 }
             }
             float ref[2];                                   // probabilities times 2^64
 #pragma unroll
-            for (int e = 0; e < 2; ++e) ref[e] = m[n][e] == -INFINITY ? 0.f : 64.f - m[n][e];
+            for (int e = 0; e < 2; ++e) ref[e] = m[e] == -INFINITY ? 0.f : 64.f - m[e];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 float p[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[e] = tc::ex2_approx(fmaf(sc[h][n][e], c, ref[e & 1]));
-                l[n][0] += p[0] + p[2]; l[n][1] += p[1] + p[3];
-                pb[h][n][0] = transpose8(pack_bf16(p[0], p[1])); pb[h][n][1] = transpose8(pack_bf16(p[2], p[3]));
+                for (int e = 0; e < 4; ++e) p[e] = tc::ex2_approx(fmaf(sc[h][e], c, ref[e & 1]));
+                l[0] += p[0] + p[2]; l[1] += p[1] + p[3];
+                pb[h][0] = transpose8(pack_bf16(p[0], p[1])); pb[h][1] = transpose8(pack_bf16(p[2], p[3]));
             }
         }
         // ---- values: rows 2 t, 2 t + 1, 2 t + 8 and 2 t + 9 of either tile
@@ -342,8 +329,7 @@ attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
                     for (int w = 0; w < 2; ++w) A[2 * e + w] = mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[e][w]), fv[e]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) mma_bf16(o[n][j], A, pb[h][n][0], pb[h][n][1]);
+                mma_bf16(o[j], A, pb[h][0], pb[h][1]);
             };
             product(std::integral_constant<int, 0>(), 0, lo4); product(std::integral_constant<int, 1>(), 1, lo4);
             product(std::integral_constant<int, 2>(), 2, lo4); product(std::integral_constant<int, 3>(), 3, lo4);
@@ -363,18 +349,15 @@ attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
                     const uint32_t b0 = __shfl_sync(0xffffffffu, above[1], 16 * h + token_of(2 * t + 8 * e)) & bit, b1 = __shfl_sync(0xffffffffu, above[1], 16 * h + token_of(2 * t + 1 + 8 * e)) & bit;
                     A[2 * e] = A[2 * e + 1] = (b0 ? 0x3F80u : 0u) | (b1 ? 0x3F800000u : 0u);
                 }
+                float in[4], count[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float in[4], count[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int e = 0; e < 4; ++e) in[e] = sees(h, e) ? 1.f : 0.f;
+                mma_bf16(count, A, transpose8(pack_bf16(in[0], in[1])), transpose8(pack_bf16(in[2], in[3])));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) in[e] = sees(n, h, e) ? 1.f : 0.f;
-                    mma_bf16(count, A, transpose8(pack_bf16(in[0], in[1])), transpose8(pack_bf16(in[2], in[3])));
+                for (int e = 0; e < 4; ++e)
+                    if (count[e] != 0.f)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (count[e] != 0.f)
-#pragma unroll
-                            for (int j = 0; j < MT; ++j) o[n][j][e] = __uint_as_float(0x7FC00000u);
-                }
+                        for (int j = 0; j < MT; ++j) o[j][e] = __uint_as_float(0x7FC00000u);
             }
         }
     }
@@ -383,21 +366,18 @@ attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
     copies_wait();
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int e = 0; e < 2; ++e) {
+        float x = l[e];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float x = l[n][e];
+        for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        if (g == 0) s_ml[warp][2 * t + e] = make_float2(m[e], x);
+    }
 #pragma unroll
-            for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-            if (g == 0) s_ml[warp][n * 8 + 2 * t + e] = make_float2(m[n][e], x);
-        }
+    for (int e = 0; e < 4; ++e) {                           // rows 2 t + (e & 1); features of the lane's first or second word (or half word)
+        const int r = 2 * t + (e & 1);
+        if (r < rows)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {                       // rows 2 t + (e & 1); features of the lane's first or second word (or half word)
-            const int r = n * 8 + 2 * t + (e & 1);
-            if (r < rows)
-#pragma unroll
-                for (int j = 0; j < MT; ++j) s_part[(warp * ROWS + r) * PITCH + g * (DH / 8) + (e >> 1) * (DH / 16) + j] = o[n][j][e];
-        }
+            for (int j = 0; j < MT; ++j) s_part[(warp * ROWS + r) * PITCH + g * (DH / 8) + (e >> 1) * (DH / 16) + j] = o[j][e];
     }
     __syncthreads();
     auto finish = [&](int r, int pair, float x, float y, float den) {
@@ -443,22 +423,33 @@ attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
     }
 }
 
-template <int DH, int NT>
-int32_t launch_few(const Cache4Args &a, cudaStream_t stream)
+// How the tokens are divided: one wave of CTAs, whole steps for every warp.
+int splits_of(long long items, long long tokens)
 {
-    constexpr int ROWS = 8 * NT;
-    constexpr size_t shared = Few<DH, NT>::kWork + (size_t)ROWS * (DH / 2) * 16;
-    const int row_tiles = (int)(((long long)a.n_q * a.group + ROWS - 1) / ROWS);
-    const long long items = (long long)a.batch * a.n_kv * row_tiles;
-    const int slots = gemm_num_sms() * Few<DH, NT>::kPerSm;
-    int log_splits = 0;                                     // one wave of CTAs, whole steps for every warp
-    while ((1 << log_splits) < kMaxSplits && (items << (log_splits + 1)) <= slots && a.capacity >= (kWarps * kStep) << (log_splits + 1)) ++log_splits;
-    const int splits = 1 << log_splits;
-    SFS_REQUIRE(items * splits <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
-    SFS_CUDA(allow_shared(attention_cache4_few<DH, NT>, shared));
-    if (splits > 8) SFS_CUDA(cudaFuncSetAttribute(attention_cache4_few<DH, NT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    if (splits > 1) SFS_CUDA(launch_pdl_cluster(attention_cache4_few<DH, NT>, splits, dim3((unsigned)(items * splits)), dim3(kThreads), shared, stream, a, log_splits, row_tiles));
-    else SFS_CUDA(launch_pdl(attention_cache4_few<DH, NT>, dim3((unsigned)items), dim3(kThreads), shared, stream, a, log_splits, row_tiles));
+    int log_splits = 0;
+    while ((1 << log_splits) < kMaxSplits && (items << (log_splits + 1)) <= (long long)gemm_num_sms() * kPerSm && tokens >= (kWarps * kStep) << (log_splits + 1)) ++log_splits;
+    return log_splits;
+}
+
+// Microseconds of a call here, to choose between this kernel and the tensor-memory one: 4.5 for start and join, 2 (one CTA on an SM) or
+// 2.75 (two) for a step of 32 tokens of a warp.  attention_cache4_many_us is the other side, with what both measured.
+double few_us(long long items, long long tokens, int log_splits)
+{
+    const long long ctas = items << log_splits, sms = gemm_num_sms(), rounds = (ctas + sms * kPerSm - 1) / (sms * kPerSm);
+    const long long steps = (tokens + ((long long)(kWarps * kStep) << log_splits) - 1) / ((long long)(kWarps * kStep) << log_splits);
+    return (ctas <= sms ? 2.0 : 2.75) * (double)steps * rounds + 4.5;
+}
+
+template <int DH>
+int32_t launch_few(const Cache4Args &a, int row_tiles, int log_splits, cudaStream_t stream)
+{
+    constexpr size_t shared = Few<DH>::kWork + (size_t)kRows * (DH / 2) * 16;
+    const long long ctas = ((long long)a.batch * a.n_kv * row_tiles) << log_splits;
+    SFS_REQUIRE(ctas <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
+    SFS_CUDA(allow_shared(attention_cache4_few<DH>, shared));
+    if (log_splits > 3) SFS_CUDA(cudaFuncSetAttribute(attention_cache4_few<DH>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    if (log_splits > 0) SFS_CUDA(launch_pdl_cluster(attention_cache4_few<DH>, 1 << log_splits, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, log_splits, row_tiles));
+    else SFS_CUDA(launch_pdl(attention_cache4_few<DH>, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, log_splits, row_tiles));
     return SFS_OK;
 }
 
@@ -488,13 +479,16 @@ extern "C" int32_t sfs_attention_cache4(const sfs_cache4 *cache, const void *d_q
                     cache->batch, cache->capacity, cache->n_kv_heads, n_heads / cache->n_kv_heads,
                     (const __nv_bfloat16 *)d_q, (long long)ld_q, (__nv_bfloat16 *)d_out, (long long)ld_out, n_q, d_lengths, d_positions,
                     left, right, sinks, (float)(1.4426950408889634 / sqrt((double)cache->head_dim)), nullptr};
-    const int64_t rows = (int64_t)n_q * a.group;
-    if (rows > 16) {
+    const int64_t rows = (int64_t)n_q * a.group, heads = (int64_t)cache->batch * cache->n_kv_heads;
+    // tokens that a row sees at most, the rows being neighbours where there is a window
+    const int64_t tokens = left >= 0 && right >= 0 ? std::min<int64_t>(cache->capacity, (int64_t)left + right + n_q + sinks) : cache->capacity;
+    const int64_t row_tiles = (rows + kRows - 1) / kRows;
+    const int log_splits = splits_of(heads * row_tiles, tokens);
+    if (rows > kRows && attention_cache4_many_us(a, tokens) < few_us(heads * row_tiles, tokens, log_splits)) {
         a.err = device_status_word();
         SFS_REQUIRE(a.err != nullptr, SFS_ERR_OOM, "cannot allocate the device status word");
-        return attention_cache4_many(a, cache->head_dim, (cudaStream_t)stream);
+        return attention_cache4_many(a, tokens, cache->head_dim, (cudaStream_t)stream);
     }
-    const bool one = rows <= 8;
-    if (cache->head_dim == 128) return one ? launch_few<128, 1>(a, (cudaStream_t)stream) : launch_few<128, 2>(a, (cudaStream_t)stream);
-    return one ? launch_few<64, 1>(a, (cudaStream_t)stream) : launch_few<64, 2>(a, (cudaStream_t)stream);
+    SFS_REQUIRE(row_tiles <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows for one call");
+    return cache->head_dim == 128 ? launch_few<128>(a, (int)row_tiles, log_splits, (cudaStream_t)stream) : launch_few<64>(a, (int)row_tiles, log_splits, (cudaStream_t)stream);
 }

@@ -554,16 +554,34 @@ int32_t launch(const Cache4Args &a, int log_splits, cudaStream_t stream)
     return SFS_OK;
 }
 
-}  // namespace
-
-int32_t attention_cache4_many(const Cache4Args &a, int head_dim, cudaStream_t stream)
+// pairs of row tiles where they fill the machine; else up to one wave of CTAs, two key tiles for each
+struct Many { bool pair; int log_splits; long long ctas, key_tiles; };
+Many plan(const Cache4Args &a, int64_t tokens)
 {
     const long long row_tiles = ((long long)a.n_q * a.group + QT - 1) / QT, heads = (long long)a.batch * a.n_kv, sms = gemm_num_sms();
-    if (row_tiles > 1 && heads * ((row_tiles + 1) / 2) >= sms)               // pairs of row tiles fill the machine
-        return head_dim == 128 ? launch<128, true>(a, 0, stream) : launch<64, true>(a, 0, stream);
-    int log_splits = 0;                                     // up to one wave of CTAs, two key tiles for each
-    while (log_splits < 3 && (heads * row_tiles << (log_splits + 1)) <= sms && a.capacity > (2 * KT) << log_splits) ++log_splits;
-    return head_dim == 128 ? launch<128, false>(a, log_splits, stream) : launch<64, false>(a, log_splits, stream);
+    Many p = {row_tiles > 1 && heads * ((row_tiles + 1) / 2) >= sms, 0, 0, 0};
+    if (!p.pair)
+        while (p.log_splits < 3 && (heads * row_tiles << (p.log_splits + 1)) <= sms && tokens > (2 * KT) << p.log_splits) ++p.log_splits;
+    p.ctas = heads * (p.pair ? (row_tiles + 1) / 2 : row_tiles) << p.log_splits;
+    const long long tiles = (tokens + KT - 1) / KT;
+    p.key_tiles = (tiles + (1 << p.log_splits) - 1) >> p.log_splits;
+    return p;
+}
+
+}  // namespace
+
+double attention_cache4_many_us(const Cache4Args &a, int64_t tokens)
+{
+    const Many p = plan(a, tokens);
+    const long long rounds = (p.ctas + gemm_num_sms() - 1) / gemm_num_sms();
+    return rounds * (7.5 + (p.pair ? 3.1 : 2.4) * p.key_tiles) + (p.log_splits > 0 ? 3.5 : 0.0);
+}
+
+int32_t attention_cache4_many(const Cache4Args &a, int64_t tokens, int head_dim, cudaStream_t stream)
+{
+    const Many p = plan(a, tokens);
+    if (p.pair) return head_dim == 128 ? launch<128, true>(a, 0, stream) : launch<64, true>(a, 0, stream);
+    return head_dim == 128 ? launch<128, false>(a, p.log_splits, stream) : launch<64, false>(a, p.log_splits, stream);
 }
 
 }  // namespace sfs
