@@ -24,7 +24,7 @@ constexpr int kCodes = 128;                                 // bytes of a row in
 constexpr int kScaleTile = 512;                             // 128 rows x 4 blocks
 
 template <int BN> struct Shape {
-    static constexpr int kRowTiles = BN > 128 ? 2 : 1;      // scale tiles along the columns' rows
+    static constexpr int kRowTiles = BN > 128 ? 2 : 1;      // scale tiles along the columns' rows (a tile of 192 starts in the middle of one, or ends there)
     static constexpr int kA = 128 * kCodes, kB = BN * kCodes;
     static constexpr int kScaleA = 2 * kScaleTile, kScaleB = kRowTiles * 2 * kScaleTile;
     static constexpr int kStage = kA + kB + kScaleA + kScaleB;
@@ -132,6 +132,7 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits;
     const int col_tile = tile % a.col_tiles, lane_tile = tile / a.col_tiles;
+    const int scale_tile = col_tile * BN / 128;             // the first one of the columns' rows
     const int n_steps = (a.blocks + kDepth / 32 - 1) / (kDepth / 32);
     const int first = (int)((long long)n_steps * split / a.splits), last = (int)((long long)n_steps * (split + 1) / a.splits);
     const uint32_t full = tc::smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
@@ -159,13 +160,13 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
             for (int k = first, s = 0, ph = 0; k < last; ++k) {
                 if (!tc::mbar_wait(empty + 8 * s, (uint32_t)ph ^ 1u, &s_abort)) break;
                 const uint32_t bar = full + 8 * s, part = (uint32_t)min(2, a.quads - 2 * k) * kScaleTile;   // (the last stage may hold one tile of scales)
-                const bool second = S::kRowTiles == 2 && (col_tile * 2 + 1) * 128 < a.cols;
+                const bool second = S::kRowTiles == 2 && (scale_tile + 1) * 128 < a.cols;
                 tc::mbar_expect_tx(bar, (uint32_t)(S::kA + S::kB) + part * (second ? 3u : 2u));
                 tc::tma_load_2d(codes_of(s), &tm_lanes, k * (kCodes / 2), lane_tile * 128, bar);
                 tc::tma_load_2d(codes_of(s) + S::kA, &tm_cols, k * (kCodes / 2), col_tile * BN, bar);
                 bulk_load(scales_of(s), a.lane_scales + ((size_t)lane_tile * a.quads + 2 * k) * kScaleTile, part, bar);
-                bulk_load(scales_of(s) + S::kScaleA, a.col_scales + ((size_t)col_tile * S::kRowTiles * a.quads + 2 * k) * kScaleTile, part, bar);
-                if (second) bulk_load(scales_of(s) + 2 * S::kScaleA, a.col_scales + ((size_t)(col_tile * 2 + 1) * a.quads + 2 * k) * kScaleTile, part, bar);
+                bulk_load(scales_of(s) + S::kScaleA, a.col_scales + ((size_t)scale_tile * a.quads + 2 * k) * kScaleTile, part, bar);
+                if (second) bulk_load(scales_of(s) + 2 * S::kScaleA, a.col_scales + ((size_t)(scale_tile + 1) * a.quads + 2 * k) * kScaleTile, part, bar);
                 issued = k + 1;
                 if (++s == S::kStages) { s = 0; ph ^= 1; }
             }
@@ -177,7 +178,7 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
         }
         __syncwarp();
     } else if (warp == 1) {
-        const uint32_t tmem_scales = tmem + BN;
+        const uint32_t tmem_scales = tmem + BN, skip = (uint32_t)(col_tile * BN % 128 / 32);          // (the columns' first row in its scale tile)
         bool ok = true;
         for (int k = first, s = 0, ph = 0; k < last; ++k) {
             ok = __all_sync(0xffffffffu, tc::mbar_wait(full + 8 * s, (uint32_t)ph, &s_abort));
@@ -195,7 +196,7 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (i < mmas)
-                    mma_mxf4_elect(tmem, da + (uint64_t)(2 * i), db + (uint64_t)(2 * i), idesc_mxf4(BN, i & 1), ta + 4 * (i >> 1), tb + (i >> 1) * 4 * S::kRowTiles,
+                    mma_mxf4_elect(tmem, da + (uint64_t)(2 * i), db + (uint64_t)(2 * i), idesc_mxf4(BN, i & 1), ta + 4 * (i >> 1), tb + (i >> 1) * 4 * S::kRowTiles + skip,
                                    (k != first || i != 0) ? 1u : 0u);
             tc::mma_commit_elect(empty + 8 * s);
             if (++s == S::kStages) { s = 0; ph ^= 1; }
@@ -262,6 +263,35 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
     if (threadIdx.x == 0 && s_abort && a.err) atomicExch(a.err, SFS_ERR_TIMEOUT);
 }
 
+// Which operand lies on the lanes, how many rows of the other a tile has, and over how many CTAs its k-steps are divided.  A step costs what
+// it takes to bring it to the SM, about 55 bytes a clock, shared by the CTAs of an SM, which is more than its MMAs take in every shape here;
+// a tile 6000 clocks around its steps, a join 2500 more.  (us, 128 x 24576 x 4096: 192 tiles of 128 x 128 16.9, 128 of 128 x 192 XXX.)
+struct Tiles { bool features_on_lanes; int bn, splits; };
+Tiles choose_tiles(int M, int N, int n_steps)
+{
+    const long long sms = gemm_num_sms();
+    Tiles best = {};
+    double best_clk = 1e30;
+    auto consider = [&](bool features_on_lanes, int bn, int splits) {
+        const long long lanes = features_on_lanes ? N : M, cols = features_on_lanes ? M : N;
+        const long long tiles = (lanes + 127) / 128 * ((cols + bn - 1) / bn), ctas = tiles * splits, per_sm = bn > 128 ? 1 : 2;
+        const double bytes = (std::min<double>(128, (double)lanes) + std::min<double>(bn, (double)cols)) * 136 + 1024;
+        // whole rounds of the machine; the last one may leave SMs with one CTA
+        const long long full = ctas / (sms * per_sm), rest = ctas - full * sms * per_sm;
+        const double step = bytes / 55, steps = (double)((n_steps + splits - 1) / splits);
+        const double clk = full * (steps * step * per_sm + 6000) + (rest == 0 ? 0 : steps * step * (rest > sms ? per_sm : 1) + 6000) + (splits > 1 ? 2500 : 0);
+        if (clk < best_clk) { best_clk = clk; best = {features_on_lanes, bn, splits}; }
+    };
+    if (M <= 128)
+        for (int splits = 1; splits <= 8 && (splits == 1 || n_steps >= 2 * splits); splits *= 2) consider(true, M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, splits);
+    if (M > 64) {
+        for (int splits = 1; splits <= 8 && (splits == 1 || n_steps >= 2 * splits); splits *= 2) consider(false, 128, splits);
+        consider(false, 192, 1);
+        consider(false, 256, 1);
+    }
+    return best;
+}
+
 int32_t codes_map(CUtensorMap *out, const void *base, uint64_t rows, uint64_t bytes, uint64_t ld, uint32_t box_rows)
 {
     // pairs of code bytes as 16-bit elements: 64 of them are one swizzled row
@@ -305,15 +335,11 @@ extern "C" int32_t sfs_linear_mx4(const void *d_A, int64_t lda, const void *d_A_
     int32_t *err = device_status_word();
     SFS_REQUIRE(err != nullptr, SFS_ERR_OOM, "cannot allocate the device status word");
 
-    const bool features_on_lanes = M <= 128;
-    const int lanes = features_on_lanes ? N : M, cols = features_on_lanes ? M : N;
-    const int lane_tiles = (lanes + 127) / 128, n_steps = (K + kDepth - 1) / kDepth, sms = gemm_num_sms();
-    int bn = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
-    if (!features_on_lanes && (long long)lane_tiles * ((cols + 255) / 256) > sms) bn = 256;
+    const int n_steps = (K + kDepth - 1) / kDepth;
+    const Tiles t = choose_tiles(M, N, n_steps);
+    const bool features_on_lanes = t.features_on_lanes;
+    const int lanes = features_on_lanes ? N : M, cols = features_on_lanes ? M : N, bn = t.bn, splits = t.splits;
     const int col_tiles = (cols + bn - 1) / bn;
-    int splits = 1;
-    if (bn <= 128)
-        while (splits < 8 && (long long)lane_tiles * col_tiles * splits * 2 <= 2 * sms && n_steps >= splits * 4) splits *= 2;
     Mx4Args a = {};
     a.lane_scales = (const uint8_t *)(features_on_lanes ? d_B_scales : d_A_scales);
     a.col_scales = (const uint8_t *)(features_on_lanes ? d_A_scales : d_B_scales);
@@ -326,6 +352,7 @@ extern "C" int32_t sfs_linear_mx4(const void *d_A, int64_t lda, const void *d_A_
     case 16: return launch<16>(a, lp, ll, cp, lc, (cudaStream_t)stream);
     case 32: return launch<32>(a, lp, ll, cp, lc, (cudaStream_t)stream);
     case 64: return launch<64>(a, lp, ll, cp, lc, (cudaStream_t)stream);
+    case 192: return launch<192>(a, lp, ll, cp, lc, (cudaStream_t)stream);
     case 128: return launch<128>(a, lp, ll, cp, lc, (cudaStream_t)stream);
     default: return launch<256>(a, lp, ll, cp, lc, (cudaStream_t)stream);
     }

@@ -115,6 +115,80 @@ def test_what_is_masked_may_hold_anything(n_q):
     c.check(lengths=lengths, positions=pos, left=9, right=2, sinks=3)
 
 
+# Enough rows and heads for the tensor-memory kernel, which few rows of a small case do not reach: one row tile per key head, pairs of them,
+# and key tiles divided over clusters of two to eight.
+MANY = [(8, 500, 8, 8, 128, 130), (4, 300, 20, 20, 64, 128), (1, 700, 40, 40, 128, 200), (2, 260, 96, 96, 64, 140), (1, 1100, 64, 2, 128, 60), (1, 2000, 8, 1, 64, 300),
+        (2, 900, 10, 2, 128, 400), (1, 3000, 16, 1, 128, 60), (1, 1500, 6, 6, 128, 1000), (3, 129, 50, 50, 128, 129), (1, 4000, 12, 4, 64, 350)]
+
+
+@pytest.mark.parametrize("batch,capacity,heads,kv,dim,n_q", MANY)
+def test_many_rows(batch, capacity, heads, kv, dim, n_q):
+    c = Case(batch, capacity, heads, kv, dim, n_q, seed=capacity)
+    c.check()
+    c.check(lengths=c.rng.integers(0, capacity + 1, size=batch), ld_pad=8)
+
+
+@pytest.mark.parametrize("batch,capacity,heads,kv,dim,n_q", MANY)
+@pytest.mark.parametrize("left,right,sinks", [(-1, 0, 0), (100, 100, 5), (300, 20, 0), (200, -1, 130)])
+def test_many_rows_with_windows(batch, capacity, heads, kv, dim, n_q, left, right, sinks):
+    c = Case(batch, capacity, heads, kv, dim, n_q, seed=capacity + left)
+    pos = c.rng.integers(0, capacity, size=(batch, n_q))
+    pos[:, 3] = -1
+    c.check(left=left, right=right, sinks=sinks)
+    c.check(lengths=c.rng.integers(capacity // 2, capacity + 1, size=batch), positions=pos, left=left, right=right, sinks=sinks)
+
+
+@pytest.mark.parametrize("batch,capacity,heads,kv,dim,n_q", [MANY[0], MANY[3], MANY[4], MANY[6]])
+def test_many_rows_beside_nan_and_infinite_values(batch, capacity, heads, kv, dim, n_q):
+    c = Case(batch, capacity, heads, kv, dim, n_q, seed=7)
+    v, k = (x.reshape(batch, capacity, kv, dim // 32) for x in (c.scales[1], c.scales[0]))
+    v[:, 40:44, 0, 1], v[:, capacity // 2, :, 0], v[0, capacity - 1] = 255, 200, 255
+    k[:, 90, 0], k[0, capacity - 1] = 255, 193
+    width = 20
+    pos = c.rng.integers(0, capacity, size=(batch, n_q))
+    pos[:, :4] = 300 % capacity
+    c.check(positions=pos, left=width, right=width, sinks=2)
+    lengths = np.full(batch, capacity - 1)                  # the last token hidden by the length
+    c.check(lengths=lengths, left=200, right=0)
+
+
+def test_many_rows_that_see_nothing():
+    c = Case(8, 400, 8, 8, 128, 130, seed=1)
+    pos = c.rng.integers(0, 400, size=(8, 130))
+    pos[:, -1] = -1
+    pos[2] = -1                                             # a whole sequence left as it was
+    c.check(lengths=[0, 400, 100, 1, 0, 399, 1000, -3], positions=pos)
+    c.check(lengths=[0, 400, 100, 1, 0, 399, 1000, -3], positions=pos, left=4, right=4)
+    c = Case(1, 1100, 64, 2, 128, 60, seed=1)               # clusters, some of whose CTAs have no tile
+    c.check(lengths=[0])
+    c.check(lengths=[130])
+
+
+@pytest.mark.parametrize("sharp", [0.0, 30.0])
+def test_many_rows_with_flat_and_peaked_scores(sharp):
+    Case(8, 500, 8, 8, 128, 130, seed=2, sharp=sharp).check()
+    Case(1, 1100, 64, 2, 64, 60, seed=2, sharp=sharp).check()
+
+
+def test_many_rows_with_scales_over_their_whole_range():
+    c = Case(8, 300, 8, 8, 128, 140, seed=8)
+    c.scales[1][:] = c.rng.integers(65, 193, size=c.scales[1].shape)
+    c.scales[0][:] = 127 - 10
+    c.check()
+
+
+def test_many_rows_with_infinite_and_nan_queries():
+    c = Case(8, 300, 8, 8, 64, 140, seed=3)
+    c.codes[0][:, :, 0] = 2
+    q = c.q.clone()
+    q[1, 0], q[2, 5] = float("inf"), float("nan")
+    c.q = q
+    got = c.run()
+    assert np.isnan(got[1, :64]).all() and np.isnan(got[2, :64]).all() and not np.isnan(got[1:3, 64:]).any()
+    assert not np.isnan(np.delete(got, [1, 2], 0)).any()
+    assert np.array_equal(got, c.run(), equal_nan=True)
+
+
 @pytest.mark.parametrize("sharp", [0.0, 30.0])
 def test_flat_and_peaked_scores(sharp):
     for n_q in (1, 130):
