@@ -10,7 +10,7 @@
 //
 // Few tiles: K is divided over a cluster of up to 8 CTAs, whose 32-bit partial sums are exchanged through shared memory and added
 // in the order of the ranks, so no workspace and no atomics are needed and the same call gives the same bits.
-#include "mx4.cuh"
+#include "mx4_gemm.cuh"
 #include "tc05.cuh"
 #include "gemm.cuh"
 #include <algorithm>
@@ -19,40 +19,23 @@ namespace sfs {
 namespace {
 
 constexpr int kThreads = 192;
-constexpr int kDepth = 256;                                 // columns of a stage
-constexpr int kCodes = 128;                                 // bytes of a row in a stage
-constexpr int kScaleTile = 512;                             // 128 rows x 4 blocks
+using namespace mx4;
 
 template <int BN> struct Shape {
     static constexpr int kRowTiles = BN > 128 ? 2 : 1;      // scale tiles along the columns' rows (a tile of 192 starts in the middle of one, or ends there)
     static constexpr int kA = 128 * kCodes, kB = BN * kCodes;
     static constexpr int kScaleA = 2 * kScaleTile, kScaleB = kRowTiles * 2 * kScaleTile;
     static constexpr int kStage = kA + kB + kScaleA + kScaleB;
-    static constexpr int kPerSm = BN > 128 ? 1 : 2;
-    static constexpr int kStages = (kPerSm == 1 ? 210 * 1024 : 106 * 1024) / kStage;
     static constexpr int kScaleCols = 8 + 8 * kRowTiles;    // tensor-memory columns of a stage's scales
+    static constexpr int kMaxStages = 210 * 1024 / kStage;
+    // stages of the ring with one or two CTAs on an SM: a lone CTA needs twice as many, or the memory's latency sets its pace
+    static constexpr int stages(int per_sm) { return (per_sm == 1 ? 210 * 1024 : 106 * 1024) / kStage; }
     // every stage has scales of its own in tensor memory: a copy may overtake an MMA issued before it, but not the stage's release
-    static constexpr int kColumns = BN + kStages * kScaleCols;
-    static constexpr int kTmem = kColumns <= 64 ? 64 : kColumns <= 128 ? 128 : kColumns <= 256 ? 256 : 512;
-    static constexpr int kBarriers = 2 * kStages + 1;
-    static constexpr int kShared = kStages * kStage + 1024 /* alignment */ + kBarriers * 8 + 16;
-    static_assert(kB % 1024 == 0 && kColumns <= kTmem && kPerSm * kTmem <= 512, "tile");
-    static_assert(kStages * kStage >= 128 * BN * 4 || BN > 128, "partial sums fit the ring");
+    static constexpr uint32_t tmem_columns(int stages) { const int n = BN + stages * kScaleCols; return n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
+    static constexpr int shared(int stages) { return stages * kStage + 1024 /* alignment */ + (2 * stages + 1) * 8 + 16; }
+    static_assert(kB % 1024 == 0 && BN + stages(1) * kScaleCols <= 512 && 2 * tmem_columns(stages(2)) <= 512 + (BN > 128 ? 512 : 0), "tile");
+    static_assert(stages(2) * kStage >= 128 * BN * 4 || BN > 128, "partial sums fit the ring");
 };
-
-struct Mx4Args {
-    const uint8_t *lane_scales, *col_scales;
-    void *C; long long ldc;
-    int lanes, cols;                                        // rows of the two operands
-    int blocks, quads;                                      // blocks of 32 columns in a row, tiles of four of them
-    int col_tiles, splits;
-    int out_f32, features_on_lanes, wide;                   // wide: rows of C take 16-byte stores
-    float scale;
-    int32_t *err;
-};
-
-// kind::mxf4, both operands e2m1 and K-major, E8M0 scales of 32 columns, fp32 accumulator; `half`: which two of a column's four scale bytes
-constexpr uint32_t idesc_mxf4(int N, int half) { return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | (1u << 27) | ((uint32_t)(2 * half) << 29); }
 
 __device__ __forceinline__ void mma_mxf4_elect(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, uint32_t accumulate)
 {
@@ -63,9 +46,8 @@ __device__ __forceinline__ void mma_mxf4_elect(uint32_t d, uint64_t a, uint64_t 
 // 32 rows of 16 bytes -> the same 32 lanes of all four quarters of tensor memory, four columns
 __device__ __forceinline__ void copy_scales_elect(uint32_t tmem, uint32_t smem)
 {
-    const uint64_t d = (uint64_t)((smem >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
     asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\t"
-                 "@P tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem), "l"(d) : "memory");
+                 "@P tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem), "l"(scale_desc(smem)) : "memory");
 }
 __device__ __forceinline__ void bulk_load(uint32_t smem, const void *global, uint32_t bytes, uint32_t bar)
 {
@@ -117,16 +99,16 @@ __device__ __forceinline__ void store_columns(const Mx4Args &a, int lane, int co
 }
 
 template <int BN>
-__global__ void __launch_bounds__(kThreads, Shape<BN>::kPerSm)
-linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_constant__ CUtensorMap tm_cols, Mx4Args a)
+__global__ void __launch_bounds__(kThreads, BN > 128 ? 1 : 2)
+linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_constant__ CUtensorMap tm_cols, Mx4Args a, int stages, uint32_t tmem_columns)
 {
     using S = Shape<BN>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     // codes first (1024-byte aligned), then every stage's scales
-    uint8_t *scales = ring + S::kStages * (S::kA + S::kB);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(ring + S::kStages * S::kStage);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + S::kBarriers);
+    uint8_t *scales = ring + stages * (S::kA + S::kB);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(ring + stages * S::kStage);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + (2 * stages + 1));
     __shared__ int s_abort;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -135,16 +117,16 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
     const int scale_tile = col_tile * BN / 128;             // the first one of the columns' rows
     const int n_steps = (a.blocks + kDepth / 32 - 1) / (kDepth / 32);
     const int first = (int)((long long)n_steps * split / a.splits), last = (int)((long long)n_steps * (split + 1) / a.splits);
-    const uint32_t full = tc::smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
+    const uint32_t full = tc::smem_u32(bars), empty = full + 8 * stages, done = empty + 8 * stages;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kStages; ++s) { tc::mbar_init(full + 8 * s, 1); tc::mbar_init(empty + 8 * s, 1); }
+        for (int s = 0; s < stages; ++s) { tc::mbar_init(full + 8 * s, 1); tc::mbar_init(empty + 8 * s, 1); }
         tc::mbar_init(done, 1);
         s_abort = 0;
         tc::mbar_init_fence();
     }
     if (warp == 0 && lane == 0) { tc::tma_prefetch_desc(&tm_lanes); tc::tma_prefetch_desc(&tm_cols); }
-    if (warp == 1) { tc::tmem_alloc(tc::smem_u32(tmem_slot), S::kTmem); tc::tmem_relinquish(); }
+    if (warp == 1) { tc::tmem_alloc(tc::smem_u32(tmem_slot), tmem_columns); tc::tmem_relinquish(); }
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
@@ -168,11 +150,11 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
                 bulk_load(scales_of(s) + S::kScaleA, a.col_scales + ((size_t)scale_tile * a.quads + 2 * k) * kScaleTile, part, bar);
                 if (second) bulk_load(scales_of(s) + 2 * S::kScaleA, a.col_scales + ((size_t)(scale_tile + 1) * a.quads + 2 * k) * kScaleTile, part, bar);
                 issued = k + 1;
-                if (++s == S::kStages) { s = 0; ph ^= 1; }
+                if (++s == stages) { s = 0; ph ^= 1; }
             }
             if (s_abort)                                    // copies in flight get a bounded time to land before the CTA retires
-                for (int k = max(first, issued - S::kStages); k < issued; ++k) {
-                    const int s = (k - first) % S::kStages, ph = ((k - first) / S::kStages) & 1;
+                for (int k = max(first, issued - stages); k < issued; ++k) {
+                    const int s = (k - first) % stages, ph = ((k - first) / stages) & 1;
                     for (int i = 0; i < (1 << 16) && !tc::mbar_try(full + 8 * s, (uint32_t)ph); ++i) {}
                 }
         }
@@ -196,10 +178,10 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (i < mmas)
-                    mma_mxf4_elect(tmem, da + (uint64_t)(2 * i), db + (uint64_t)(2 * i), idesc_mxf4(BN, i & 1), ta + 4 * (i >> 1), tb + (i >> 1) * 4 * S::kRowTiles + skip,
+                    mma_mxf4_elect(tmem, da + (uint64_t)(2 * i), db + (uint64_t)(2 * i), idesc_mxf4(128, BN, i & 1), ta + 4 * (i >> 1), tb + (i >> 1) * 4 * S::kRowTiles + skip,
                                    (k != first || i != 0) ? 1u : 0u);
             tc::mma_commit_elect(empty + 8 * s);
-            if (++s == S::kStages) { s = 0; ph ^= 1; }
+            if (++s == stages) { s = 0; ph ^= 1; }
         }
         if (ok) tc::mma_commit_elect(done);
         __syncwarp();
@@ -259,14 +241,14 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (warp == 1) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, S::kTmem); }
+    if (warp == 1) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, tmem_columns); }
     if (threadIdx.x == 0 && s_abort && a.err) atomicExch(a.err, SFS_ERR_TIMEOUT);
 }
 
-// Which operand lies on the lanes, how many rows of the other a tile has, and over how many CTAs its k-steps are divided.  A step costs what
-// it takes to bring it to the SM, about 55 bytes a clock, shared by the CTAs of an SM, which is more than its MMAs take in every shape here;
-// a tile 6000 clocks around its steps, a join 2500 more.  (us, 128 x 24576 x 4096: 192 tiles of 128 x 128 16.9, 128 of 128 x 192 XXX.)
-struct Tiles { bool features_on_lanes; int bn, splits; };
+// Which operand lies on the lanes, how many rows of the other a tile has, and over how many CTAs its k-steps are divided; or pairs of CTAs.
+// A step costs what it takes to bring it to the SM, about 55 bytes a clock, shared by the CTAs of an SM, which is more than its MMAs take in
+// every shape here; a tile 6000 clocks around its steps, a join 2500 more.
+struct Tiles { bool features_on_lanes, pairs; int bn, splits; };
 Tiles choose_tiles(int M, int N, int n_steps)
 {
     const long long sms = gemm_num_sms();
@@ -274,13 +256,13 @@ Tiles choose_tiles(int M, int N, int n_steps)
     double best_clk = 1e30;
     auto consider = [&](bool features_on_lanes, int bn, int splits) {
         const long long lanes = features_on_lanes ? N : M, cols = features_on_lanes ? M : N;
-        const long long tiles = (lanes + 127) / 128 * ((cols + bn - 1) / bn), ctas = tiles * splits, per_sm = bn > 128 ? 1 : 2;
+        const long long ctas = (lanes + 127) / 128 * ((cols + bn - 1) / bn) * splits, per_sm = bn > 128 ? 1 : 2;
         const double bytes = (std::min<double>(128, (double)lanes) + std::min<double>(bn, (double)cols)) * 136 + 1024;
         // whole rounds of the machine; the last one may leave SMs with one CTA
         const long long full = ctas / (sms * per_sm), rest = ctas - full * sms * per_sm;
         const double step = bytes / 55, steps = (double)((n_steps + splits - 1) / splits);
         const double clk = full * (steps * step * per_sm + 6000) + (rest == 0 ? 0 : steps * step * (rest > sms ? per_sm : 1) + 6000) + (splits > 1 ? 2500 : 0);
-        if (clk < best_clk) { best_clk = clk; best = {features_on_lanes, bn, splits}; }
+        if (clk < best_clk) { best_clk = clk; best = {features_on_lanes, false, bn, splits}; }
     };
     if (M <= 128)
         for (int splits = 1; splits <= 8 && (splits == 1 || n_steps >= 2 * splits); splits *= 2) consider(true, M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, splits);
@@ -289,28 +271,30 @@ Tiles choose_tiles(int M, int N, int n_steps)
         consider(false, 192, 1);
         consider(false, 256, 1);
     }
+    if (M > 128) {                                          // stored beside the next tile's steps
+        const long long tiles = (long long)((M + kMx4PairRows - 1) / kMx4PairRows) * ((N + kMx4PairCols - 1) / kMx4PairCols), rounds = (tiles + sms / 2 - 1) / (sms / 2);
+        const double clk = (double)rounds * n_steps * ((128 + kMx4PairCols / 2) * 136 + 2048) / 55 + 6500;
+        if (clk < best_clk) best = {false, true, kMx4PairCols, 1};
+    }
     return best;
 }
 
-int32_t codes_map(CUtensorMap *out, const void *base, uint64_t rows, uint64_t bytes, uint64_t ld, uint32_t box_rows)
-{
-    // pairs of code bytes as 16-bit elements: 64 of them are one swizzled row
-    return make_tmap_bf16(out, base, rows, bytes / 2, ld / 2, box_rows);
-}
-
 template <int BN>
-int32_t launch(const Mx4Args &a, const void *lanes, long long ld_lanes, const void *cols, long long ld_cols, cudaStream_t stream)
+int32_t launch(const Mx4Args &a, const Mx4Operands &x, cudaStream_t stream)
 {
     using S = Shape<BN>;
     CUtensorMap tl, tcol;
     int32_t rc;
-    if ((rc = codes_map(&tl, lanes, (uint64_t)a.lanes, (uint64_t)a.blocks * 16, (uint64_t)ld_lanes, 128)) != SFS_OK) return rc;
-    if ((rc = codes_map(&tcol, cols, (uint64_t)a.cols, (uint64_t)a.blocks * 16, (uint64_t)ld_cols, BN)) != SFS_OK) return rc;
-    SFS_CUDA(allow_shared(linear_mx4_kernel<BN>, S::kShared));
+    // codes as 16-bit elements: 64 of them are one swizzled row of 128 bytes
+    if ((rc = make_tmap_bf16(&tl, x.lanes, (uint64_t)a.lanes, (uint64_t)a.blocks * 8, (uint64_t)x.ld_lanes / 2, 128)) != SFS_OK) return rc;
+    if ((rc = make_tmap_bf16(&tcol, x.cols, (uint64_t)a.cols, (uint64_t)a.blocks * 8, (uint64_t)x.ld_cols / 2, BN)) != SFS_OK) return rc;
     const long long ctas = (long long)((a.lanes + 127) / 128) * a.col_tiles * a.splits;
     SFS_REQUIRE(ctas <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "linear_mx4: too many tiles");
-    if (a.splits > 1) SFS_CUDA(launch_pdl_cluster(linear_mx4_kernel<BN>, a.splits, dim3((unsigned)ctas), dim3(kThreads), (size_t)S::kShared, stream, tl, tcol, a));
-    else SFS_CUDA(launch_pdl(linear_mx4_kernel<BN>, dim3((unsigned)ctas), dim3(kThreads), (size_t)S::kShared, stream, tl, tcol, a));
+    const int stages = S::stages(BN > 128 || ctas <= gemm_num_sms() ? 1 : 2);
+    const size_t shared = (size_t)S::shared(stages);
+    SFS_CUDA(allow_shared(linear_mx4_kernel<BN>, shared));
+    if (a.splits > 1) SFS_CUDA(launch_pdl_cluster(linear_mx4_kernel<BN>, a.splits, dim3((unsigned)ctas), dim3(kThreads), shared, stream, tl, tcol, a, stages, S::tmem_columns(stages)));
+    else SFS_CUDA(launch_pdl(linear_mx4_kernel<BN>, dim3((unsigned)ctas), dim3(kThreads), shared, stream, tl, tcol, a, stages, S::tmem_columns(stages)));
     return SFS_OK;
 }
 
@@ -346,14 +330,14 @@ extern "C" int32_t sfs_linear_mx4(const void *d_A, int64_t lda, const void *d_A_
     a.C = d_C; a.ldc = ldc; a.lanes = lanes; a.cols = cols; a.blocks = (K + 31) / 32; a.quads = (K + 127) / 128;
     a.col_tiles = col_tiles; a.splits = splits; a.out_f32 = out_dtype; a.features_on_lanes = features_on_lanes; a.scale = scale; a.err = err;
     a.wide = aligned_to(d_C, 16) && ldc * (out_dtype ? 4 : 2) % 16 == 0;
-    const void *lp = features_on_lanes ? d_B : d_A, *cp = features_on_lanes ? d_A : d_B;
-    const long long ll = features_on_lanes ? ldb : lda, lc = features_on_lanes ? lda : ldb;
+    const Mx4Operands x = features_on_lanes ? Mx4Operands{d_B, d_A, ldb, lda} : Mx4Operands{d_A, d_B, lda, ldb};
+    if (t.pairs) return linear_mx4_pairs(a, x, (cudaStream_t)stream);
     switch (bn) {
-    case 16: return launch<16>(a, lp, ll, cp, lc, (cudaStream_t)stream);
-    case 32: return launch<32>(a, lp, ll, cp, lc, (cudaStream_t)stream);
-    case 64: return launch<64>(a, lp, ll, cp, lc, (cudaStream_t)stream);
-    case 192: return launch<192>(a, lp, ll, cp, lc, (cudaStream_t)stream);
-    case 128: return launch<128>(a, lp, ll, cp, lc, (cudaStream_t)stream);
-    default: return launch<256>(a, lp, ll, cp, lc, (cudaStream_t)stream);
+    case 16: return launch<16>(a, x, (cudaStream_t)stream);
+    case 32: return launch<32>(a, x, (cudaStream_t)stream);
+    case 64: return launch<64>(a, x, (cudaStream_t)stream);
+    case 128: return launch<128>(a, x, (cudaStream_t)stream);
+    case 192: return launch<192>(a, x, (cudaStream_t)stream);
+    default: return launch<256>(a, x, (cudaStream_t)stream);
     }
 }

@@ -1,0 +1,41 @@
+// The product of two matrices of microscaled 4-bit numbers: what its kernels share.
+#pragma once
+#include "mx4.cuh"
+
+namespace sfs {
+
+namespace mx4 {
+constexpr int kDepth = 256;                                 // columns of a stage
+constexpr int kCodes = 128;                                 // bytes of a row in a stage
+constexpr int kScaleTile = 512;                             // 128 rows x 4 blocks
+
+}  // namespace mx4
+
+struct Mx4Args {
+    const uint8_t *lane_scales, *col_scales;
+    void *C; long long ldc;
+    int lanes, cols;                                        // rows of the two operands
+    int blocks, quads;                                      // blocks of 32 columns in a row, tiles of four of them
+    int col_tiles, splits;
+    int out_f32, features_on_lanes, wide;                   // wide: rows of C take 16-byte stores
+    float scale;
+    int32_t *err;
+};
+
+
+namespace mx4 {
+// kind::mxf4, both operands e2m1 and K-major, E8M0 scales of 32 columns, fp32 accumulator; `half`: which two of a column's four scale bytes
+__host__ __device__ constexpr uint32_t idesc_mxf4(int M, int N, int half) { return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 7) << 27) | ((uint32_t)(2 * half) << 29); }
+
+#ifdef __CUDACC__
+// shared-memory descriptor of 32 rows of 16 bytes, a scale tile as tcgen05.cp reads it: 8 rows are 128 consecutive bytes
+__device__ __forceinline__ uint64_t scale_desc(uint32_t smem) { return (uint64_t)((smem >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46); }
+#endif
+}  // namespace mx4
+
+// Pairs of CTAs on tiles of 256 tokens x 192 features; lanes are tokens.
+struct Mx4Operands { const void *lanes, *cols; long long ld_lanes, ld_cols; };
+int32_t linear_mx4_pairs(const Mx4Args &a, const Mx4Operands &x, cudaStream_t stream);
+constexpr int kMx4PairRows = 256, kMx4PairCols = 192;
+
+}  // namespace sfs

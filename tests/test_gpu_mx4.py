@@ -118,12 +118,12 @@ def check_linear(M, N, K, out="bf16", scale=1.0, seed=0, ld_pad=0, ldc_pad=0, of
     c = buf[offset:].view(M, N + ldc_pad)
     sfs.sfs_linear_mx4(a, a.stride(0), a_s, b, b.stride(0), b_s, c, N + ldc_pad, M, N, K, code, scale)
     sfs.sfs_check_device_status()
-    want = scale * (av @ bv.T)
+    want = scale * (torch.from_numpy(av).to(DEV) @ torch.from_numpy(bv).to(DEV).T).cpu().numpy()           # in 64 bits
     # products are exact; every addition of a 32-bit sum is off by at most 2^-23 of the terms' magnitudes, whichever way it rounds.
     # In any order no term passes through more additions than there are blocks of 64 columns, four levels inside them and the joining
     # of up to 16 parts and the scale.
     steps = (K + 63) // 64 + 4 + 16 + 1
-    bound = steps * 2.0 ** -23 * abs(scale) * (np.abs(av) @ np.abs(bv).T)
+    bound = steps * 2.0 ** -23 * abs(scale) * (torch.from_numpy(np.abs(av)).to(DEV) @ torch.from_numpy(np.abs(bv)).to(DEV).T).cpu().numpy()
     if out == "bf16":
         bound = bound * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)
     got = c.double().cpu().numpy()
@@ -152,6 +152,30 @@ def test_linear_depths(K):
 @pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (8, 4096, 12288), (128, 1024, 4096), (640, 1536, 2048), (16, 12288, 64), (1000, 1000, 1000)])
 def test_linear_larger(M, N, K):
     check_linear(M, N, K, seed=5)
+
+
+# enough tiles for pairs of CTAs: whole and ragged ones in either direction, one or several for each pair, short and long rows
+@pytest.mark.parametrize("M,N,K", [(256, 192, 4096), (512, 384, 1024), (2048, 4096, 512), (300, 20000, 96), (5000, 1000, 352), (777, 2500, 1056), (129, 24576, 64), (4100, 8200, 32), (1537, 3001, 688)])
+def test_linear_many_rows(M, N, K):
+    check_linear(M, N, K, seed=M)
+    if M * N < 4e6:
+        check_linear(M, N, K, out="f32", scale=-0.75, ldc_pad=4, seed=N)
+        check_linear(M, N, K, ld_pad=32, ldc_pad=3, offset=1, seed=K)
+
+
+def test_linear_many_rows_does_not_let_a_nan_leave_its_row_or_column():
+    M, N, K = 1030, 6000, 512
+    a, a_s, _ = operand(M, K, 1)
+    b, b_s, _ = operand(N, K, 2)
+    a_s[int(R.scale_places(M, 16)[1029, 15])] = 255
+    b_s[int(R.scale_places(N, 16)[777, 3])] = 255
+    out = torch.zeros((M, N), dtype=torch.float32, device=DEV)
+    sfs.sfs_linear_mx4(a, 256, a_s, b, 256, b_s, out, N, M, N, K, 1)
+    bad = out.isnan()
+    assert bad[1029].all() and bad[:, 777].all()
+    bad[1029], bad[:, 777] = False, False
+    assert not bad.any()
+    sfs.sfs_check_device_status()
 
 
 @pytest.mark.parametrize("M,N", [(4, 100), (150, 257), (300, 512)])
