@@ -54,22 +54,6 @@ int32_t make_tmap_bf16(CUtensorMap *out, const void *base, uint64_t rows, uint64
     return SFS_OK;
 }
 
-int32_t make_tmap_scale_tiles(CUtensorMap *out, const void *base, uint64_t tiles)
-{
-    EncodeTiledFn enc = get_encode();
-    SFS_REQUIRE(enc != nullptr, SFS_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
-    SFS_REQUIRE(aligned_to(base, 16) && tiles >= 1, SFS_ERR_INVALID_ARG, "tensor map: scales must be 16-byte aligned");
-    cuuint64_t dims[2] = {128, tiles};
-    cuuint64_t strides[1] = {512};
-    cuuint32_t box[2] = {128, 2};
-    cuuint32_t estr[2] = {1, 1};
-    CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void *>(base), dims, strides, box, estr,
-                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    SFS_REQUIRE(r == CUDA_SUCCESS, SFS_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d", (int)r);
-    return SFS_OK;
-}
-
 // A weight matrix for projections whose epilogue rotates pairs (j, j + half) of every head: the box's rows are, head by head, 16 rows of
 // the first half and the same 16 of the second, so that 32 consecutive accumulator columns hold 16 whole pairs.  Dimensions: k, row of a
 // half, half, head.  For a plain matrix half = 16.

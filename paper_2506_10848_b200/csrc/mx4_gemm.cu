@@ -34,7 +34,7 @@ template <int BN> struct Shape {
     static constexpr uint32_t tmem_columns(int stages) { const int n = BN + stages * kScaleCols; return n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
     static constexpr int shared(int stages) { return stages * kStage + 1024 /* alignment */ + (2 * stages + 1) * 8 + 16; }
     static_assert(kB % 1024 == 0 && BN + stages(1) * kScaleCols <= 512 && 2 * tmem_columns(stages(2)) <= 512 + (BN > 128 ? 512 : 0), "tile");
-    static_assert(stages(2) * kStage >= 128 * BN * 4 || BN > 128, "partial sums fit the ring");
+    static_assert(2 * kStage >= 128 * BN * 4 || BN > 128, "partial sums fit the ring");
 };
 
 __device__ __forceinline__ void mma_mxf4_elect(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, uint32_t accumulate)
@@ -245,11 +245,11 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
     if (threadIdx.x == 0 && s_abort && a.err) atomicExch(a.err, SFS_ERR_TIMEOUT);
 }
 
-// Which operand lies on the lanes, how many rows of the other a tile has, and over how many CTAs its k-steps are divided; or pairs of CTAs.
+// Which operand lies on the lanes, how many rows of the other a tile has, and over how many CTAs its k-steps are divided; or persistent CTAs.
 // A step costs what it takes to bring it to the SM, about 55 bytes a clock, shared by the CTAs of an SM, which is more than its MMAs take in
 // every shape here; a tile 6000 clocks around its steps, a join 2500 more.
-struct Tiles { bool features_on_lanes, pairs; int bn, splits; };
-Tiles choose_tiles(int M, int N, int n_steps)
+struct Tiles { bool features_on_lanes, many; int bn, splits; };
+Tiles choose_tiles(int M, int N, int n_steps, bool wide)
 {
     const long long sms = gemm_num_sms();
     Tiles best = {};
@@ -264,17 +264,19 @@ Tiles choose_tiles(int M, int N, int n_steps)
         const double clk = full * (steps * step * per_sm + 6000) + (rest == 0 ? 0 : steps * step * (rest > sms ? per_sm : 1) + 6000) + (splits > 1 ? 2500 : 0);
         if (clk < best_clk) { best_clk = clk; best = {features_on_lanes, false, bn, splits}; }
     };
-    if (M <= 128)
+    // Rows of C that take no wide stores: with features on the lanes a warp's stores are consecutive all the same (235 x 2177 x 112: 19.6 us
+    // with tokens on the lanes, XXX so).
+    if (M <= 128 || !wide)
         for (int splits = 1; splits <= 8 && (splits == 1 || n_steps >= 2 * splits); splits *= 2) consider(true, M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, splits);
-    if (M > 64) {
+    if (M > 64 && wide) {
         for (int splits = 1; splits <= 8 && (splits == 1 || n_steps >= 2 * splits); splits *= 2) consider(false, 128, splits);
         consider(false, 192, 1);
         consider(false, 256, 1);
     }
-    if (M > 128) {                                          // stored beside the next tile's steps
-        const long long tiles = (long long)((M + kMx4PairRows - 1) / kMx4PairRows) * ((N + kMx4PairCols - 1) / kMx4PairCols), rounds = (tiles + sms / 2 - 1) / (sms / 2);
-        const double clk = (double)rounds * n_steps * ((128 + kMx4PairCols / 2) * 136 + 2048) / 55 + 6500;
-        if (clk < best_clk) best = {false, true, kMx4PairCols, 1};
+    if (M > 128 && wide) {                                          // the next tile's stages are loaded while a tile is stored
+        const long long tiles = (long long)((M + 127) / 128) * ((N + kMx4ManyCols - 1) / kMx4ManyCols), rounds = (tiles + sms - 1) / sms;
+        const double clk = (double)rounds * (n_steps * 700.0 + 2500) + 5000;
+        if (clk < best_clk) best = {false, true, kMx4ManyCols, 1};
     }
     return best;
 }
@@ -290,7 +292,9 @@ int32_t launch(const Mx4Args &a, const Mx4Operands &x, cudaStream_t stream)
     if ((rc = make_tmap_bf16(&tcol, x.cols, (uint64_t)a.cols, (uint64_t)a.blocks * 8, (uint64_t)x.ld_cols / 2, BN)) != SFS_OK) return rc;
     const long long ctas = (long long)((a.lanes + 127) / 128) * a.col_tiles * a.splits;
     SFS_REQUIRE(ctas <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "linear_mx4: too many tiles");
-    const int stages = S::stages(BN > 128 || ctas <= gemm_num_sms() ? 1 : 2);
+    // no more than there are steps (but room for the partial sums): what a short call leaves free lets the next launch's CTAs start beside it
+    const int n_steps = (a.blocks + kDepth / 32 - 1) / (kDepth / 32);
+    const int stages = std::min(S::stages(BN > 128 || ctas <= gemm_num_sms() ? 1 : 2), std::max(2, (n_steps + a.splits - 1) / a.splits));
     const size_t shared = (size_t)S::shared(stages);
     SFS_CUDA(allow_shared(linear_mx4_kernel<BN>, shared));
     if (a.splits > 1) SFS_CUDA(launch_pdl_cluster(linear_mx4_kernel<BN>, a.splits, dim3((unsigned)ctas), dim3(kThreads), shared, stream, tl, tcol, a, stages, S::tmem_columns(stages)));
@@ -320,7 +324,8 @@ extern "C" int32_t sfs_linear_mx4(const void *d_A, int64_t lda, const void *d_A_
     SFS_REQUIRE(err != nullptr, SFS_ERR_OOM, "cannot allocate the device status word");
 
     const int n_steps = (K + kDepth - 1) / kDepth;
-    const Tiles t = choose_tiles(M, N, n_steps);
+    const bool wide = aligned_to(d_C, 16) && ldc * (out_dtype ? 4 : 2) % 16 == 0;
+    const Tiles t = choose_tiles(M, N, n_steps, wide);
     const bool features_on_lanes = t.features_on_lanes;
     const int lanes = features_on_lanes ? N : M, cols = features_on_lanes ? M : N, bn = t.bn, splits = t.splits;
     const int col_tiles = (cols + bn - 1) / bn;
@@ -329,9 +334,9 @@ extern "C" int32_t sfs_linear_mx4(const void *d_A, int64_t lda, const void *d_A_
     a.col_scales = (const uint8_t *)(features_on_lanes ? d_A_scales : d_B_scales);
     a.C = d_C; a.ldc = ldc; a.lanes = lanes; a.cols = cols; a.blocks = (K + 31) / 32; a.quads = (K + 127) / 128;
     a.col_tiles = col_tiles; a.splits = splits; a.out_f32 = out_dtype; a.features_on_lanes = features_on_lanes; a.scale = scale; a.err = err;
-    a.wide = aligned_to(d_C, 16) && ldc * (out_dtype ? 4 : 2) % 16 == 0;
+    a.wide = wide;
     const Mx4Operands x = features_on_lanes ? Mx4Operands{d_B, d_A, ldb, lda} : Mx4Operands{d_A, d_B, lda, ldb};
-    if (t.pairs) return linear_mx4_pairs(a, x, (cudaStream_t)stream);
+    if (t.many) return linear_mx4_many(a, x, (cudaStream_t)stream);
     switch (bn) {
     case 16: return launch<16>(a, x, (cudaStream_t)stream);
     case 32: return launch<32>(a, x, (cudaStream_t)stream);

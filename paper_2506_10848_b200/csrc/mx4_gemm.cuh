@@ -33,9 +33,9 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t smem) { return (uint64_t
 #endif
 }  // namespace mx4
 
-// Pairs of CTAs on tiles of 256 tokens x 192 features; lanes are tokens.
 struct Mx4Operands { const void *lanes, *cols; long long ld_lanes, ld_cols; };
-int32_t linear_mx4_pairs(const Mx4Args &a, const Mx4Operands &x, cudaStream_t stream);
-constexpr int kMx4PairRows = 256, kMx4PairCols = 192;
+// Many tiles, of 128 tokens (lanes) x 256 features: persistent CTAs.
+int32_t linear_mx4_many(const Mx4Args &a, const Mx4Operands &x, cudaStream_t stream);
+constexpr int kMx4ManyCols = 256;
 
 }  // namespace sfs

@@ -226,7 +226,5 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {
 // 2-D bf16 row-major tensor [rows, cols] with `ld` elements between rows; box = box_rows x 64 columns,
 // 128-byte swizzle.  Out-of-range parts of a box are zero-filled.
 int32_t make_tmap_bf16(CUtensorMap *out, const void *base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows);
-// `tiles` consecutive pieces of 512 bytes, the tiles of a 4-bit matrix's scales; box = two of them.
-int32_t make_tmap_scale_tiles(CUtensorMap *out, const void *base, uint64_t tiles);
 
 }  // namespace sfs
