@@ -233,13 +233,14 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
             tc::mbar_arrive(bar_vfull + 8 * s);
             return true;
         };
-        if (n_tiles > 0) { fetch_k(0); if (has_values) fetch_v(0); }
+        if (n_tiles > 0) fetch_k(0);
         // Streams over odd and even tiles: keys one tile ahead of values, for the other stream's first scores (128 rows over 1536 tokens, 32
         // heads: 17.3 us without, 16.7 with; row tiles that share a tile want its values sooner, 105 us instead of 102 for 2048 x 2048).
         bool ok = true;
         for (int j = PAIR ? 0 : -1; j < n_tiles && ok; ++j) {
             const int jk = PAIR ? j : j + 1;
             if (jk < n_tiles) ok = decode_k(jk);
+            if (jk == 0 && has_values) fetch_v(0);          // (not sooner: the first keys and the queries come first)
             if (ok && j >= 0 && has_values) ok = decode_v(j);
         }
         __syncwarp();
@@ -295,23 +296,19 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
         const int w = (warp - 8) >> 2, row = (warp & 3) * 32 + lane;
         {
             // queries, in the features' order of a decoded word: (0, 4), (1, 5), (2, 6), (3, 7); neighbouring lanes have a row's words
-            constexpr int ROWS_AT_ONCE = 2 * QT / WORDS, BATCH = 8;
+            constexpr int ROWS_AT_ONCE = 2 * QT / WORDS, BATCH = ROWS / ROWS_AT_ONCE;      // all of a thread's loads in flight
             const int wd = (threadIdx.x - kDecoders) % WORDS, first_row = (threadIdx.x - kDecoders) / WORDS;
+            uint4 v[BATCH];
 #pragma unroll
-            for (int c = 0; c < ROWS; c += BATCH * ROWS_AT_ONCE) {
-                uint4 v[BATCH];
+            for (int k = 0; k < BATCH; ++k) {
+                const int rq = first_row + k * ROWS_AT_ONCE;
+                v[k] = rq < n_rows ? *reinterpret_cast<const uint4 *>(a.q + row_of(rq, a.ld_q) + wd * 8) : make_uint4(0, 0, 0, 0);
+            }
 #pragma unroll
-                for (int k = 0; k < BATCH; ++k) {
-                    const int rq = first_row + c + k * ROWS_AT_ONCE;
-                    v[k] = rq < min(n_rows, ROWS) ? *reinterpret_cast<const uint4 *>(a.q + row_of(rq, a.ld_q) + wd * 8) : make_uint4(0, 0, 0, 0);
-                }
-#pragma unroll
-                for (int k = 0; k < BATCH; ++k) {
-                    const int rq = first_row + c + k * ROWS_AT_ONCE, tile = rq / QT, rr = rq % QT;
-                    if (rq < ROWS)
-                        store_chunk(tc::smem_u32(sQ) + tile * Q_BYTES + (wd / 8) * (QT * 128) + rr * 128 + (((wd % 8) ^ (rr & 7)) * 16),
-                                    __byte_perm(v[k].x, v[k].z, 0x5410), __byte_perm(v[k].x, v[k].z, 0x7632), __byte_perm(v[k].y, v[k].w, 0x5410), __byte_perm(v[k].y, v[k].w, 0x7632));
-                }
+            for (int k = 0; k < BATCH; ++k) {
+                const int rq = first_row + k * ROWS_AT_ONCE, tile = rq / QT, rr = rq % QT;
+                store_chunk(tc::smem_u32(sQ) + tile * Q_BYTES + (wd / 8) * (QT * 128) + rr * 128 + (((wd % 8) ^ (rr & 7)) * 16),
+                            __byte_perm(v[k].x, v[k].z, 0x5410), __byte_perm(v[k].x, v[k].z, 0x7632), __byte_perm(v[k].y, v[k].w, 0x5410), __byte_perm(v[k].y, v[k].w, 0x7632));
             }
             fence_async_shared();
             tc::mbar_arrive(bar_q);
