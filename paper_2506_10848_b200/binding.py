@@ -193,40 +193,65 @@ def mx4_scale_bytes(rows, cols):
     return (rows + 127) // 128 * ((cols + 127) // 128) * 512
 
 
+def _here(*tensors):
+    """Addresses of tensors on the current device (None and ints pass): a kernel that follows another's address faults the GPU."""
+    out, device = [], None
+    for t in tensors:
+        if t is None or isinstance(t, int):
+            out.append(t)
+            continue
+        if device is None:
+            import torch
+            device = torch.cuda.current_device() if t.is_cuda else None
+        if not t.is_cuda or t.get_device() != device:
+            raise SfsError(ERR_INVALID_ARG, f"tensor on {t.device}: this call takes tensors of the current CUDA device")
+        out.append(t.data_ptr())
+    return out
+
+
 def sfs_mx4_quantize(x, ldx, in_dtype, rows, cols, codes, ld_codes, scales, stream=None):
-    _check(lib().sfs_mx4_quantize(_ptr(x), ldx, in_dtype, rows, cols, _ptr(codes), ld_codes, _ptr(scales), _stream(stream)))
+    x, codes, scales = _here(x, codes, scales)
+    _check(lib().sfs_mx4_quantize(x, ldx, in_dtype, rows, cols, codes, ld_codes, scales, _stream(stream)))
 
 
 def sfs_mx4_dequantize(codes, ld_codes, scales, rows, cols, x, ldx, out_dtype, stream=None):
-    _check(lib().sfs_mx4_dequantize(_ptr(codes), ld_codes, _ptr(scales), rows, cols, _ptr(x), ldx, out_dtype, _stream(stream)))
+    codes, scales, x = _here(codes, scales, x)
+    _check(lib().sfs_mx4_dequantize(codes, ld_codes, scales, rows, cols, x, ldx, out_dtype, _stream(stream)))
 
 
 def sfs_linear_mx4(A, lda, A_scales, Bm, ldb, B_scales, C, ldc, M, N, K, out_dtype=0, scale=1.0, stream=None):
-    _check(lib().sfs_linear_mx4(_ptr(A), lda, _ptr(A_scales), _ptr(Bm), ldb, _ptr(B_scales), _ptr(C), ldc, M, N, K,
-                                out_dtype, scale, _stream(stream)))
+    A, A_scales, Bm, B_scales, C = _here(A, A_scales, Bm, B_scales, C)
+    _check(lib().sfs_linear_mx4(A, lda, A_scales, Bm, ldb, B_scales, C, ldc, M, N, K, out_dtype, scale, _stream(stream)))
 
 
 class Cache4(Structure):
-    """A 4-bit key / value cache in the caller's tensors, which the handle keeps alive."""
+    """A 4-bit key / value cache in the caller's uint8 tensors (or at given addresses), which the handle keeps alive."""
     _fields_ = [(n, c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")] + \
                [(n, c_int32) for n in ("batch", "capacity", "n_kv_heads", "head_dim")]
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales, batch, capacity, n_kv_heads, head_dim):
-        super().__init__(*(_ptr(t) for t in (k_codes, k_scales, v_codes, v_scales)), batch, capacity, n_kv_heads, head_dim)
-        self._tensors = (k_codes, k_scales, v_codes, v_scales)
+        parts = (k_codes, k_scales, v_codes, v_scales)
+        for name, t, per in zip(("k_codes", "k_scales", "v_codes", "v_scales"), parts, (2, 32, 2, 32)):
+            if t is not None and not isinstance(t, int):
+                if t.element_size() != 1 or not t.is_contiguous() or t.numel() < batch * capacity * n_kv_heads * (head_dim // per):
+                    raise SfsError(ERR_INVALID_ARG, f"{name}: contiguous bytes for {batch} x {capacity} tokens of {n_kv_heads} heads needed")
+        super().__init__(*_here(*parts), batch, capacity, n_kv_heads, head_dim)
+        self._tensors = parts
 
 
 def sfs_cache4_store(cache, k, ld_k, v, ld_v, in_dtype, slots, n_rows, stream=None):
-    _check(lib().sfs_cache4_store(byref(cache), _ptr(k), ld_k, _ptr(v), ld_v, in_dtype, _ptr(slots), n_rows, _stream(stream)))
+    k, v, slots = _here(k, v, slots)
+    _check(lib().sfs_cache4_store(byref(cache), k, ld_k, v, ld_v, in_dtype, slots, n_rows, _stream(stream)))
 
 
 def sfs_cache4_load(cache, slots, n_rows, k, ld_k, v, ld_v, out_dtype, stream=None):
-    _check(lib().sfs_cache4_load(byref(cache), _ptr(slots), n_rows, _ptr(k), ld_k, _ptr(v), ld_v, out_dtype, _stream(stream)))
+    k, v, slots = _here(k, v, slots)
+    _check(lib().sfs_cache4_load(byref(cache), slots, n_rows, k, ld_k, v, ld_v, out_dtype, _stream(stream)))
 
 
 def sfs_attention_cache4(cache, q, ld_q, out, ld_out, n_heads, n_q, lengths=None, positions=None, left=-1, right=-1, sinks=0, stream=None):
-    _check(lib().sfs_attention_cache4(byref(cache), _ptr(q), ld_q, _ptr(out), ld_out, n_heads, n_q, _ptr(lengths), _ptr(positions),
-                                      left, right, sinks, _stream(stream)))
+    q, out, lengths, positions = _here(q, out, lengths, positions)
+    _check(lib().sfs_attention_cache4(byref(cache), q, ld_q, out, ld_out, n_heads, n_q, lengths, positions, left, right, sinks, _stream(stream)))
 
 
 class Model:

@@ -11,6 +11,10 @@
 // Decoded values are exact: bits moved into bf16 (times 2^-126), one product with 2^(c - 65), so a common factor of 2^-64 remains, which
 // scores get back in 32 bits and values from the probabilities, taken 2^64 times as large.
 //
+// Bound: the softmax warps' chain (scores, maximum, exponentials, hand-over: 3300 clocks of a tile, which the decoding warps stretch by
+// sharing the pipes) with the MMAs behind it (1300), about 5300 clocks for a tile of both streams; the tensor pipe is 29 % busy, issue 49 %.
+// Measured, 32 heads of 128, us: 2048 rows over 2048 tokens 101 (attention_kernel on bf16 values 73), 128 rows over 1536 16.5.
+//
 // Only key tiles that some row sees are visited.  With few CTAs the tiles are divided over a cluster of up to 8, whose partial outputs
 // meet in shared memory, in rank order.
 #include "attention_cache4.cuh"
@@ -551,14 +555,16 @@ int32_t launch(const Cache4Args &a, int log_splits, cudaStream_t stream)
     return SFS_OK;
 }
 
-// pairs of row tiles where they fill the machine; else up to one wave of CTAs, two key tiles for each
+// Pairs of row tiles where they fill the machine; else up to one wave of CTAs, two key tiles for each.  Clusters do not cover every SM, since
+// they do not cross the GPU's partitions: 128 CTAs in clusters of four run at once, in clusters of eight they do not (128 rows over 1536
+// tokens, 16 heads: 14.6 us with four, 25.4 with eight).
 struct Many { bool pair; int log_splits; long long ctas, key_tiles; };
 Many plan(const Cache4Args &a, int64_t tokens)
 {
     const long long row_tiles = ((long long)a.n_q * a.group + QT - 1) / QT, heads = (long long)a.batch * a.n_kv, sms = gemm_num_sms();
     Many p = {row_tiles > 1 && heads * ((row_tiles + 1) / 2) >= sms, 0, 0, 0};
     if (!p.pair)
-        while (p.log_splits < 3 && (heads * row_tiles << (p.log_splits + 1)) <= sms && tokens > (2 * KT) << p.log_splits) ++p.log_splits;
+        while (p.log_splits < 3 && (heads * row_tiles << (p.log_splits + 1)) <= (p.log_splits == 2 ? sms / 2 : sms * 7 / 8) && tokens > (2 * KT) << p.log_splits) ++p.log_splits;
     p.ctas = heads * (p.pair ? (row_tiles + 1) / 2 : row_tiles) << p.log_splits;
     const long long tiles = (tokens + KT - 1) / KT;
     p.key_tiles = (tiles + (1 << p.log_splits) - 1) >> p.log_splits;

@@ -62,4 +62,7 @@ __device__ __forceinline__ uint4 decode8(uint32_t w, uint32_t c)
 #endif
 
 }  // namespace mx4
+
+// The current device's status word, allocated on first use, which a capture of `stream` does not allow (and would not survive).
+int32_t status_word_outside_captures(cudaStream_t stream, int32_t **word);
 }  // namespace sfs

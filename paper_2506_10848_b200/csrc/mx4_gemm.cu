@@ -220,6 +220,11 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
                 for (int i = 0; i < CH; ++i) mine[(c + i) * 128 + row] = __uint_as_float(u[i]);
             }
         }
+        // Tensor memory is given back before the ranks wait for one another: a CTA that kept it could hold up another launch's CTA on this SM
+        // whose own rank a third SM's CTA waits for.
+        tc::tc_fence_before();
+        __syncthreads();
+        if (warp == 1) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, tmem_columns); }
         tc::cluster_sync();
         if (storing) {
             constexpr int W = BN / 8;                       // columns of a slice
@@ -239,9 +244,11 @@ linear_mx4_kernel(const __grid_constant__ CUtensorMap tm_lanes, const __grid_con
         }
         tc::cluster_sync();                                 // the ring stays until every rank has read it
     }
-    tc::tc_fence_before();
-    __syncthreads();
-    if (warp == 1) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, tmem_columns); }
+    if (a.splits == 1) {
+        tc::tc_fence_before();
+        __syncthreads();
+        if (warp == 1) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, tmem_columns); }
+    }
     if (threadIdx.x == 0 && s_abort && a.err) atomicExch(a.err, SFS_ERR_TIMEOUT);
 }
 
@@ -265,7 +272,7 @@ Tiles choose_tiles(int M, int N, int n_steps, bool wide)
         if (clk < best_clk) { best_clk = clk; best = {features_on_lanes, false, bn, splits}; }
     };
     // Rows of C that take no wide stores: with features on the lanes a warp's stores are consecutive all the same (235 x 2177 x 112: 19.6 us
-    // with tokens on the lanes, XXX so).
+    // with tokens on the lanes, 5.7 so).
     if (M <= 128 || !wide)
         for (int splits = 1; splits <= 8 && (splits == 1 || n_steps >= 2 * splits); splits *= 2) consider(true, M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, splits);
     if (M > 64 && wide) {
@@ -320,8 +327,9 @@ extern "C" int32_t sfs_linear_mx4(const void *d_A, int64_t lda, const void *d_A_
     SFS_REQUIRE(lda % 16 == 0 && ldb % 16 == 0 && lda >= bytes && ldb >= bytes, SFS_ERR_INVALID_ARG,
                 "linear_mx4: lda and ldb must be multiples of 16 and hold a row");
     SFS_REQUIRE(ldc >= N && aligned_to(d_C, out_dtype ? 4 : 2), SFS_ERR_INVALID_ARG, "linear_mx4: misaligned C, or ldc below N");
-    int32_t *err = device_status_word();
-    SFS_REQUIRE(err != nullptr, SFS_ERR_OOM, "cannot allocate the device status word");
+    int32_t *err = nullptr;
+    const int32_t rc = status_word_outside_captures((cudaStream_t)stream, &err);
+    if (rc != SFS_OK) return rc;
 
     const int n_steps = (K + kDepth - 1) / kDepth;
     const bool wide = aligned_to(d_C, 16) && ldc * (out_dtype ? 4 : 2) % 16 == 0;

@@ -1,11 +1,13 @@
 // C = scale * A * B^T of two matrices of microscaled 4-bit numbers, many tiles: one persistent CTA per SM on tiles of 128 tokens x 256
 // features (tcgen05.mma kind::mxf4).
 //
-// A step of 256 columns of depth brings 51 KB to the SM, in about 700 clocks; its four MMAs take as long.  What a CTA for each tile spends
-// around its steps, 15000 clocks for its start, the filling of the ring and the storing of its tile, is what persistence saves: the next
-// tile's stages are loaded while a tile is stored, its MMAs begin once the accumulator has been read.  XXX
-// The accumulator takes half of tensor memory and the stages' scales 96 columns of the rest, so there is one.  Pairs of CTAs on 256 x 256
-// tiles (cta_group::2) pull 35 KB a step instead, but copying scales for a pair kept its MMAs waiting: 171 us where single CTAs took 147.
+// Bound: a step of 256 columns of depth writes 51 KB to the SM's shared memory and its four MMAs read 48 KB of it, about 800 of a step's
+// 1000 clocks at 128 bytes a clock; loads alone take 120 us of 6144 x 4096 x 12288's 142 - 155, MMAs alone 119, copying the scales 4.  What a
+// CTA for every tile spends around its steps, 15000 clocks for its start, the filling of the ring and the storing of its tile, is what
+// persistence saves: the next tile's stages are loaded while a tile is stored, and its MMAs begin once the accumulator has been read (us,
+// 6144 x 12288 x 4096: 211 -> 164, 1536 x 12288 x 4096: 55 -> 40, 512 x 24576 x 4096: 43 -> 32).  The accumulator takes half of tensor memory and the
+// stages' scales 96 columns of the rest, so there is one.  Pairs of CTAs on 256 x 256 tiles (cta_group::2) bring 35 KB a step instead, but
+// copying scales for a pair kept its MMAs waiting: 171 us.
 //
 // Warp 0 loads, warp 1 issues, warps 2-9 store: bf16 rows pass through shared memory and leave in whole sectors.
 #include "mx4_gemm.cuh"

@@ -225,6 +225,63 @@ def test_quantise_and_multiply_in_a_graph_on_another_stream():
         assert (np.abs(out.double().cpu().numpy() - av @ bv.T) <= bound).all()
 
 
+FIRST_CALL = """
+import torch
+from paper_2506_10848_b200 import binding as sfs
+z = lambda *s: torch.zeros(s, dtype=torch.uint8, device="cuda:0")
+a, b, sa, sb = z(40, 64), z(96, 64), z(sfs.mx4_scale_bytes(40, 128)), z(sfs.mx4_scale_bytes(96, 128))
+out = torch.full((40, 96), 7.0, device="cuda:0")
+call = lambda: sfs.sfs_linear_mx4(a, 64, sa, b, 64, sb, out, 96, 40, 96, 128, 1)
+graph, status = torch.cuda.CUDAGraph(), None
+with torch.cuda.graph(graph):
+    try:
+        call()
+    except sfs.SfsError as e:
+        status = e.status
+    out.add_(1.0)                                           # the capture goes on
+assert status == sfs.ERR_INVALID_ARG, status
+call()
+torch.cuda.synchronize()
+assert not out.any()
+graph.replay()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    call()
+out.fill_(3.0)
+graph.replay()
+torch.cuda.synchronize()
+assert not out.any()
+"""
+
+
+def test_the_first_call_of_a_process_is_not_captured():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
+def test_two_products_at_once():
+    """Divided over clusters and not, on two streams that overlap."""
+    cases = [(9, 512, 8192), (16, 256, 12288), (128, 640, 8192), (300, 4096, 512)]
+    ops = [(operand(m, k, m), operand(n, k, n)) for m, n, k in cases]
+    outs = [[torch.zeros((m, n), dtype=torch.float32, device=DEV) for m, n, k in cases] for _ in range(2)]
+    torch.cuda.synchronize()
+    for out in outs:
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                for (m, n, k), ((a, a_s, _), (b, b_s, _)), o in zip(cases, ops, out):
+                    sfs.sfs_linear_mx4(a, k // 2, a_s, b, k // 2, b_s, o, n, m, n, k, 1)
+    torch.cuda.synchronize()
+    sfs.sfs_check_device_status()
+    for (m, n, k), ((_, _, av), (_, _, bv)), x, y in zip(cases, ops, *outs):
+        assert torch.equal(x, y)
+        bound = ((k + 63) // 64 + 21) * 2.0 ** -23 * (np.abs(av) @ np.abs(bv).T)
+        assert (np.abs(x.double().cpu().numpy() - av @ bv.T) <= bound).all()
+
+
 # ---- the cache ------------------------------------------------------------------------------------------------------------------------
 
 def new_cache(batch, capacity, heads, dim):

@@ -74,6 +74,25 @@ def test_attention(change):
     refused(sfs.ERR_INVALID_ARG, sfs.sfs_attention_cache4, **kw)
 
 
+def test_sizes_that_would_pass_an_index():
+    refused(sfs.ERR_UNSUPPORTED, sfs.sfs_attention_cache4, cache(batch=1, capacity=(1 << 30) + 1), A, 128, A, 128, 2, 1)
+    refused(sfs.ERR_UNSUPPORTED, sfs.sfs_attention_cache4, cache(batch=1, n_kv_heads=1), A, 1 << 22, A, 1 << 22, 65535, 1 << 16)
+
+
+def test_tensors_of_the_host_are_refused():
+    torch = pytest.importorskip("torch")
+    t, b = torch.zeros(1 << 12, dtype=torch.bfloat16), torch.zeros(1 << 12, dtype=torch.uint8)
+    refused(sfs.ERR_INVALID_ARG, sfs.sfs_mx4_quantize, t, 64, 0, 4, 64, A, 32, A)
+    refused(sfs.ERR_INVALID_ARG, sfs.sfs_mx4_dequantize, b, 32, A, 4, 64, A, 64, 0)
+    refused(sfs.ERR_INVALID_ARG, sfs.sfs_linear_mx4, A, 32, A, A, 32, b, A, 64, 4, 64, 64)
+    refused(sfs.ERR_INVALID_ARG, sfs.sfs_cache4_store, cache(), A, 128, t, 128, 0, None, 1)
+    refused(sfs.ERR_INVALID_ARG, sfs.sfs_cache4_load, cache(), None, 1, t, 128, A, 128, 0)
+    refused(sfs.ERR_INVALID_ARG, sfs.sfs_attention_cache4, cache(), A, 128, A, 128, 2, 1, lengths=b)
+    for bad in (b, torch.zeros(8, dtype=torch.uint8), torch.zeros(1 << 12, dtype=torch.int32)):
+        with pytest.raises(sfs.SfsError):
+            cache(k_codes=bad)
+
+
 def test_nothing_to_do_is_no_error():
     sfs.sfs_cache4_store(cache(), A, 128, A, 128, 0, None, 0, stream=0)
     sfs.sfs_cache4_load(cache(), None, 0, A, 128, A, 128, 0, stream=0)
