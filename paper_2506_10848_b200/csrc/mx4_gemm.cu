@@ -75,18 +75,23 @@ __device__ __forceinline__ void store_columns(const Mx4Args &a, int lane, int co
             }
     } else {
         const long long at = (long long)lane * a.ldc + col;
-        if (a.wide && col + N <= a.cols && N % 8 == 0) {
-            if (a.out_f32) {
+        if (a.wide && N % 8 == 0 && !a.out_f32) {
 #pragma unroll
-                for (int i = 0; i < N / 4; ++i) reinterpret_cast<float4 *>(static_cast<float *>(a.C) + at)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-            } else {
+            for (int i = 0; i < N / 8; ++i) {
+                uint32_t w[4];
 #pragma unroll
-                for (int i = 0; i < N / 8; ++i) {
-                    uint32_t w[4];
+                for (int t = 0; t < 4; ++t) { const __nv_bfloat162 h = __floats2bfloat162_rn(v[8 * i + 2 * t], v[8 * i + 2 * t + 1]); w[t] = *reinterpret_cast<const uint32_t *>(&h); }
+                put_bf16(static_cast<__nv_bfloat16 *>(a.C) + at + 8 * i, make_uint4(w[0], w[1], w[2], w[3]), a.cols - col - 8 * i);
+            }
+        } else if (a.wide && N % 8 == 0) {
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) { const __nv_bfloat162 h = __floats2bfloat162_rn(v[8 * i + 2 * t], v[8 * i + 2 * t + 1]); w[t] = *reinterpret_cast<const uint32_t *>(&h); }
-                    reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.C) + at)[i] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
+            for (int i = 0; i < N / 4; ++i) {
+                float *to = static_cast<float *>(a.C) + at + 4 * i;
+                if (col + 4 * i + 4 <= a.cols) *reinterpret_cast<float4 *>(to) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                else
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if (col + 4 * i + t < a.cols) to[t] = v[4 * i + t];
             }
         } else {
 #pragma unroll
@@ -280,9 +285,9 @@ Tiles choose_tiles(int M, int N, int n_steps, bool wide)
         consider(false, 192, 1);
         consider(false, 256, 1);
     }
-    if (M > 128 && wide) {                                          // the next tile's stages are loaded while a tile is stored
+    if (M > 128) {                                                  // the next tile's stages are loaded while a tile is stored
         const long long tiles = (long long)((M + 127) / 128) * ((N + kMx4ManyCols - 1) / kMx4ManyCols), rounds = (tiles + sms - 1) / sms;
-        const double clk = (double)rounds * (n_steps * 700.0 + 2500) + 5000;
+        const double clk = (double)rounds * (n_steps * 700.0 + (wide ? 2500 : 5500)) + 5000;
         if (clk < best_clk) best = {false, true, kMx4ManyCols, 1};
     }
     return best;
@@ -342,7 +347,7 @@ extern "C" int32_t sfs_linear_mx4(const void *d_A, int64_t lda, const void *d_A_
     a.col_scales = (const uint8_t *)(features_on_lanes ? d_A_scales : d_B_scales);
     a.C = d_C; a.ldc = ldc; a.lanes = lanes; a.cols = cols; a.blocks = (K + 31) / 32; a.quads = (K + 127) / 128;
     a.col_tiles = col_tiles; a.splits = splits; a.out_f32 = out_dtype; a.features_on_lanes = features_on_lanes; a.scale = scale; a.err = err;
-    a.wide = wide;
+    a.wide = wide; a.unit = wide ? 16 : out_dtype || (aligned_to(d_C, 4) && ldc % 2 == 0) ? 4 : 2;
     const Mx4Operands x = features_on_lanes ? Mx4Operands{d_B, d_A, ldb, lda} : Mx4Operands{d_A, d_B, lda, ldb};
     if (t.many) return linear_mx4_many(a, x, (cudaStream_t)stream);
     switch (bn) {

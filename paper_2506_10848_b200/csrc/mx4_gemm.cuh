@@ -17,7 +17,7 @@ struct Mx4Args {
     int lanes, cols;                                        // rows of the two operands
     int blocks, quads;                                      // blocks of 32 columns in a row, tiles of four of them
     int col_tiles, splits;
-    int out_f32, features_on_lanes, wide;                   // wide: rows of C take 16-byte stores
+    int out_f32, features_on_lanes, wide, unit;             // wide: rows of C take 16-byte stores; unit: the widest that they all take
     float scale;
     int32_t *err;
 };
@@ -30,6 +30,15 @@ __host__ __device__ constexpr uint32_t idesc_mxf4(int M, int N, int half) { retu
 #ifdef __CUDACC__
 // shared-memory descriptor of 32 rows of 16 bytes, a scale tile as tcgen05.cp reads it: 8 rows are 128 consecutive bytes
 __device__ __forceinline__ uint64_t scale_desc(uint32_t smem) { return (uint64_t)((smem >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46); }
+// eight bf16 values to an aligned place of which `n` belong to the row
+__device__ __forceinline__ void put_bf16(__nv_bfloat16 *at, const uint4 &v, int n)
+{
+    if (n >= 8) { *reinterpret_cast<uint4 *>(at) = v; return; }
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) at[i] = __ushort_as_bfloat16((unsigned short)((i & 1) ? w[i / 2] >> 16 : w[i / 2]));
+}
 #endif
 }  // namespace mx4
 

@@ -9,7 +9,8 @@
 // stages' scales 96 columns of the rest, so there is one.  Pairs of CTAs on 256 x 256 tiles (cta_group::2) bring 35 KB a step instead, but
 // copying scales for a pair kept its MMAs waiting: 171 us.
 //
-// Warp 0 loads, warp 1 issues, warps 2-9 store: bf16 rows pass through shared memory and leave in whole sectors.
+// Warp 0 loads, warp 1 issues, warps 2-9 store: rows pass through shared memory and leave in whole sectors, or, where they do not take
+// 16-byte stores, 4 or 2 bytes of neighbouring lanes together.
 #include "mx4_gemm.cuh"
 #include "tc05.cuh"
 #include "gemm.cuh"
@@ -155,7 +156,6 @@ linear_mx4_many_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_co
             tc::tc_fence_after();
             const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16);
             const int row0 = tile % row_tiles * 128 + q * 32, col0 = tile / row_tiles * BN;
-            const bool whole = !a.out_f32 && a.wide && col0 + BN <= a.cols;
 #pragma unroll 1
             for (int g = half * (BN / 64); g < (half + 1) * (BN / 64); ++g) {          // 32 columns: 64 bytes of bf16
                 uint32_t u[32];
@@ -166,42 +166,58 @@ linear_mx4_many_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_co
                     __syncwarp();
                     if (lane == 0) tc::mbar_arrive(acc_empty);
                 }
-                if (whole) {
+                // 64 bytes of a row at a time (32 columns of bf16, half of them of fp32), parked so that neighbouring lanes store neighbouring bytes
+                const int passes = a.out_f32 ? 2 : 1;
+#pragma unroll 1
+                for (int pass = 0; pass < passes; ++pass) {
+                    if (a.out_f32) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t w[4];
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t w[4];
 #pragma unroll
-                        for (int t = 0; t < 4; ++t) {
-                            const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(u[8 * c + 2 * t]) * a.scale, __uint_as_float(u[8 * c + 2 * t + 1]) * a.scale);
-                            w[t] = *reinterpret_cast<const uint32_t *>(&h);
+                            for (int t = 0; t < 4; ++t) w[t] = __float_as_uint(__uint_as_float(pass == 0 ? u[4 * c + t] : u[16 + 4 * c + t]) * a.scale);
+                            *reinterpret_cast<uint4 *>(mine + lane * 64 + ((c ^ ((lane >> 1) & 3)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
-                        *reinterpret_cast<uint4 *>(mine + lane * 64 + ((c ^ ((lane >> 1) & 3)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {           // eight rows at a time
-                        const int r = 8 * i + (lane >> 2), c = lane & 3;
-                        const uint4 v = *reinterpret_cast<const uint4 *>(mine + r * 64 + ((c ^ ((r >> 1) & 3)) * 16));
-                        if (row0 + r < a.lanes) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.C) + (long long)(row0 + r) * a.ldc + col0 + g * 32 + c * 8) = v;
-                    }
-                } else if (row0 + lane < a.lanes) {
-                    const long long at = (long long)(row0 + lane) * a.ldc + col0 + g * 32;
-                    const int n = a.cols - col0 - g * 32;
-                    if (a.out_f32 && a.wide && n >= 32) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            reinterpret_cast<float4 *>(static_cast<float *>(a.C) + at)[i] = make_float4(__uint_as_float(u[4 * i]) * a.scale, __uint_as_float(u[4 * i + 1]) * a.scale,
-                                                                                                        __uint_as_float(u[4 * i + 2]) * a.scale, __uint_as_float(u[4 * i + 3]) * a.scale);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i < n) {
-                                const float v = __uint_as_float(u[i]) * a.scale;
-                                if (a.out_f32) static_cast<float *>(a.C)[at + i] = v; else static_cast<__nv_bfloat16 *>(a.C)[at + i] = __float2bfloat16_rn(v);
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int t = 0; t < 4; ++t) {
+                                const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(u[8 * c + 2 * t]) * a.scale, __uint_as_float(u[8 * c + 2 * t + 1]) * a.scale);
+                                w[t] = *reinterpret_cast<const uint32_t *>(&h);
                             }
+                            *reinterpret_cast<uint4 *>(mine + lane * 64 + ((c ^ ((lane >> 1) & 3)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
                     }
+                    __syncwarp();
+                    const int left = (a.cols - col0 - g * 32 - pass * 16) * (a.out_f32 ? 4 : 2);               // bytes of a row from here on
+                    uint8_t *to = static_cast<uint8_t *>(a.C) + ((long long)row0 * a.ldc + col0 + g * 32 + pass * 16) * (a.out_f32 ? 4 : 2);
+                    const long long pitch = a.ldc * (a.out_f32 ? 4 : 2);
+                    auto parked = [&](int r, int byte) { return mine + r * 64 + (((byte >> 4) ^ ((r >> 1) & 3)) * 16) + (byte & 15); };
+                    const int rows = a.lanes - row0;
+                    if (a.unit == 16) {                     // eight rows at a time
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int r = 8 * i + (lane >> 2), byte = (lane & 3) * 16;
+                            if (r < rows && byte + 16 <= left) *reinterpret_cast<uint4 *>(to + r * pitch + byte) = *reinterpret_cast<const uint4 *>(parked(r, byte));
+                            else if (r < rows)
+                                for (int e = byte; e < min(byte + 16, left); e += 2) *reinterpret_cast<uint16_t *>(to + r * pitch + e) = *reinterpret_cast<const uint16_t *>(parked(r, e));
+                        }
+                    } else if (a.unit == 4) {               // two
+#pragma unroll 4
+                        for (int i = 0; i < 16; ++i) {
+                            const int r = 2 * i + (lane >> 4), byte = (lane & 15) * 4;
+                            if (r < rows && byte + 4 <= left) *reinterpret_cast<uint32_t *>(to + r * pitch + byte) = *reinterpret_cast<const uint32_t *>(parked(r, byte));
+                            else if (r < rows && byte + 2 <= left) *reinterpret_cast<uint16_t *>(to + r * pitch + byte) = *reinterpret_cast<const uint16_t *>(parked(r, byte));
+                        }
+                    } else {
+#pragma unroll 4
+                        for (int r = 0; r < 32; ++r)
+                            if (r < rows && lane * 2 < left) *reinterpret_cast<uint16_t *>(to + r * pitch + lane * 2) = *reinterpret_cast<const uint16_t *>(parked(r, lane * 2));
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
         }
     }

@@ -161,6 +161,7 @@ def test_linear_many_rows(M, N, K):
     if M * N < 4e6:
         check_linear(M, N, K, out="f32", scale=-0.75, ldc_pad=4, seed=N)
         check_linear(M, N, K, ld_pad=32, ldc_pad=3, offset=1, seed=K)
+        check_linear(M, N, K, ldc_pad=-N % 8, seed=K + 1)           # aligned rows whose last columns are no whole store
 
 
 def test_linear_many_rows_does_not_let_a_nan_leave_its_row_or_column():
@@ -180,6 +181,8 @@ def test_linear_many_rows_does_not_let_a_nan_leave_its_row_or_column():
 
 @pytest.mark.parametrize("M,N", [(4, 100), (150, 257), (300, 512)])
 def test_linear_types_strides_and_scale(M, N):
+    check_linear(M, N, 352, out="f32", ldc_pad=-N % 4)
+    check_linear(M, N, 352, out="bf16", ldc_pad=-N % 8)
     check_linear(M, N, 352, out="f32", scale=0.375, ld_pad=16, ldc_pad=3, offset=1)
     check_linear(M, N, 352, out="bf16", scale=-2.5, ld_pad=48, ldc_pad=5, offset=1)
     check_linear(M, N, 352, out="bf16", ldc_pad=8)
