@@ -82,6 +82,132 @@ __device__ __forceinline__ void put_some(T *at, const uint4 &v, int n)
         }
 }
 
+// ---- rows that do not lie on 16-byte boundaries: a warp's bytes are consecutive, so lanes load and store the aligned vectors that hold them
+// and shift their own bytes out of two neighbours' (element by element, 103658 x 3706 to codes and back took 1519 us).
+
+// words `at` .. `at` + N - 1 of w, where a word may start in the middle of another: `at` in bytes, even, below 16
+template <int N>
+__device__ __forceinline__ void words_at(const uint32_t (&w)[N + 4], uint32_t at, uint32_t (&out)[N])
+{
+    uint32_t x[N + 4];
+#pragma unroll
+    for (int i = 0; i < N + 4; ++i) x[i] = (at & 8) && i + 2 < N + 4 ? w[i + 2 < N + 4 ? i + 2 : i] : w[i];
+#pragma unroll
+    for (int i = 0; i + 1 < N + 4; ++i) x[i] = (at & 4) ? x[i + 1] : x[i];
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i] = (at & 2) ? __funnelshift_r(x[i], x[i + 1], 16) : x[i];
+}
+// the aligned vector at `at`, of which only what lies in [lo, hi) is read
+__device__ __forceinline__ uint4 load_within(uintptr_t at, uintptr_t lo, uintptr_t hi)
+{
+    if (at >= lo && at + 16 <= hi) return __ldcs(reinterpret_cast<const uint4 *>(at));
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (at + 2 * i >= lo && at + 2 * i < hi) w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t *>(at + 2 * i) << (16 * (i & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// What lane + 1 has, and lane 31 what lane 0 has of the warp's next piece, or `last` behind the last one.
+__device__ __forceinline__ uint4 of_next_lane(const uint4 &mine, const uint4 &piece_after, const uint4 &last, bool is_last, int lane)
+{
+    const uint4 t = lane == 0 && !is_last ? piece_after : mine;
+    uint4 n;
+    n.x = __shfl_sync(0xffffffffu, t.x, (lane + 1) & 31); n.y = __shfl_sync(0xffffffffu, t.y, (lane + 1) & 31);
+    n.z = __shfl_sync(0xffffffffu, t.z, (lane + 1) & 31); n.w = __shfl_sync(0xffffffffu, t.w, (lane + 1) & 31);
+    return lane == 31 && is_last ? last : n;
+}
+// What lane - 1 has, and lane 0 what lane 31 had of the piece before.
+__device__ __forceinline__ uint4 of_lane_before(const uint4 &mine, const uint4 &piece_before, int lane)
+{
+    const uint4 t = lane == 31 ? piece_before : mine;
+    uint4 n;
+    n.x = __shfl_sync(0xffffffffu, t.x, (lane + 31) & 31); n.y = __shfl_sync(0xffffffffu, t.y, (lane + 31) & 31);
+    n.z = __shfl_sync(0xffffffffu, t.z, (lane + 31) & 31); n.w = __shfl_sync(0xffffffffu, t.w, (lane + 31) & 31);
+    return n;
+}
+// a warp's U pieces of a row, lane's first value at `p`, the row's end at `row_end`, the matrix from `lo` to `hi`
+template <int U>
+__device__ __forceinline__ void load_shifted(Eight<__nv_bfloat16> (&v)[U], uintptr_t p, uintptr_t row_end, uintptr_t lo, uintptr_t hi, int)
+{
+    // five aligned words hold a lane's eight values (fewer instructions than vectors and shuffles, and the cache serves them as fast)
+    const uint32_t shift = (uint32_t)(p & 2) * 8;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uintptr_t at = (p & ~(uintptr_t)3) + u * 512;
+        if (p + u * 512 + 16 <= row_end && at >= lo && at + 20 <= hi) {
+            uint32_t w[5];
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t *>(at) + i);
+            v[u].a = make_uint4(__funnelshift_r(w[0], w[1], shift), __funnelshift_r(w[1], w[2], shift), __funnelshift_r(w[2], w[3], shift), __funnelshift_r(w[3], w[4], shift));
+        } else if (p + u * 512 < row_end) v[u].load_some(reinterpret_cast<const __nv_bfloat16 *>(p + u * 512), (int)min((uintptr_t)8, (row_end - p - u * 512) / 2));
+        else v[u].zero();
+    }
+}
+template <int U>
+__device__ __forceinline__ void load_shifted(Eight<float> (&v)[U], uintptr_t p, uintptr_t row_end, uintptr_t lo, uintptr_t hi, int lane)
+{
+    const uint32_t m = (uint32_t)(p & 15);
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    uint4 a[U], b[U], last = zero;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uintptr_t at = p - m + u * 1024;
+        a[u] = at < row_end ? load_within(at, lo, hi) : zero;
+        b[u] = at + 16 < row_end ? load_within(at + 16, lo, hi) : zero;
+    }
+    if (lane == 31 && m != 0) { const uintptr_t at = p - m + (U - 1) * 1024 + 32; if (at < row_end) last = load_within(at, lo, hi); }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint4 n = of_next_lane(a[u], a[u + 1 < U ? u + 1 : u], last, u + 1 == U, lane);
+        const uint32_t w[12] = {a[u].x, a[u].y, a[u].z, a[u].w, b[u].x, b[u].y, b[u].z, b[u].w, n.x, n.y, n.z, n.w};
+        uint32_t x[8];
+        words_at<8>(w, m, x);
+        const int left = (int)min((long long)8, max(0ll, ((long long)row_end - (long long)(p + u * 1024)) / 4));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i >= left ? 0u : x[i];
+        v[u].a = make_float4(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3]));
+        v[u].b = make_float4(__uint_as_float(x[4]), __uint_as_float(x[5]), __uint_as_float(x[6]), __uint_as_float(x[7]));
+    }
+}
+// The reverse: piece u of a warp's run [lo, hi) of a row, `v` this lane's values at `p`, `before` its piece u - 1.  Whole vectors inside the
+// run are stored by the lane in whose place they begin, what is left at the run's ends element by element.
+template <typename T>
+__device__ __forceinline__ void store_shifted(uintptr_t p, uintptr_t lo, uintptr_t hi, const uint4 &v, const uint4 &before, int lane)
+{
+    constexpr int WORDS = sizeof(T) == 4 ? 8 : 4;
+    const uint32_t m = (uint32_t)(p & 15);
+    const uint4 b = of_lane_before(v, before, lane);
+    uint32_t w[WORDS + 4], x[WORDS];
+    if constexpr (sizeof(T) == 4) {                         // (a bf16 value is the upper half of an fp32 one)
+        const uint32_t t[12] = {b.z << 16, b.z & 0xFFFF0000u, b.w << 16, b.w & 0xFFFF0000u, v.x << 16, v.x & 0xFFFF0000u, v.y << 16, v.y & 0xFFFF0000u,
+                                v.z << 16, v.z & 0xFFFF0000u, v.w << 16, v.w & 0xFFFF0000u};
+#pragma unroll
+        for (int i = 0; i < 12; ++i) w[i] = t[i];
+    } else {
+        const uint32_t t[8] = {b.x, b.y, b.z, b.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = t[i];
+    }
+    if (m == 0) {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) x[i] = w[i + 4];
+    } else words_at<WORDS>(w, 16 - m, x);
+    const uintptr_t a = p - m, own_end = p + WORDS * 4;
+#pragma unroll
+    for (int i = 0; i < WORDS / 4; ++i)
+        if (a + 16 * i >= lo && a + 16 * i + 16 <= hi) *reinterpret_cast<uint4 *>(a + 16 * i) = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    if (a < lo || ((own_end + 15) & ~(uintptr_t)15) > hi) { // this lane has values that no whole vector holds
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uintptr_t q = p + e * sizeof(T), qa = q & ~(uintptr_t)15;
+            if (q < hi && !(qa >= lo && qa + 16 <= hi)) {
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t *>(q) = w[4 + e];
+                else *reinterpret_cast<uint16_t *>(q) = (uint16_t)((e & 1) ? w[4 + e / 2] >> 16 : w[4 + e / 2]);
+            }
+        }
+    }
+}
+
 // the four lanes of a block: its scale, and this lane's eight codes
 template <typename T>
 __device__ __forceinline__ uint32_t quantize8(const Eight<T> &x, int lo, int hi, int &c)
@@ -128,13 +254,16 @@ quantize_kernel(const T *__restrict__ x, long long ldx, int rows, int cols, uint
         const bool in = at.row < rows, full = in && wide && (at.seg + 1) * 2 * U * 128 <= cols;
         const T *src = x + at.row * ldx + col0;
         Eight<T> v[U];
+        if (!in || wide) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int left = cols - col0 - u * 256;
-            if (full || (in && wide && left >= 8)) v[u].load(src + u * 256);
-            else if (in && left > 0) v[u].load_some(src + u * 256, left);
-            else v[u].zero();
-        }
+            for (int u = 0; u < U; ++u) {
+                const int left = cols - col0 - u * 256;
+                if (full || (in && left >= 8)) v[u].load(src + u * 256);
+                else if (in && left > 0) v[u].load_some(src + u * 256, left);
+                else v[u].zero();
+            }
+        } else
+            load_shifted<U>(v, (uintptr_t)src, (uintptr_t)(x + at.row * ldx + cols), (uintptr_t)x, (uintptr_t)(x + (rows - 1) * ldx + cols), lane);
         uint8_t *to = codes + at.row * ld_codes + quad0 * 64 + l * 4, *s = scales + scale_quad(at.row, quad0, quads) + (l >> 2);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -165,11 +294,82 @@ dequantize_kernel(const uint8_t *__restrict__ codes, long long ld_codes, const u
             if (col0 + u * 256 < cols) { w[u] = __ldcs(reinterpret_cast<const uint32_t *>(from + u * 128)); c[u] = s[u * 1024]; }
         }
         T *to = x + at.row * ldx + col0;
+        if (wide) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int left = cols - col0 - u * 256;
+                const uint4 v = mx4::decode8(w[u], c[u]);
+                if (left >= 8) put(to + u * 256, v); else put_some(to + u * 256, v, left);
+            }
+        } else {
+            const uintptr_t lo = (uintptr_t)(x + at.row * ldx + at.seg * 2 * U * 128), hi = min(lo + 2 * U * 128 * sizeof(T), (uintptr_t)(x + at.row * ldx + cols));
+            uint4 before = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint4 v = mx4::decode8(w[u], c[u]);
+                store_shifted<T>((uintptr_t)(to + u * 256), lo, hi, v, before, lane);
+                before = v;
+            }
+        }
+    }
+}
+
+// Rows of at most 256 columns: LANES lanes for one, so that a warp works on 32 / LANES rows (131072 x 32 with a warp for a row: 47 us).
+template <typename T, int LANES>
+__global__ void __launch_bounds__(kThreads)
+quantize_short_kernel(const T *__restrict__ x, long long ldx, int rows, int cols, uint8_t *__restrict__ codes, long long ld_codes, uint8_t *__restrict__ scales, int wide)
+{
+    pdl_wait();
+    pdl_trigger();
+    constexpr int PER = 32 / LANES, U = 4, QUADS = LANES == 32 ? 2 : 1;
+    const int lane = threadIdx.x & 31, l = lane % LANES, col = l * 8, tile_rows = (rows + 127) / 128 * 128, stride = gridDim.x * kWarps * PER;
+    for (int row0 = (blockIdx.x * kWarps + threadIdx.x / 32) * PER + lane / LANES; __any_sync(0xffffffffu, row0 < tile_rows); row0 += U * stride) {
+        Eight<T> v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int left = cols - col0 - u * 256;
+            const int row = row0 + u * stride;
+            const T *src = x + row * ldx + col;
+            if (row >= rows || col >= cols) v[u].zero();
+            else if (wide && col + 8 <= cols) v[u].load(src);
+            else v[u].load_some(src, cols - col);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = row0 + u * stride;
+            int c;
+            const uint32_t w = quantize8(v[u], 0, 254, c);
+            const bool in = row < rows && (l & ~3) * 8 < cols;                    // the lane's block exists
+            if (in) *reinterpret_cast<uint32_t *>(codes + row * ld_codes + l * 4) = w;
+            uint32_t s = in ? (uint32_t)c << ((l & 12) * 2) : 0u;                  // the padding of the tiles holds zeros
+            if (LANES >= 8) s |= __shfl_xor_sync(0xffffffffu, s, 4);
+            if (LANES >= 16) s |= __shfl_xor_sync(0xffffffffu, s, 8);
+            if ((l & 15) == 0 && row < tile_rows) *reinterpret_cast<uint32_t *>(scales + scale_quad(row, l / 16, QUADS)) = s;
+        }
+    }
+}
+template <typename T, int LANES>
+__global__ void __launch_bounds__(kThreads)
+dequantize_short_kernel(const uint8_t *__restrict__ codes, long long ld_codes, const uint8_t *__restrict__ scales, int rows, int cols, T *__restrict__ x, long long ldx, int wide)
+{
+    pdl_wait();
+    pdl_trigger();
+    constexpr int PER = 32 / LANES, U = 4, QUADS = LANES == 32 ? 2 : 1;
+    const int lane = threadIdx.x & 31, l = lane % LANES, col = l * 8, stride = gridDim.x * kWarps * PER;
+    if (col >= cols) return;
+    for (int row0 = (blockIdx.x * kWarps + threadIdx.x / 32) * PER + lane / LANES; row0 < rows; row0 += U * stride) {
+        uint32_t w[U], c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = row0 + u * stride;
+            w[u] = c[u] = 0;
+            if (row < rows) { w[u] = *reinterpret_cast<const uint32_t *>(codes + row * ld_codes + l * 4); c[u] = scales[scale_quad(row, l / 16, QUADS) + ((l & 15) >> 2)]; }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = row0 + u * stride;
+            if (row >= rows) break;
             const uint4 v = mx4::decode8(w[u], c[u]);
-            if (wide && left >= 8) put(to + u * 256, v); else put_some(to + u * 256, v, left);
+            if (wide && col + 8 <= cols) put(x + row * ldx + col, v); else put_some(x + row * ldx + col, v, cols - col);
         }
     }
 }
@@ -282,10 +482,19 @@ bool wide_rows(const void *base, int64_t ld, size_t element) { return aligned_to
 // CTAs for that many warps' segments: eight on an SM at most
 unsigned grid_for(long long segs) { return (unsigned)std::max<long long>(1, std::min<long long>((segs + kWarps - 1) / kWarps, (long long)gemm_num_sms() * 8)); }
 
+int short_lanes(int cols) { return cols <= 32 ? 4 : cols <= 64 ? 8 : cols <= 128 ? 16 : 32; }
+
 template <typename T>
 cudaError_t launch_quantize(const void *x, int64_t ldx, int rows, int cols, void *codes, int64_t ld_codes, void *scales, cudaStream_t stream)
 {
     const int quads = (cols + 127) / 128;
+    if (cols <= 256) {
+        const int lanes = short_lanes(cols);
+        const dim3 grid(grid_for(((long long)((rows + 127) / 128 * 128) * lanes / 32 + 3) / 4));
+        auto kernel = lanes == 4 ? quantize_short_kernel<T, 4> : lanes == 8 ? quantize_short_kernel<T, 8> : lanes == 16 ? quantize_short_kernel<T, 16> : quantize_short_kernel<T, 32>;
+        return launch_pdl(kernel, grid, dim3(kThreads), 0, stream, (const T *)x, (long long)ldx, rows, cols, (uint8_t *)codes, (long long)ld_codes, (uint8_t *)scales,
+                          (int)wide_rows(x, ldx, sizeof(T)));
+    }
     const dim3 grid(grid_for((long long)((rows + 127) / 128 * 128) * segments(quads)));
     return launch_pdl(long_rows(quads) ? quantize_kernel<T, kLong> : quantize_kernel<T, 1>, grid, dim3(kThreads), 0, stream, (const T *)x, (long long)ldx, rows, cols,
                       (uint8_t *)codes, (long long)ld_codes, (uint8_t *)scales, quads, (int)wide_rows(x, ldx, sizeof(T)));
@@ -294,6 +503,13 @@ template <typename T>
 cudaError_t launch_dequantize(const void *codes, int64_t ld_codes, const void *scales, int rows, int cols, void *x, int64_t ldx, cudaStream_t stream)
 {
     const int quads = (cols + 127) / 128;
+    if (cols <= 256) {
+        const int lanes = short_lanes(cols);
+        const dim3 grid(grid_for(((long long)rows * lanes / 32 + 3) / 4));
+        auto kernel = lanes == 4 ? dequantize_short_kernel<T, 4> : lanes == 8 ? dequantize_short_kernel<T, 8> : lanes == 16 ? dequantize_short_kernel<T, 16> : dequantize_short_kernel<T, 32>;
+        return launch_pdl(kernel, grid, dim3(kThreads), 0, stream, (const uint8_t *)codes, (long long)ld_codes, (const uint8_t *)scales, rows, cols, (T *)x, (long long)ldx,
+                          (int)wide_rows(x, ldx, sizeof(T)));
+    }
     const dim3 grid(grid_for((long long)rows * segments(quads)));
     return launch_pdl(long_rows(quads) ? dequantize_kernel<T, kLong> : dequantize_kernel<T, 1>, grid, dim3(kThreads), 0, stream, (const uint8_t *)codes,
                       (long long)ld_codes, (const uint8_t *)scales, rows, cols, (T *)x, (long long)ldx, quads, (int)wide_rows(x, ldx, sizeof(T)));

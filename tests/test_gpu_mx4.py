@@ -43,7 +43,7 @@ def quantize_on_gpu(t, dtype, ld=None, offset=0, pad=0):
     return codes, scales
 
 
-SHAPES = [(1, 1), (1, 32), (3, 40), (128, 128), (129, 96), (5, 688), (130, 257), (33, 4096), (257, 1000)]
+SHAPES = [(1, 1), (1, 32), (3, 40), (128, 128), (129, 96), (5, 688), (130, 257), (33, 4096), (257, 1000), (7, 3), (1000, 20), (700, 64), (3000, 33), (261, 256), (300, 200), (9, 519), (6, 1021), (4, 1031), (5, 2047), (3, 3706)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -51,7 +51,8 @@ SHAPES = [(1, 1), (1, 32), (3, 40), (128, 128), (129, 96), (5, 688), (130, 257),
 def test_quantize_gives_the_formats_codes_and_scales(rows, cols, dtype):
     t, x = as_input(matrix(rows, cols, rows * 7 + cols), dtype)
     want_codes, want_scales = R.quantize(x, R.MATRIX)
-    for ld, offset, pad in ((cols, 0, 0), (cols + 3, 1, 16)):       # aligned rows, and rows at odd addresses beside a guard
+    # aligned rows, and rows at every other address, beside a guard
+    for ld, offset, pad in ((cols, 0, 0), (cols + 3, 1, 16), (cols + 1, 3, 0), (cols + 2, 6, 32), (cols, 5, 0)):
         codes, scales = quantize_on_gpu(t, dtype, ld, offset, pad)
         n = sfs.mx4_code_bytes(cols)
         assert (codes[:, :n].cpu().numpy() == R.pack(want_codes)).all()
@@ -93,7 +94,7 @@ def test_dequantize_gives_the_values(rows, cols, dtype):
     scales[0, 0] = 255
     scales[-1, -1] = 0 if dtype == "f32" else 30
     want = R.values(codes, scales)[:, :cols]
-    for ld, offset in ((cols, 0), (cols + 5, 1)):
+    for ld, offset in ((cols, 0), (cols + 5, 1), (cols, 3), (cols + 1, 2), (cols + 2, 7)):
         buf = torch.full((rows * ld + offset,), 77.0, dtype=TYPES[dtype][0], device=DEV)
         out = buf[offset:].view(rows, ld)
         sfs.sfs_mx4_dequantize(dev(R.pack(codes)), blocks * 16, dev(R.tile_scales(scales)), rows, cols, out, ld, TYPES[dtype][1])
