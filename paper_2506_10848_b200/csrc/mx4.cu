@@ -474,10 +474,21 @@ cache_load_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restrict
     }
 }
 
-// A segment of a row: 8 quads (1024 columns), four loads of a lane in flight, or 2 where rows are short.
-constexpr int kLong = 4;
-bool long_rows(int quads) { return quads > 4; }
-int segments(int quads) { return long_rows(quads) ? (quads + 2 * kLong - 1) / (2 * kLong) : (quads + 1) / 2; }
+// Pieces of a lane in a segment (2 U quads), one to four loads in flight: the longest segment that leaves at most an eighth of a row's
+// lanes without work, else the one that leaves the fewest. 81713 x 597 16-bit values, 5 quads: 111 us at one piece, 137 at four;
+// 39518 x 3382, 27 quads: 241 us at two, 260 at four.
+int pieces(int quads)
+{
+    int best = 1, waste = 1 << 30;
+    for (int u = 1; u <= 4; ++u) {
+        const int w = (quads + 2 * u - 1) / (2 * u) * (2 * u) - quads;
+        if (w * 8 <= quads || w <= waste) { waste = w; best = u; }
+    }
+    return best;
+}
+int segments(int quads) { const int u = pieces(quads); return (quads + 2 * u - 1) / (2 * u); }
+// the instance of a kernel template <T, U> for rows of that many quads
+#define SFS_BY_PIECES(kernel, quads) (pieces(quads) == 4 ? kernel<T, 4> : pieces(quads) == 3 ? kernel<T, 3> : pieces(quads) == 2 ? kernel<T, 2> : kernel<T, 1>)
 bool wide_rows(const void *base, int64_t ld, size_t element) { return aligned_to(base, 16) && (ld * (int64_t)element) % 16 == 0; }
 // CTAs for that many warps' segments: eight on an SM at most
 unsigned grid_for(long long segs) { return (unsigned)std::max<long long>(1, std::min<long long>((segs + kWarps - 1) / kWarps, (long long)gemm_num_sms() * 8)); }
@@ -496,7 +507,7 @@ cudaError_t launch_quantize(const void *x, int64_t ldx, int rows, int cols, void
                           (int)wide_rows(x, ldx, sizeof(T)));
     }
     const dim3 grid(grid_for((long long)((rows + 127) / 128 * 128) * segments(quads)));
-    return launch_pdl(long_rows(quads) ? quantize_kernel<T, kLong> : quantize_kernel<T, 1>, grid, dim3(kThreads), 0, stream, (const T *)x, (long long)ldx, rows, cols,
+    return launch_pdl(SFS_BY_PIECES(quantize_kernel, quads), grid, dim3(kThreads), 0, stream, (const T *)x, (long long)ldx, rows, cols,
                       (uint8_t *)codes, (long long)ld_codes, (uint8_t *)scales, quads, (int)wide_rows(x, ldx, sizeof(T)));
 }
 template <typename T>
@@ -511,7 +522,7 @@ cudaError_t launch_dequantize(const void *codes, int64_t ld_codes, const void *s
                           (int)wide_rows(x, ldx, sizeof(T)));
     }
     const dim3 grid(grid_for((long long)rows * segments(quads)));
-    return launch_pdl(long_rows(quads) ? dequantize_kernel<T, kLong> : dequantize_kernel<T, 1>, grid, dim3(kThreads), 0, stream, (const uint8_t *)codes,
+    return launch_pdl(SFS_BY_PIECES(dequantize_kernel, quads), grid, dim3(kThreads), 0, stream, (const uint8_t *)codes,
                       (long long)ld_codes, (const uint8_t *)scales, rows, cols, (T *)x, (long long)ldx, quads, (int)wide_rows(x, ldx, sizeof(T)));
 }
 template <typename T>
@@ -521,7 +532,7 @@ cudaError_t launch_store(const sfs_cache4 &c, const void *k, int64_t ld_k, const
     // few rows: one or two for a CTA, so that they spread over the machine
     const int cta_rows = std::min(kStoreRows, std::max(1, n_rows / gemm_num_sms()));
     const dim3 grid((unsigned)((n_rows + cta_rows - 1) / cta_rows), 2);
-    return launch_pdl(long_rows(quads) ? cache_store_kernel<T, kLong> : cache_store_kernel<T, 1>, grid, dim3(kThreads), 0, stream, (uint8_t *)c.k_codes,
+    return launch_pdl(SFS_BY_PIECES(cache_store_kernel, quads), grid, dim3(kThreads), 0, stream, (uint8_t *)c.k_codes,
                       (uint8_t *)c.k_scales, (uint8_t *)c.v_codes, (uint8_t *)c.v_scales, c.batch * c.capacity, width, (const T *)k, (long long)ld_k,
                       (const T *)v, (long long)ld_v, (int)wide_rows(k, ld_k, sizeof(T)), (int)wide_rows(v, ld_v, sizeof(T)), slots, n_rows, cta_rows);
 }
@@ -530,7 +541,7 @@ cudaError_t launch_load(const sfs_cache4 &c, const int32_t *slots, int n_rows, v
 {
     const int width = c.n_kv_heads * c.head_dim, quads = (width + 127) / 128;
     const dim3 grid(grid_for((long long)n_rows * segments(quads)), 2);
-    return launch_pdl(long_rows(quads) ? cache_load_kernel<T, kLong> : cache_load_kernel<T, 1>, grid, dim3(kThreads), 0, stream, (const uint8_t *)c.k_codes,
+    return launch_pdl(SFS_BY_PIECES(cache_load_kernel, quads), grid, dim3(kThreads), 0, stream, (const uint8_t *)c.k_codes,
                       (const uint8_t *)c.k_scales, (const uint8_t *)c.v_codes, (const uint8_t *)c.v_scales, c.batch * c.capacity, width, (T *)k, (long long)ld_k,
                       (T *)v, (long long)ld_v, (int)wide_rows(k, ld_k, sizeof(T)), (int)wide_rows(v, ld_v, sizeof(T)), slots, n_rows);
 }
