@@ -46,6 +46,9 @@ __device__ __forceinline__ void store_chunk(uint32_t smem, uint32_t x, uint32_t 
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
+__device__ __forceinline__ void copy16(uint32_t smem, const void *global) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory"); }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void store_remote4(uint32_t cluster_addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
 {
@@ -71,13 +74,13 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
     constexpr int KB = DH / 64, WORDS = DH / 8, BLOCKS = DH / 32;
     constexpr int Q_BYTES = QT * DH * 2, K_BYTES = KT * DH * 2, V_BYTES = DH * KT * 2;
     constexpr int ROWS = NQ * QT;
-    constexpr int V_WARPS = DH / 16;                        // decoding warps that have values (16 token groups x WORDS pieces)
+    constexpr int RAW = DH / 2 + 16, RAW_BYTES = KT * RAW;  // a token's values as they lie in the cache, codes and scales; odd in 16 bytes
     constexpr uint32_t TMEM_COLS = 512;                     // S / P and O of each stream: 2 x (128 + DH) columns
 
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t *sQ = smem, *sK = smem + NQ * Q_BYTES, *sV = sK + kStages * K_BYTES;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(sV + kStages * V_BYTES);
+    uint8_t *sQ = smem, *sK = smem + NQ * Q_BYTES, *sV = sK + kStages * K_BYTES, *sRaw = sV + kStages * V_BYTES;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(sRaw + 2 * RAW_BYTES);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + kBars);
     float4 *s_o = reinterpret_cast<float4 *>(sK);           // [splits][QT / splits][DH / 4], what the ranks send once all MMAs are done
     __shared__ int s_abort, s_any_bad, s_range[3];          // first, lo, hi over the CTA's rows
@@ -100,7 +103,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             tc::mbar_init(bar_kfull + 8 * s, kDecoders); tc::mbar_init(bar_kempty + 8 * s, 1);
-            tc::mbar_init(bar_vfull + 8 * s, V_WARPS * 32); tc::mbar_init(bar_vempty + 8 * s, 1);
+            tc::mbar_init(bar_vfull + 8 * s, kDecoders); tc::mbar_init(bar_vempty + 8 * s, 1);
         }
         for (int w = 0; w < 2; ++w) { tc::mbar_init(bar_s + 8 * w, 1); tc::mbar_init(bar_p + 16 * w, QT); tc::mbar_init(bar_p + 16 * w + 8, QT); }
         tc::mbar_init(bar_x, 2 * QT); tc::mbar_init(bar_q, 2 * QT);
@@ -155,25 +158,32 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
         constexpr int LANES = BLOCKS, KEYS = KT * LANES / kDecoders;         // lanes of a key, one block of features each, and keys of a thread
         const int n0 = threadIdx.x / LANES, kt = threadIdx.x % LANES;
-        const int ct = lane & 7, u = warp * 4 + (lane >> 3), kb = u / WORDS, w0 = u % WORDS;
-        const bool has_values = warp < V_WARPS;
-        uint4 k_next[KEYS], kc[KEYS]; uint32_t ks_next[KEYS], ks[KEYS], v_next[8], vc[8], vs_next[8], vs[8];
+        constexpr int HALVES = kDecoders / (16 * WORDS);                     // threads of a value piece, each with 8 or 4 of the word's features
+        const int ct = lane & 7, u = warp * 4 + (lane >> 3), kb = u / (WORDS * HALVES), w0 = u % (WORDS * HALVES) / HALVES, part = u % HALVES;
+        const int code_pitch = a.n_kv * (DH / 2), scale_pitch = a.n_kv * BLOCKS;
+        const uint8_t *k_codes = a.k_codes + base * (DH / 2) + kt * 16, *k_scales = a.k_scales + base * BLOCKS + kt;
+        const uint8_t *v_codes = a.v_codes + base * (DH / 2) + kt * 16, *v_scales = a.v_scales + base * BLOCKS + kt;
+        uint4 k_next[KEYS], kc[KEYS]; uint32_t ks_next[KEYS], ks[KEYS], vs_next[KEYS];
         auto fetch_k = [&](int j) {
 #pragma unroll
             for (int e = 0; e < KEYS; ++e) {
-                const size_t at = base + (size_t)token(tile_start(j) + n0 + e * (KT / KEYS)) * a.n_kv;
-                k_next[e] = *reinterpret_cast<const uint4 *>(a.k_codes + at * (DH / 2) + kt * 16);
-                ks_next[e] = a.k_scales[at * BLOCKS + kt];
+                const long long t = token(tile_start(j) + n0 + e * (KT / KEYS));
+                k_next[e] = *reinterpret_cast<const uint4 *>(k_codes + t * code_pitch);
+                ks_next[e] = k_scales[t * scale_pitch];
             }
         };
+        // Values come as whole blocks too: a thread's own words of eight tokens would be sixteen loads of eight cache lines each (tile of
+        // 128 tokens, 128 features: XXX).  Token n lies in slot 64 (n / 64) + 8 (n % 8) + n / 8 % 8, so that the readers' banks differ.
+        auto raw_slot = [&](int j, int slot) { return tc::smem_u32(sRaw) + (j & 1) * RAW_BYTES + slot * RAW; };
+        auto own_slot = [&](int j, int e) { const int n = n0 + e * (KT / KEYS); return raw_slot(j, (n & ~63) + (n & 7) * 8 + ((n >> 3) & 7)); };
         auto fetch_v = [&](int j) {
-            const int v0 = tile_start(j) + kb * 64 + ct * 8;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const size_t at = base + (size_t)token(v0 + i) * a.n_kv;
-                v_next[i] = *reinterpret_cast<const uint32_t *>(a.v_codes + at * (DH / 2) + w0 * 4);
-                vs_next[i] = a.v_scales[at * BLOCKS + w0 / 4];
+            for (int e = 0; e < KEYS; ++e) {
+                const long long t = token(tile_start(j) + n0 + e * (KT / KEYS));
+                copy16(own_slot(j, e) + kt * 16, v_codes + t * code_pitch);
+                vs_next[e] = v_scales[t * scale_pitch];
             }
+            copies_commit();
         };
         auto free_phase = [](int j) { return ((uint32_t)(j / kStages) & 1u) ^ 1u; };
         auto decode_k = [&](int j) {
@@ -203,11 +213,23 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
             tc::mbar_arrive(bar_kfull + 8 * s);
             return true;
         };
+        auto share_v = [&](int j) {                         // all decoders, also after a wait that gave up: they meet here
+            copies_wait();
+#pragma unroll
+            for (int e = 0; e < KEYS; ++e) asm volatile("st.shared.u8 [%0], %1;" ::"r"(own_slot(j, e) + DH / 2 + kt), "r"(vs_next[e]) : "memory");
+            __syncwarp();
+            asm volatile("barrier.sync 1, %0;" ::"n"(kDecoders) : "memory");
+            if (j + 1 < n_tiles) fetch_v(j + 1);            // (its place was read before tile j was shared)
+        };
         auto decode_v = [&](int j) {
             const int s = j % kStages;
+            uint32_t vc[8], vs[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { vc[i] = v_next[i]; vs[i] = vs_next[i]; }
-            if (j + 1 < n_tiles) fetch_v(j + 1);
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t at = raw_slot(j, kb * 64 + i * 8 + ct);
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(vc[i]) : "r"(at + w0 * 4) : "memory");
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(vs[i]) : "r"(at + DH / 2 + w0 / 4) : "memory");
+            }
             uint32_t f[4], bad = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -217,7 +239,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
                 f[i] = (bad0 ? 0u : (vs[2 * i] + 62) << 7) | (bad1 ? 0u : (vs[2 * i + 1] + 62) << 23);
             }
             if (!tc::mbar_wait(bar_vempty + 8 * s, free_phase(j), &s_abort)) return false;
-            if (w0 % 4 == 0) s_bad[j & 3][w0 / 4][kb * 8 + ct] = (uint8_t)bad;
+            if (w0 % 4 == 0 && part == 0) s_bad[j & 3][w0 / 4][kb * 8 + ct] = (uint8_t)bad;
             if (bad) s_any_bad = 1;
             const uint32_t sv = tc::smem_u32(sV) + s * V_BYTES + kb * (DH * 128) + w0 * 8 * 128;
             uint32_t x[4];
@@ -225,14 +247,13 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
                 store_chunk(sv + d * 128 + ((ct ^ d) * 16), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[0]), f[0]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[1]), f[1]),
                             mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[2]), f[2]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[3]), f[3]));
             };
+            auto four = [&](int h) {                        // features 4 h to 4 h + 3 of the word
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = __byte_perm(vc[2 * i], vc[2 * i + 1], 0x5410);              // features 0-3 of both tokens
-            feature(std::integral_constant<int, 0>(), 0); feature(std::integral_constant<int, 1>(), 1);
-            feature(std::integral_constant<int, 2>(), 2); feature(std::integral_constant<int, 3>(), 3);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = __byte_perm(vc[2 * i], vc[2 * i + 1], 0x7632);              // features 4-7
-            feature(std::integral_constant<int, 0>(), 4); feature(std::integral_constant<int, 1>(), 5);
-            feature(std::integral_constant<int, 2>(), 6); feature(std::integral_constant<int, 3>(), 7);
+                for (int i = 0; i < 4; ++i) x[i] = __byte_perm(vc[2 * i], vc[2 * i + 1], h ? 0x7632 : 0x5410);
+                feature(std::integral_constant<int, 0>(), 4 * h); feature(std::integral_constant<int, 1>(), 4 * h + 1);
+                feature(std::integral_constant<int, 2>(), 4 * h + 2); feature(std::integral_constant<int, 3>(), 4 * h + 3);
+            };
+            if (HALVES == 1) { four(0); four(1); } else four(part);
             fence_async_shared();
             tc::mbar_arrive(bar_vfull + 8 * s);
             return true;
@@ -241,11 +262,14 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
         // Streams over odd and even tiles: keys one tile ahead of values, for the other stream's first scores (128 rows over 1536 tokens, 32
         // heads: 17.3 us without, 16.7 with; row tiles that share a tile want its values sooner, 105 us instead of 102 for 2048 x 2048).
         bool ok = true;
-        for (int j = PAIR ? 0 : -1; j < n_tiles && ok; ++j) {
+        for (int j = PAIR ? 0 : -1; j < n_tiles; ++j) {
             const int jk = PAIR ? j : j + 1;
-            if (jk < n_tiles) ok = decode_k(jk);
-            if (jk == 0 && has_values) fetch_v(0);          // (not sooner: the first keys and the queries come first)
-            if (ok && j >= 0 && has_values) ok = decode_v(j);
+            if (jk < n_tiles && ok) ok = decode_k(jk);
+            if (jk == 0) fetch_v(0);                        // (not sooner: the first keys and the queries come first)
+            if (j >= 0) {
+                share_v(j);
+                ok = ok && decode_v(j);
+            }
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
@@ -542,7 +566,7 @@ template <int DH, bool PAIR>
 int32_t launch(const Cache4Args &a, int log_splits, cudaStream_t stream)
 {
     constexpr int NQ = PAIR ? 2 : 1;
-    constexpr size_t shared = 1024 + (size_t)NQ * QT * DH * 2 + (size_t)kStages * 2 * KT * DH * 2 + kBars * 8 + 16;
+    constexpr size_t shared = 1024 + (size_t)NQ * QT * DH * 2 + (size_t)kStages * 2 * KT * DH * 2 + 2 * (size_t)KT * (DH / 2 + 16) + kBars * 8 + 16;
     const long long row_tiles = ((long long)a.n_q * a.group + NQ * QT - 1) / (NQ * QT), ctas = ((long long)a.batch * a.n_kv * row_tiles) << log_splits;
     SFS_REQUIRE(ctas <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
     SFS_CUDA(allow_shared(attention_cache4_many_kernel<DH, PAIR>, shared));
