@@ -173,7 +173,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
             }
         };
         // Values come as whole blocks too: a thread's own words of eight tokens would be sixteen loads of eight cache lines each (tile of
-        // 128 tokens, 128 features: XXX).  Token n lies in slot 64 (n / 64) + 8 (n % 8) + n / 8 % 8, so that the readers' banks differ.
+        // 128 tokens, 128 features: 800 clocks to issue).  Token n lies in slot 64 (n / 64) + 8 (n % 8) + n / 8 % 8, so that the readers' banks differ.
         auto raw_slot = [&](int j, int slot) { return tc::smem_u32(sRaw) + (j & 1) * RAW_BYTES + slot * RAW; };
         auto own_slot = [&](int j, int e) { const int n = n0 + e * (KT / KEYS); return raw_slot(j, (n & ~63) + (n & 7) * 8 + ((n >> 3) & 7)); };
         auto fetch_v = [&](int j) {
@@ -265,7 +265,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
         for (int j = PAIR ? 0 : -1; j < n_tiles; ++j) {
             const int jk = PAIR ? j : j + 1;
             if (jk < n_tiles && ok) ok = decode_k(jk);
-            if (jk == 0) fetch_v(0);                        // (not sooner: the first keys and the queries come first)
+            if (jk == 0 && n_tiles > 0) fetch_v(0);         // (not sooner: the first keys and the queries come first)
             if (j >= 0) {
                 share_v(j);
                 ok = ok && decode_v(j);
