@@ -490,7 +490,7 @@ extern "C" int32_t sfs_attention_cache4(const sfs_cache4 *cache, const void *d_q
     const int64_t tokens = left >= 0 && right >= 0 ? std::min<int64_t>(cache->capacity, (int64_t)left + right + n_q + sinks) : cache->capacity;
     const int64_t row_tiles = (rows + kRows - 1) / kRows;
     const int log_splits = splits_of(heads * row_tiles, tokens);
-    if (rows > kRows && attention_cache4_many_us(a, tokens) < few_us(heads * row_tiles, tokens, log_splits)) {
+    if (rows > kRows && attention_cache4_many_us(a, tokens, cache->head_dim) < few_us(heads * row_tiles, tokens, log_splits)) {
         const int32_t rc = status_word_outside_captures((cudaStream_t)stream, &a.err);
         return rc != SFS_OK ? rc : attention_cache4_many(a, tokens, cache->head_dim, (cudaStream_t)stream);
     }

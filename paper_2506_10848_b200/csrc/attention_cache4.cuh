@@ -33,7 +33,7 @@ __device__ __forceinline__ Seen cache4_seen(const Cache4Args &a, int length, lon
 
 // Rows are many: the tensor-memory kernel, and an estimate of its time.  `tokens`: how many a row sees at most.
 int32_t attention_cache4_many(const Cache4Args &a, int64_t tokens, int head_dim, cudaStream_t stream);
-double attention_cache4_many_us(const Cache4Args &a, int64_t tokens);
+double attention_cache4_many_us(const Cache4Args &a, int64_t tokens, int head_dim);
 int32_t cache4_check(const sfs_cache4 *c, const char *what);
 
 }  // namespace sfs

@@ -3,17 +3,20 @@
 //
 // A CTA has two streams of 128 rows x 128-key tiles, so that the tensor core works on one while the other is in its softmax: two row tiles
 // that share every decoded key and value tile (PAIR), or the even and the odd key tiles of one row tile.  A row is a (query, head) pair of
-// the key head's group.  Warps 0-7 decode: blocks of keys' codes, whose words of 8 features become 16-byte chunks of the
+// the key head's group.  The first 8 or 16 warps decode: blocks of keys' codes, whose words of 8 features become 16-byte chunks of the
 // 128-byte-swizzled K-major tile (the order of features within a word is that of the decoding, the same for queries), then a piece of eight
 // tokens' values, which comes out transposed, eight tokens of a feature to a chunk.  The codes of the next tile are in flight meanwhile.
-// Warps 8-15 are the softmax of the streams, one thread per row, warp 16 issues the MMAs.
+// The next eight are the softmax of the streams, one thread per row, the last issues the MMAs.
 //
 // Decoded values are exact: bits moved into bf16 (times 2^-126), one product with 2^(c - 65), so a common factor of 2^-64 remains, which
 // scores get back in 32 bits and values from the probabilities, taken 2^64 times as large.
 //
-// Bound: the softmax warps' chain (scores, maximum, exponentials, hand-over: 3300 clocks of a tile, which the decoding warps stretch by
-// sharing the pipes) with the MMAs behind it (1300), about 5300 clocks for a tile of both streams; the tensor pipe is 29 % busy, issue 49 %.
-// Measured, 32 heads of 128, us: 2048 rows over 2048 tokens 101 (attention_kernel on bf16 values 73), 128 rows over 1536 16.5.
+// Bound, where row tiles share what is decoded: the softmax warps' chain (scores, maximum, exponentials, hand-over: 3300 clocks of a tile,
+// which the decoding warps stretch by sharing the pipes) with the MMAs behind it (1300), about 5000 clocks for a tile of both streams.
+// Alone, the decoders: 3300 clocks of a tile, 16 instructions for a word of 8 codes; issue 57 % busy, shared memory 36 %, tensor pipe 21 %.
+// Measured, 32 heads of 128, us: 2048 rows over 2048 tokens 97 (attention_kernel on bf16 values 73), 72 rows over 4 x 5344 88, 128 rows
+// over 1536 15.2.  Scores of the next tile's second half issued while this one's is in its softmax: 118 instead of 97, MMAs of 64 keys
+// read the queries twice as often.
 //
 // Only key tiles that some row sees are visited.  With few CTAs the tiles are divided over a cluster of up to 8, whose partial outputs
 // meet in shared memory, in rank order.
@@ -29,12 +32,18 @@ using mx4::cache_factor;
 using mx4::codes_as_bf16;
 using mx4::mul_bf16x2;
 
-constexpr int kMmaWarp = 16;
-constexpr int kThreads = (kMmaWarp + 1) * 32;               // 8 decoding warps, 2 x 4 softmax warps, the MMA warp
-constexpr int kDecoders = 256;
-// Registers: the launch's share is what five warps of a quarter of the SM can have; the decoders give some to the softmax.
-constexpr int kRegs = 96, kDecodeRegs = 64, kSoftmaxRegs = 128;
-static_assert(kDecoders * kDecodeRegs + 256 * kSoftmaxRegs + 32 * kRegs <= kThreads * kRegs, "what is taken was given or is free");
+constexpr int kDecoders = 256;                              // threads that decode keys, and those that decode values: the same, or others
+// Warps: 8 or 16 that decode, 2 x 4 for the softmax, one for the MMAs.  Pairs of row tiles of 128 features want their decoding in the
+// background: warps for keys and others for values (2048 rows over 2048 tokens, 32 heads: 97 us, 105 with the same; 5440 over 4096, 12
+// heads: 176 and 166).  Registers: the launch's share is what the warps of a quarter of the SM can have, seven or five; the decoders give
+// some to the softmax, four or two of them to two in each quarter, so that each quarter has what it needs.
+template <int DH, bool PAIR>
+struct Roles {
+    static constexpr bool kApart = DH == 128 && PAIR;
+    static constexpr int kSoftmaxWarp = kApart ? 16 : 8, kMmaWarp = kSoftmaxWarp + 8, kThreads = (kMmaWarp + 1) * 32;
+    static constexpr int kRegs = kApart ? 72 : 96, kDecodeRegs = kApart ? 40 : DH == 64 ? 56 : 64, kSoftmaxRegs = kApart || DH == 64 ? 136 : 128;
+    static_assert(kSoftmaxWarp / 4 * kDecodeRegs + 2 * kSoftmaxRegs <= (kSoftmaxWarp / 4 + 2) * kRegs, "what is taken was given or is free");
+};
 constexpr int QT = 128;                                     // rows of a stream
 constexpr int KT = 128;                                     // keys of a tile
 constexpr int kStages = 2;
@@ -47,6 +56,20 @@ __device__ __forceinline__ void store_chunk(uint32_t smem, uint32_t x, uint32_t 
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 __device__ __forceinline__ void copy16(uint32_t smem, const void *global) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory"); }
+// Loads that keep out of the first-level cache: next to this much shared memory it has 28 KB, in lines of 128 bytes, of which a token's
+// codes and scales would each take one for as long as they are under way.
+__device__ __forceinline__ uint4 load16(const uint8_t *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t load1(const uint8_t *p)
+{
+    uint32_t v;
+    asm volatile("ld.global.L1::no_allocate.u8 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -67,14 +90,17 @@ __device__ __forceinline__ unsigned long long bit_range(int from, int to)
 }
 
 template <int DH, bool PAIR>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Roles<DH, PAIR>::kThreads, 1)
 attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
 {
+    using R = Roles<DH, PAIR>;
+    constexpr int kSoftmaxWarp = R::kSoftmaxWarp, kMmaWarp = R::kMmaWarp, kThreads = R::kThreads;
     constexpr int NQ = PAIR ? 2 : 1;
     constexpr int KB = DH / 64, WORDS = DH / 8, BLOCKS = DH / 32;
     constexpr int Q_BYTES = QT * DH * 2, K_BYTES = KT * DH * 2, V_BYTES = DH * KT * 2;
     constexpr int ROWS = NQ * QT;
-    constexpr int RAW = DH / 2 + 16, RAW_BYTES = KT * RAW;  // a token's values as they lie in the cache, codes and scales; odd in 16 bytes
+    constexpr int RAW = DH / 2 + 16;                        // a token's codes of values as they lie in the cache; odd in 16 bytes
+    constexpr int RAW8 = 8 * RAW + DH / 2, RAW_BYTES = KT / 8 * RAW8;
     constexpr uint32_t TMEM_COLS = 512;                     // S / P and O of each stream: 2 x (128 + DH) columns
 
     extern __shared__ uint8_t smem_raw[];
@@ -86,6 +112,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
     __shared__ int s_abort, s_any_bad, s_range[3];          // first, lo, hi over the CTA's rows
     __shared__ int s_lo[ROWS], s_hi[ROWS], s_first[ROWS], s_query[ROWS];          // s_query: a row's query; its head in the group is what is left
     __shared__ uint8_t s_bad[4][BLOCKS][KT / 8];            // tokens whose values are NaN, by tile (four in turn) and block of features
+    __shared__ __align__(16) uint16_t s_factor[2][BLOCKS][KT];     // of values' scales, by tile (two in turn), block and token
     __shared__ float s_max[2][QT], s_den[2][QT];
     __shared__ float2 s_ml[QT];                             // [splits][QT / splits], their maxima and denominators
     __shared__ uint32_t s_nan[2][QT];
@@ -152,40 +179,25 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
     auto key_tile = [&](int w, int i) { return PAIR ? i : 2 * i + w; };
 
     const size_t base = (size_t)b * a.capacity * a.n_kv + kv;
-    if (warp < kDecoders / 32) {
+    if (warp < kSoftmaxWarp) {
         // ---------------- decoding, the codes of the next tile in flight.  Keys: a thread has a block of one or two keys.  Values: a piece of
         // eight tokens (8 ct .. of half kb of the tile) by a word of features, which comes out transposed.
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R::kDecodeRegs));
         constexpr int LANES = BLOCKS, KEYS = KT * LANES / kDecoders;         // lanes of a key, one block of features each, and keys of a thread
-        const int n0 = threadIdx.x / LANES, kt = threadIdx.x % LANES;
-        constexpr int HALVES = kDecoders / (16 * WORDS);                     // threads of a value piece, each with 8 or 4 of the word's features
-        const int ct = lane & 7, u = warp * 4 + (lane >> 3), kb = u / (WORDS * HALVES), w0 = u % (WORDS * HALVES) / HALVES, part = u % HALVES;
-        const int code_pitch = a.n_kv * (DH / 2), scale_pitch = a.n_kv * BLOCKS;
-        const uint8_t *k_codes = a.k_codes + base * (DH / 2) + kt * 16, *k_scales = a.k_scales + base * BLOCKS + kt;
-        const uint8_t *v_codes = a.v_codes + base * (DH / 2) + kt * 16, *v_scales = a.v_scales + base * BLOCKS + kt;
-        uint4 k_next[KEYS], kc[KEYS]; uint32_t ks_next[KEYS], ks[KEYS], vs_next[KEYS];
+        const int tid = threadIdx.x % kDecoders, n0 = tid / LANES, kt = tid % LANES;
+        const long long block0 = (long long)base * BLOCKS + kt;             // of a slot's first token, in blocks of 16 bytes of codes and a scale
+        const int block_pitch = a.n_kv * BLOCKS;
+        auto free_phase = [](int j) { return ((uint32_t)(j / kStages) & 1u) ^ 1u; };
+        bool ok = true;
+        uint4 k_next[KEYS], kc[KEYS]; uint32_t ks_next[KEYS], ks[KEYS];
         auto fetch_k = [&](int j) {
 #pragma unroll
             for (int e = 0; e < KEYS; ++e) {
-                const long long t = token(tile_start(j) + n0 + e * (KT / KEYS));
-                k_next[e] = *reinterpret_cast<const uint4 *>(k_codes + t * code_pitch);
-                ks_next[e] = k_scales[t * scale_pitch];
+                const long long block = block0 + (long long)token(tile_start(j) + n0 + e * (KT / KEYS)) * block_pitch;
+                k_next[e] = load16(a.k_codes + block * 16);
+                ks_next[e] = load1(a.k_scales + block);
             }
         };
-        // Values come as whole blocks too: a thread's own words of eight tokens would be sixteen loads of eight cache lines each (tile of
-        // 128 tokens, 128 features: 800 clocks to issue).  Token n lies in slot 64 (n / 64) + 8 (n % 8) + n / 8 % 8, so that the readers' banks differ.
-        auto raw_slot = [&](int j, int slot) { return tc::smem_u32(sRaw) + (j & 1) * RAW_BYTES + slot * RAW; };
-        auto own_slot = [&](int j, int e) { const int n = n0 + e * (KT / KEYS); return raw_slot(j, (n & ~63) + (n & 7) * 8 + ((n >> 3) & 7)); };
-        auto fetch_v = [&](int j) {
-#pragma unroll
-            for (int e = 0; e < KEYS; ++e) {
-                const long long t = token(tile_start(j) + n0 + e * (KT / KEYS));
-                copy16(own_slot(j, e) + kt * 16, v_codes + t * code_pitch);
-                vs_next[e] = v_scales[t * scale_pitch];
-            }
-            copies_commit();
-        };
-        auto free_phase = [](int j) { return ((uint32_t)(j / kStages) & 1u) ^ 1u; };
         auto decode_k = [&](int j) {
             const int s = j % kStages;
             // lanes of the second half of the features take their words in another order, so that a warp's stores spread over the banks
@@ -213,41 +225,56 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
             tc::mbar_arrive(bar_kfull + 8 * s);
             return true;
         };
-        auto share_v = [&](int j) {                         // all decoders, also after a wait that gave up: they meet here
+        // Values come as whole blocks too: a thread's own words of eight tokens would be sixteen loads of eight cache lines each (tile of
+        // 128 tokens, 128 features: 800 clocks to issue).  Token i of eight ct lies in place 8 i + ct, so that readers' and writers'
+        // banks differ.
+        constexpr int HALVES = kDecoders / (16 * WORDS);                 // threads of a piece, each with 8 or 4 of the word's features
+        const int ct = lane & 7, u = tid / 8, kb = u / (WORDS * HALVES), w0 = u % (WORDS * HALVES) / HALVES, part = u % HALVES;
+        uint32_t vs_next[KEYS];
+        auto raw = [&](int j, int half, int c, int i) { return tc::smem_u32(sRaw) + (j & 1) * RAW_BYTES + (half * 8 + i) * RAW8 + c * RAW; };
+        auto own = [&](int j, int e) { const int n = n0 + e * (KT / KEYS); return raw(j, n / 64, n / 8 % 8, n % 8); };
+        auto fetch_v = [&](int j) {
+#pragma unroll
+            for (int e = 0; e < KEYS; ++e) {
+                const long long block = block0 + (long long)token(tile_start(j) + n0 + e * (KT / KEYS)) * block_pitch;
+                copy16(own(j, e) + kt * 16, a.v_codes + block * 16);
+                vs_next[e] = load1(a.v_scales + block);
+            }
+            copies_commit();
+        };
+        auto share_v = [&](int j) {
             copies_wait();
 #pragma unroll
-            for (int e = 0; e < KEYS; ++e) asm volatile("st.shared.u8 [%0], %1;" ::"r"(own_slot(j, e) + DH / 2 + kt), "r"(vs_next[e]) : "memory");
+            for (int e = 0; e < KEYS; ++e)              // a NaN block counts as zeros: it must not reach the rows that do not see its token
+                s_factor[j & 1][kt][n0 + e * (KT / KEYS)] = (uint16_t)(vs_next[e] > mx4::kCacheHi ? 0u : (vs_next[e] + 62) << 7);
             __syncwarp();
-            asm volatile("barrier.sync 1, %0;" ::"n"(kDecoders) : "memory");
-            if (j + 1 < n_tiles) fetch_v(j + 1);            // (its place was read before tile j was shared)
+            asm volatile("barrier.sync 1, %0;" ::"n"(kDecoders) : "memory");      // (also after a wait that gave up: the others come here)
+            if (j + 1 < n_tiles) fetch_v(j + 1);        // (its place was read before tile j was shared)
         };
         auto decode_v = [&](int j) {
             const int s = j % kStages;
-            uint32_t vc[8], vs[8];
+            const uint4 factors = *reinterpret_cast<const uint4 *>(&s_factor[j & 1][w0 / 4][kb * 64 + ct * 8]);
+            const uint32_t f[4] = {factors.x, factors.y, factors.z, factors.w};
+            uint32_t vc[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t at = raw_slot(j, kb * 64 + i * 8 + ct);
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(vc[i]) : "r"(at + w0 * 4) : "memory");
-                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(vs[i]) : "r"(at + DH / 2 + w0 / 4) : "memory");
-            }
-            uint32_t f[4], bad = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                // a NaN block counts as zeros here: it must not reach the rows that do not see its token
-                const bool bad0 = vs[2 * i] > mx4::kCacheHi, bad1 = vs[2 * i + 1] > mx4::kCacheHi;
-                bad |= (bad0 ? 1u : 0u) << (2 * i) | (bad1 ? 2u : 0u) << (2 * i);
-                f[i] = (bad0 ? 0u : (vs[2 * i] + 62) << 7) | (bad1 ? 0u : (vs[2 * i + 1] + 62) << 23);
-            }
+            for (int i = 0; i < 8; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(vc[i]) : "r"(raw(j, kb, ct, i) + w0 * 4) : "memory");
             if (!tc::mbar_wait(bar_vempty + 8 * s, free_phase(j), &s_abort)) return false;
-            if (w0 % 4 == 0 && part == 0) s_bad[j & 3][w0 / 4][kb * 8 + ct] = (uint8_t)bad;
-            if (bad) s_any_bad = 1;
+            if (w0 % 4 == 0 && part == 0) {
+                uint32_t bad = 0;
+                if (((f[0] - 0x00010001u) | (f[1] - 0x00010001u) | (f[2] - 0x00010001u) | (f[3] - 0x00010001u)) & 0x80008000u) {      // some factor is 0
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) bad |= ((f[i / 2] >> (i & 1) * 16) & 0xFFFFu) == 0u ? 1u << i : 0u;
+                    if (bad) s_any_bad = 1;
+                }
+                s_bad[j & 3][w0 / 4][kb * 8 + ct] = (uint8_t)bad;
+            }
             const uint32_t sv = tc::smem_u32(sV) + s * V_BYTES + kb * (DH * 128) + w0 * 8 * 128;
             uint32_t x[4];
             auto feature = [&](auto J, int d) {
                 store_chunk(sv + d * 128 + ((ct ^ d) * 16), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[0]), f[0]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[1]), f[1]),
                             mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[2]), f[2]), mul_bf16x2(codes_as_bf16<decltype(J)::value>(x[3]), f[3]));
             };
-            auto four = [&](int h) {                        // features 4 h to 4 h + 3 of the word
+            auto four = [&](int h) {                    // features 4 h to 4 h + 3 of the word
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = __byte_perm(vc[2 * i], vc[2 * i + 1], h ? 0x7632 : 0x5410);
                 feature(std::integral_constant<int, 0>(), 4 * h); feature(std::integral_constant<int, 1>(), 4 * h + 1);
@@ -258,17 +285,27 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
             tc::mbar_arrive(bar_vfull + 8 * s);
             return true;
         };
-        if (n_tiles > 0) fetch_k(0);
-        // Streams over odd and even tiles: keys one tile ahead of values, for the other stream's first scores (128 rows over 1536 tokens, 32
-        // heads: 17.3 us without, 16.7 with; row tiles that share a tile want its values sooner, 105 us instead of 102 for 2048 x 2048).
-        bool ok = true;
-        for (int j = PAIR ? 0 : -1; j < n_tiles; ++j) {
-            const int jk = PAIR ? j : j + 1;
-            if (jk < n_tiles && ok) ok = decode_k(jk);
-            if (jk == 0 && n_tiles > 0) fetch_v(0);         // (not sooner: the first keys and the queries come first)
-            if (j >= 0) {
+        if (R::kApart && warp < kDecoders / 32) {
+            if (n_tiles > 0) fetch_k(0);
+            for (int j = 0; j < n_tiles && ok; ++j) ok = decode_k(j);
+        } else if (R::kApart) {
+            if (n_tiles > 0) fetch_v(0);
+            for (int j = 0; j < n_tiles; ++j) {
                 share_v(j);
                 ok = ok && decode_v(j);
+            }
+        } else {
+            if (n_tiles > 0) fetch_k(0);
+            // Streams over odd and even tiles: keys one tile ahead of values, for the other stream's first scores (128 rows over 1536 tokens,
+            // 32 heads: 17.3 us without, 16.7 with); row tiles that share a tile want its values sooner.
+            for (int j = PAIR ? 0 : -1; j < n_tiles; ++j) {
+                const int jk = PAIR ? j : j + 1;
+                if (jk < n_tiles && ok) ok = decode_k(jk);
+                if (jk == 0 && n_tiles > 0) fetch_v(0);     // (not sooner: the first keys and the queries come first)
+                if (j >= 0) {
+                    share_v(j);
+                    ok = ok && decode_v(j);
+                }
             }
         }
         __syncwarp();
@@ -320,12 +357,12 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
         __syncwarp();
     } else {
         // ---------------- online softmax, one thread per row, against a reference maximum that follows the true one lazily
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        const int w = (warp - 8) >> 2, row = (warp & 3) * 32 + lane;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R::kSoftmaxRegs));
+        const int w = (warp - kSoftmaxWarp) >> 2, row = (warp & 3) * 32 + lane;
         {
             // queries, in the features' order of a decoded word: (0, 4), (1, 5), (2, 6), (3, 7); neighbouring lanes have a row's words
             constexpr int ROWS_AT_ONCE = 2 * QT / WORDS, BATCH = ROWS / ROWS_AT_ONCE;      // all of a thread's loads in flight
-            const int wd = (threadIdx.x - kDecoders) % WORDS, first_row = (threadIdx.x - kDecoders) / WORDS;
+            const int wd = (threadIdx.x - kSoftmaxWarp * 32) % WORDS, first_row = (threadIdx.x - kSoftmaxWarp * 32) / WORDS;
             uint4 v[BATCH];
 #pragma unroll
             for (int k = 0; k < BATCH; ++k) {
@@ -530,7 +567,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
     }
     if (!PAIR && splits > 1) {
         // ---------------- join the ranks: each writes its share of the rows
-        if (warp < 8 || warp == kMmaWarp) tc::cluster_sync();                   // (the softmax warps have passed theirs)
+        if (warp < kSoftmaxWarp || warp == kMmaWarp) tc::cluster_sync();                   // (the softmax warps have passed theirs)
         tc::cluster_sync();
         if (!s_abort) {
             for (int x = threadIdx.x; x < share * (DH / 4); x += kThreads) {
@@ -565,48 +602,46 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
 template <int DH, bool PAIR>
 int32_t launch(const Cache4Args &a, int log_splits, cudaStream_t stream)
 {
+    using R = Roles<DH, PAIR>;
     constexpr int NQ = PAIR ? 2 : 1;
-    constexpr size_t shared = 1024 + (size_t)NQ * QT * DH * 2 + (size_t)kStages * 2 * KT * DH * 2 + 2 * (size_t)KT * (DH / 2 + 16) + kBars * 8 + 16;
+    constexpr size_t shared = 1024 + (size_t)NQ * QT * DH * 2 + (size_t)kStages * 2 * KT * DH * 2 + 2 * (size_t)(KT / 8) * (8 * (DH / 2 + 16) + DH / 2) + kBars * 8 + 16;
     const long long row_tiles = ((long long)a.n_q * a.group + NQ * QT - 1) / (NQ * QT), ctas = ((long long)a.batch * a.n_kv * row_tiles) << log_splits;
     SFS_REQUIRE(ctas <= 0x7FFFFFFF, SFS_ERR_UNSUPPORTED, "attention_cache4: too many rows and heads for one call");
     SFS_CUDA(allow_shared(attention_cache4_many_kernel<DH, PAIR>, shared));
     // the softmax warps wait for registers that the launch must have brought: without them the kernel would not end
     cudaFuncAttributes attr;
     SFS_CUDA(cudaFuncGetAttributes(&attr, attention_cache4_many_kernel<DH, PAIR>));
-    SFS_REQUIRE(attr.numRegs >= kRegs, SFS_ERR_UNSUPPORTED, "attention_cache4: built with %d registers a thread, %d needed", attr.numRegs, kRegs);
-    if (log_splits > 0) SFS_CUDA(launch_pdl_cluster(attention_cache4_many_kernel<DH, PAIR>, 1 << log_splits, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, log_splits, (int)row_tiles));
-    else SFS_CUDA(launch_pdl(attention_cache4_many_kernel<DH, PAIR>, dim3((unsigned)ctas), dim3(kThreads), shared, stream, a, 0, (int)row_tiles));
+    SFS_REQUIRE(attr.numRegs >= R::kRegs, SFS_ERR_UNSUPPORTED, "attention_cache4: built with %d registers a thread, %d needed", attr.numRegs, R::kRegs);
+    if (log_splits > 0) SFS_CUDA(launch_pdl_cluster(attention_cache4_many_kernel<DH, PAIR>, 1 << log_splits, dim3((unsigned)ctas), dim3(R::kThreads), shared, stream, a, log_splits, (int)row_tiles));
+    else SFS_CUDA(launch_pdl(attention_cache4_many_kernel<DH, PAIR>, dim3((unsigned)ctas), dim3(R::kThreads), shared, stream, a, 0, (int)row_tiles));
     return SFS_OK;
 }
 
-// Pairs of row tiles where they fill the machine; else up to one wave of CTAs, two key tiles for each.  Clusters do not cover every SM, since
-// they do not cross the GPU's partitions: 128 CTAs in clusters of four run at once, in clusters of eight they do not (128 rows over 1536
-// tokens, 16 heads: 14.6 us with four, 25.4 with eight).
-struct Many { bool pair; int log_splits; long long ctas, key_tiles; };
-Many plan(const Cache4Args &a, int64_t tokens)
+// Row tiles in pairs, or alone: up to one wave of CTAs then, two key tiles for each.  Clusters do not cover every SM, since they do not
+// cross the GPU's partitions: 128 CTAs in clusters of four run at once, in clusters of eight they do not (128 rows over 1536 tokens, 16
+// heads: 14.6 us with four, 25.4 with eight).
+// Microseconds: 7.5 for a CTA's start and end, 3.5 for a join, and for a key tile 1.95 of 128 features or 1.35 of 64 (72 rows over 5344
+// tokens, 4 x 32 heads: 88 and 62), 2.55 and 2.0 for a pair's (2048 rows over 2048, 32 heads: 97; over 8192, 2 x 32 heads of 64: 519).
+// So 544 rows over 1692 tokens of 32 heads go in 96 pairs, 48.2 us, and not in two rounds of 160 CTAs, 62.6.
+struct Many { bool pair; int log_splits; double us; };
+Many plan(const Cache4Args &a, int64_t tokens, int head_dim)
 {
     const long long row_tiles = ((long long)a.n_q * a.group + QT - 1) / QT, heads = (long long)a.batch * a.n_kv, sms = gemm_num_sms();
-    Many p = {row_tiles > 1 && heads * ((row_tiles + 1) / 2) >= sms, 0, 0, 0};
-    if (!p.pair)
-        while (p.log_splits < 3 && (heads * row_tiles << (p.log_splits + 1)) <= (p.log_splits == 2 ? sms / 2 : sms * 7 / 8) && tokens > (2 * KT) << p.log_splits) ++p.log_splits;
-    p.ctas = heads * (p.pair ? (row_tiles + 1) / 2 : row_tiles) << p.log_splits;
-    const long long tiles = (tokens + KT - 1) / KT;
-    p.key_tiles = (tiles + (1 << p.log_splits) - 1) >> p.log_splits;
-    return p;
+    const long long tiles = (tokens + KT - 1) / KT, pairs = heads * ((row_tiles + 1) / 2), singles = heads * row_tiles;
+    int log_splits = 0;
+    while (log_splits < 3 && (singles << (log_splits + 1)) <= (log_splits == 2 ? sms / 2 : sms * 7 / 8) && tokens > (2 * KT) << log_splits) ++log_splits;
+    const Many one = {false, log_splits, (double)(((singles << log_splits) + sms - 1) / sms) * (7.5 + (head_dim == 128 ? 1.95 : 1.35) * (double)((tiles + (1 << log_splits) - 1) >> log_splits)) + (log_splits > 0 ? 3.5 : 0.0)};
+    const Many two = {true, 0, (double)((pairs + sms - 1) / sms) * (7.5 + (head_dim == 128 ? 2.55 : 2.0) * (double)tiles)};
+    return row_tiles > 1 && two.us < one.us ? two : one;
 }
 
 }  // namespace
 
-double attention_cache4_many_us(const Cache4Args &a, int64_t tokens)
-{
-    const Many p = plan(a, tokens);
-    const long long rounds = (p.ctas + gemm_num_sms() - 1) / gemm_num_sms();
-    return rounds * (7.5 + (p.pair ? 3.1 : 2.4) * p.key_tiles) + (p.log_splits > 0 ? 3.5 : 0.0);
-}
+double attention_cache4_many_us(const Cache4Args &a, int64_t tokens, int head_dim) { return plan(a, tokens, head_dim).us; }
 
 int32_t attention_cache4_many(const Cache4Args &a, int64_t tokens, int head_dim, cudaStream_t stream)
 {
-    const Many p = plan(a, tokens);
+    const Many p = plan(a, tokens, head_dim);
     if (p.pair) return head_dim == 128 ? launch<128, true>(a, 0, stream) : launch<64, true>(a, 0, stream);
     return head_dim == 128 ? launch<128, false>(a, p.log_splits, stream) : launch<64, false>(a, p.log_splits, stream);
 }
