@@ -14,8 +14,8 @@
 // Bound, where row tiles share what is decoded: the softmax warps' chain (scores, maximum, exponentials, hand-over: 3300 clocks of a tile,
 // which the decoding warps stretch by sharing the pipes) with the MMAs behind it (1300), about 5000 clocks for a tile of both streams.
 // Alone, the decoders: 3300 clocks of a tile, 16 instructions for a word of 8 codes; issue 57 % busy, shared memory 36 %, tensor pipe 21 %.
-// Measured, 32 heads of 128, us: 2048 rows over 2048 tokens 97 (attention_kernel on bf16 values 73), 72 rows over 4 x 5344 88, 128 rows
-// over 1536 15.2.  Scores of the next tile's second half issued while this one's is in its softmax: 118 instead of 97, MMAs of 64 keys
+// Measured, 32 heads of 128, us: 2048 rows over 2048 tokens 94 (attention_kernel on bf16 values 73), 72 rows over 4 x 5344 87, 128 rows
+// over 1536 13.9.  Scores of the next tile's second half issued while this one's is in its softmax: 118 instead of 97, MMAs of 64 keys
 // read the queries twice as often.
 //
 // Only key tiles that some row sees are visited.  With few CTAs the tiles are divided over a cluster of up to 8, whose partial outputs
@@ -55,7 +55,7 @@ __device__ __forceinline__ void store_chunk(uint32_t smem, uint32_t x, uint32_t 
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
-__device__ __forceinline__ void copy16(uint32_t smem, const void *global) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory"); }
+__device__ __forceinline__ void copy16(uint32_t smem, const void *global, int bytes = 16) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(global), "r"(bytes) : "memory"); }
 // Loads that keep out of the first-level cache: next to this much shared memory it has 28 KB, in lines of 128 bytes, of which a token's
 // codes and scales would each take one for as long as they are under way.
 __device__ __forceinline__ uint4 load16(const uint8_t *p)
@@ -151,6 +151,19 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
 
     pdl_wait();
     pdl_trigger();
+    // The softmax warps send the queries on their way before anything else is known (256 rows in a window, 8 x 32 heads: 46.2 us without, 42.1
+    // with); neighbouring lanes have a row's words.
+    constexpr int ROWS_AT_ONCE = 2 * QT / WORDS, BATCH = ROWS / ROWS_AT_ONCE;
+    const int q_word = threadIdx.x % WORDS, q_row = (threadIdx.x - kSoftmaxWarp * 32) / WORDS;
+    auto q_place = [&](int rq) { return tc::smem_u32(sQ) + rq / QT * Q_BYTES + (q_word / 8) * (QT * 128) + rq % QT * 128 + (((q_word % 8) ^ (rq & 7)) * 16); };
+    if (warp >= kSoftmaxWarp && warp < kMmaWarp) {
+#pragma unroll 4
+        for (int k = 0; k < BATCH; ++k) {
+            const int rq = q_row + k * ROWS_AT_ONCE, r = min(row0 + rq, a.n_q * a.group - 1), i = a.group == 1 ? r : r / a.group;
+            copy16(q_place(rq), a.q + ((long long)b * a.n_q + i) * a.ld_q + (long long)(kv * a.group + r - i * a.group) * DH + q_word * 8, rq < n_rows ? 16 : 0);
+        }
+        copies_commit();
+    }
     if (warp < ROWS / 32) {
         const int r = threadIdx.x;
         Seen s = {0, 0, 0};
@@ -364,20 +377,14 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R::kSoftmaxRegs));
         const int w = (warp - kSoftmaxWarp) >> 2, row = (warp & 3) * 32 + lane;
         {
-            // queries, in the features' order of a decoded word: (0, 4), (1, 5), (2, 6), (3, 7); neighbouring lanes have a row's words
-            constexpr int ROWS_AT_ONCE = 2 * QT / WORDS, BATCH = ROWS / ROWS_AT_ONCE;      // all of a thread's loads in flight
-            const int wd = (threadIdx.x - kSoftmaxWarp * 32) % WORDS, first_row = (threadIdx.x - kSoftmaxWarp * 32) / WORDS;
-            uint4 v[BATCH];
-#pragma unroll
+            // in the features' order of a decoded word: (0, 4), (1, 5), (2, 6), (3, 7)
+            copies_wait();
+#pragma unroll 4
             for (int k = 0; k < BATCH; ++k) {
-                const int rq = first_row + k * ROWS_AT_ONCE;
-                v[k] = rq < n_rows ? *reinterpret_cast<const uint4 *>(a.q + row_of(rq, a.ld_q) + wd * 8) : make_uint4(0, 0, 0, 0);
-            }
-#pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                const int rq = first_row + k * ROWS_AT_ONCE, tile = rq / QT, rr = rq % QT;
-                store_chunk(tc::smem_u32(sQ) + tile * Q_BYTES + (wd / 8) * (QT * 128) + rr * 128 + (((wd % 8) ^ (rr & 7)) * 16),
-                            __byte_perm(v[k].x, v[k].z, 0x5410), __byte_perm(v[k].x, v[k].z, 0x7632), __byte_perm(v[k].y, v[k].w, 0x5410), __byte_perm(v[k].y, v[k].w, 0x7632));
+                const uint32_t at = q_place(q_row + k * ROWS_AT_ONCE);
+                uint4 v;
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+                store_chunk(at, __byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
             }
             fence_async_shared();
             tc::mbar_arrive(bar_q);
