@@ -631,9 +631,9 @@ int32_t launch(const Cache4Args &a, int log_splits, cudaStream_t stream)
 // Row tiles in pairs, or alone: up to one wave of CTAs then, two key tiles for each.  Clusters do not cover every SM, since they do not
 // cross the GPU's partitions: 128 CTAs in clusters of four run at once, in clusters of eight they do not (128 rows over 1536 tokens, 16
 // heads: 14.6 us with four, 25.4 with eight).
-// Microseconds: 7.5 for a CTA's start and end, 3.5 for a join, and for a key tile 1.95 of 128 features or 1.35 of 64 (72 rows over 5344
-// tokens, 4 x 32 heads: 88 and 62), 2.55 and 2.0 for a pair's (2048 rows over 2048, 32 heads: 97; over 8192, 2 x 32 heads of 64: 519).
-// So 544 rows over 1692 tokens of 32 heads go in 96 pairs, 48.2 us, and not in two rounds of 160 CTAs, 62.6.
+// Microseconds: 5.5 for a CTA's start and end, 2.5 for a join, and for a key tile 1.95 of 128 features or 1.35 of 64 (72 rows over 5344
+// tokens, 4 x 32 heads: 87 and 61), 2.55 and 2.0 for a pair's (2048 rows over 2048, 32 heads: 94; over 8192, 2 x 32 heads of 64: 523).
+// So 544 rows over 1692 tokens of 32 heads go in 96 pairs, 46 us, and not in two rounds of 160 CTAs, 62.6 when pairs took 48.
 struct Many { bool pair; int log_splits; double us; };
 Many plan(const Cache4Args &a, int64_t tokens, int head_dim)
 {
@@ -641,8 +641,8 @@ Many plan(const Cache4Args &a, int64_t tokens, int head_dim)
     const long long tiles = (tokens + KT - 1) / KT, pairs = heads * ((row_tiles + 1) / 2), singles = heads * row_tiles;
     int log_splits = 0;
     while (log_splits < 3 && (singles << (log_splits + 1)) <= (log_splits == 2 ? sms / 2 : sms * 7 / 8) && tokens > (2 * KT) << log_splits) ++log_splits;
-    const Many one = {false, log_splits, (double)(((singles << log_splits) + sms - 1) / sms) * (7.5 + (head_dim == 128 ? 1.95 : 1.35) * (double)((tiles + (1 << log_splits) - 1) >> log_splits)) + (log_splits > 0 ? 3.5 : 0.0)};
-    const Many two = {true, 0, (double)((pairs + sms - 1) / sms) * (7.5 + (head_dim == 128 ? 2.55 : 2.0) * (double)tiles)};
+    const Many one = {false, log_splits, (double)(((singles << log_splits) + sms - 1) / sms) * (5.5 + (head_dim == 128 ? 1.95 : 1.35) * (double)((tiles + (1 << log_splits) - 1) >> log_splits)) + (log_splits > 0 ? 2.5 : 0.0)};
+    const Many two = {true, 0, (double)((pairs + sms - 1) / sms) * (5.5 + (head_dim == 128 ? 2.55 : 2.0) * (double)tiles)};
     return row_tiles > 1 && two.us < one.us ? two : one;
 }
 
