@@ -4,7 +4,7 @@
 // magnitude is the maximum of the bit patterns over 4 lanes, so a NaN or an infinity shows in it, and each value is scaled by a power of
 // two (exact) and rounded once, by the conversion instruction.  A warp works on 1024 neighbouring columns, so that addresses are computed
 // once for four loads in flight: with one piece at a time, found anew, the instructions and not the memory set the pace (126464 x 4096 to
-// codes and back: 624 us, 490 so; 2.6 GB move, 5.35 TB/s of a measured copy rate of 6.57).
+// codes and back: 624 us, 485 so; 2.6 GB move, 5.4 TB/s of a measured copy rate of 6.57).
 #include "attention_cache4.cuh"
 #include "gemm.cuh"
 #include <algorithm>
@@ -241,20 +241,20 @@ struct Walk {
 };
 __device__ __forceinline__ Walk warps_of_grid(int segs) { return Walk(blockIdx.x * kWarps + threadIdx.x / 32, gridDim.x * kWarps, segs); }
 
-template <typename T, int U>
+template <typename T, int U, bool WIDE>
 __global__ void __launch_bounds__(kThreads)
 quantize_kernel(const T *__restrict__ x, long long ldx, int rows, int cols, uint8_t *__restrict__ codes, long long ld_codes,
-                uint8_t *__restrict__ scales, int quads, int wide)
+                uint8_t *__restrict__ scales, int quads)
 {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, half = lane >> 4, l = lane & 15, tile_rows = (rows + 127) / 128 * 128, blocks = (cols + 31) / 32;
     for (Walk at = warps_of_grid((quads + 2 * U - 1) / (2 * U)); at.row < tile_rows; at.next()) {
         const int quad0 = at.seg * 2 * U + half, col0 = quad0 * 128 + l * 8;
-        const bool in = at.row < rows, full = in && wide && (at.seg + 1) * 2 * U * 128 <= cols;
+        const bool in = at.row < rows, full = in && WIDE && (at.seg + 1) * 2 * U * 128 <= cols;
         const T *src = x + at.row * ldx + col0;
         Eight<T> v[U];
-        if (!in || wide) {
+        if (WIDE || !in) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int left = cols - col0 - u * 256;
@@ -276,10 +276,10 @@ quantize_kernel(const T *__restrict__ x, long long ldx, int rows, int cols, uint
     }
 }
 
-template <typename T, int U>
+template <typename T, int U, bool WIDE>
 __global__ void __launch_bounds__(kThreads)
 dequantize_kernel(const uint8_t *__restrict__ codes, long long ld_codes, const uint8_t *__restrict__ scales, int rows, int cols, T *__restrict__ x,
-                  long long ldx, int quads, int wide)
+                  long long ldx, int quads)
 {
     pdl_wait();
     pdl_trigger();
@@ -294,7 +294,7 @@ dequantize_kernel(const uint8_t *__restrict__ codes, long long ld_codes, const u
             if (col0 + u * 256 < cols) { w[u] = __ldcs(reinterpret_cast<const uint32_t *>(from + u * 128)); c[u] = s[u * 1024]; }
         }
         T *to = x + at.row * ldx + col0;
-        if (wide) {
+        if (WIDE) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int left = cols - col0 - u * 256;
@@ -474,21 +474,22 @@ cache_load_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restrict
     }
 }
 
-// Pieces of a lane in a segment (2 U quads), one to four loads in flight: the longest segment that leaves at most an eighth of a row's
-// lanes without work, else the one that leaves the fewest. 81713 x 597 16-bit values, 5 quads: 111 us at one piece, 137 at four;
-// 39518 x 3382, 27 quads: 241 us at two, 260 at four.
-int pieces(int quads)
+// Pieces of a lane in a segment (2 U quads), one to four loads in flight: the longest segment that leaves at most a third of a row's lanes
+// without work (40000 x 1280 fp32, 10 quads, to codes and back: 77 us at one piece, 63 at three; 40000 x 2688 bf16, 21 quads: 130 and 105 at
+// four), an eighth where lanes shift their values together, which costs more than a load does (39518 x 3382, 27 quads: 233 us at three, 263 at
+// four); else the one that leaves the fewest.
+int pieces(int quads, bool wide)
 {
     int best = 1, waste = 1 << 30;
     for (int u = 1; u <= 4; ++u) {
         const int w = (quads + 2 * u - 1) / (2 * u) * (2 * u) - quads;
-        if (w * 8 <= quads || w <= waste) { waste = w; best = u; }
+        if (w * (wide ? 3 : 8) <= quads || w <= waste) { waste = w; best = u; }
     }
     return best;
 }
-int segments(int quads) { const int u = pieces(quads); return (quads + 2 * u - 1) / (2 * u); }
-// the instance of a kernel template <T, U> for rows of that many quads
-#define SFS_BY_PIECES(kernel, quads) (pieces(quads) == 4 ? kernel<T, 4> : pieces(quads) == 3 ? kernel<T, 3> : pieces(quads) == 2 ? kernel<T, 2> : kernel<T, 1>)
+int segments(int quads, bool wide) { const int u = pieces(quads, wide); return (quads + 2 * u - 1) / (2 * u); }
+// the instance of a kernel template <T, U, ...> for so many pieces
+#define SFS_BY_PIECES(kernel, u, ...) (u == 4 ? kernel<T, 4, ##__VA_ARGS__> : u == 3 ? kernel<T, 3, ##__VA_ARGS__> : u == 2 ? kernel<T, 2, ##__VA_ARGS__> : kernel<T, 1, ##__VA_ARGS__>)
 bool wide_rows(const void *base, int64_t ld, size_t element) { return aligned_to(base, 16) && (ld * (int64_t)element) % 16 == 0; }
 // CTAs for that many warps' segments: eight on an SM at most
 unsigned grid_for(long long segs) { return (unsigned)std::max<long long>(1, std::min<long long>((segs + kWarps - 1) / kWarps, (long long)gemm_num_sms() * 8)); }
@@ -506,9 +507,11 @@ cudaError_t launch_quantize(const void *x, int64_t ldx, int rows, int cols, void
         return launch_pdl(kernel, grid, dim3(kThreads), 0, stream, (const T *)x, (long long)ldx, rows, cols, (uint8_t *)codes, (long long)ld_codes, (uint8_t *)scales,
                           (int)wide_rows(x, ldx, sizeof(T)));
     }
-    const dim3 grid(grid_for((long long)((rows + 127) / 128 * 128) * segments(quads)));
-    return launch_pdl(SFS_BY_PIECES(quantize_kernel, quads), grid, dim3(kThreads), 0, stream, (const T *)x, (long long)ldx, rows, cols,
-                      (uint8_t *)codes, (long long)ld_codes, (uint8_t *)scales, quads, (int)wide_rows(x, ldx, sizeof(T)));
+    const bool wide = wide_rows(x, ldx, sizeof(T));
+    const int u = pieces(quads, wide);
+    const dim3 grid(grid_for((long long)((rows + 127) / 128 * 128) * segments(quads, wide)));
+    return launch_pdl(wide ? SFS_BY_PIECES(quantize_kernel, u, true) : SFS_BY_PIECES(quantize_kernel, u, false), grid, dim3(kThreads), 0, stream, (const T *)x, (long long)ldx, rows, cols,
+                      (uint8_t *)codes, (long long)ld_codes, (uint8_t *)scales, quads);
 }
 template <typename T>
 cudaError_t launch_dequantize(const void *codes, int64_t ld_codes, const void *scales, int rows, int cols, void *x, int64_t ldx, cudaStream_t stream)
@@ -521,9 +524,11 @@ cudaError_t launch_dequantize(const void *codes, int64_t ld_codes, const void *s
         return launch_pdl(kernel, grid, dim3(kThreads), 0, stream, (const uint8_t *)codes, (long long)ld_codes, (const uint8_t *)scales, rows, cols, (T *)x, (long long)ldx,
                           (int)wide_rows(x, ldx, sizeof(T)));
     }
-    const dim3 grid(grid_for((long long)rows * segments(quads)));
-    return launch_pdl(SFS_BY_PIECES(dequantize_kernel, quads), grid, dim3(kThreads), 0, stream, (const uint8_t *)codes,
-                      (long long)ld_codes, (const uint8_t *)scales, rows, cols, (T *)x, (long long)ldx, quads, (int)wide_rows(x, ldx, sizeof(T)));
+    const bool wide = wide_rows(x, ldx, sizeof(T));
+    const int u = pieces(quads, wide);
+    const dim3 grid(grid_for((long long)rows * segments(quads, wide)));
+    return launch_pdl(wide ? SFS_BY_PIECES(dequantize_kernel, u, true) : SFS_BY_PIECES(dequantize_kernel, u, false), grid, dim3(kThreads), 0, stream, (const uint8_t *)codes,
+                      (long long)ld_codes, (const uint8_t *)scales, rows, cols, (T *)x, (long long)ldx, quads);
 }
 template <typename T>
 cudaError_t launch_store(const sfs_cache4 &c, const void *k, int64_t ld_k, const void *v, int64_t ld_v, const int32_t *slots, int n_rows, cudaStream_t stream)
@@ -532,7 +537,8 @@ cudaError_t launch_store(const sfs_cache4 &c, const void *k, int64_t ld_k, const
     // few rows: one or two for a CTA, so that they spread over the machine
     const int cta_rows = std::min(kStoreRows, std::max(1, n_rows / gemm_num_sms()));
     const dim3 grid((unsigned)((n_rows + cta_rows - 1) / cta_rows), 2);
-    return launch_pdl(SFS_BY_PIECES(cache_store_kernel, quads), grid, dim3(kThreads), 0, stream, (uint8_t *)c.k_codes,
+    const int u = pieces(quads, true);
+    return launch_pdl(SFS_BY_PIECES(cache_store_kernel, u), grid, dim3(kThreads), 0, stream, (uint8_t *)c.k_codes,
                       (uint8_t *)c.k_scales, (uint8_t *)c.v_codes, (uint8_t *)c.v_scales, c.batch * c.capacity, width, (const T *)k, (long long)ld_k,
                       (const T *)v, (long long)ld_v, (int)wide_rows(k, ld_k, sizeof(T)), (int)wide_rows(v, ld_v, sizeof(T)), slots, n_rows, cta_rows);
 }
@@ -540,8 +546,9 @@ template <typename T>
 cudaError_t launch_load(const sfs_cache4 &c, const int32_t *slots, int n_rows, void *k, int64_t ld_k, void *v, int64_t ld_v, cudaStream_t stream)
 {
     const int width = c.n_kv_heads * c.head_dim, quads = (width + 127) / 128;
-    const dim3 grid(grid_for((long long)n_rows * segments(quads)), 2);
-    return launch_pdl(SFS_BY_PIECES(cache_load_kernel, quads), grid, dim3(kThreads), 0, stream, (const uint8_t *)c.k_codes,
+    const int u = pieces(quads, true);
+    const dim3 grid(grid_for((long long)n_rows * segments(quads, true)), 2);
+    return launch_pdl(SFS_BY_PIECES(cache_load_kernel, u), grid, dim3(kThreads), 0, stream, (const uint8_t *)c.k_codes,
                       (const uint8_t *)c.k_scales, (const uint8_t *)c.v_codes, (const uint8_t *)c.v_scales, c.batch * c.capacity, width, (T *)k, (long long)ld_k,
                       (T *)v, (long long)ld_v, (int)wide_rows(k, ld_k, sizeof(T)), (int)wide_rows(v, ld_v, sizeof(T)), slots, n_rows);
 }
@@ -603,7 +610,7 @@ int32_t sfs_mx4_quantize(const void *d_x, int64_t ldx, int32_t in_dtype, int32_t
 {
     const int32_t rc = check_matrix("mx4_quantize", d_x, ldx, in_dtype, rows, cols, d_codes, ld_codes, d_scales);
     if (rc != SFS_OK) return rc;
-    SFS_REQUIRE((int64_t)rows * segments((cols + 127) / 128) < 0x7FFF0000, SFS_ERR_UNSUPPORTED, "mx4_quantize: matrix too large for one call");
+    SFS_REQUIRE((int64_t)rows * std::max(segments((cols + 127) / 128, false), segments((cols + 127) / 128, true)) < 0x7FFF0000, SFS_ERR_UNSUPPORTED, "mx4_quantize: matrix too large for one call");
     if (in_dtype == SFS_LOGITS_BF16) SFS_CUDA(launch_quantize<__nv_bfloat16>(d_x, ldx, rows, cols, d_codes, ld_codes, d_scales, (cudaStream_t)stream));
     else SFS_CUDA(launch_quantize<float>(d_x, ldx, rows, cols, d_codes, ld_codes, d_scales, (cudaStream_t)stream));
     return SFS_OK;
@@ -614,7 +621,7 @@ int32_t sfs_mx4_dequantize(const void *d_codes, int64_t ld_codes, const void *d_
 {
     const int32_t rc = check_matrix("mx4_dequantize", d_x, ldx, out_dtype, rows, cols, d_codes, ld_codes, d_scales);
     if (rc != SFS_OK) return rc;
-    SFS_REQUIRE((int64_t)rows * segments((cols + 127) / 128) < 0x7FFF0000, SFS_ERR_UNSUPPORTED, "mx4_dequantize: matrix too large for one call");
+    SFS_REQUIRE((int64_t)rows * std::max(segments((cols + 127) / 128, false), segments((cols + 127) / 128, true)) < 0x7FFF0000, SFS_ERR_UNSUPPORTED, "mx4_dequantize: matrix too large for one call");
     if (out_dtype == SFS_LOGITS_BF16) SFS_CUDA(launch_dequantize<__nv_bfloat16>(d_codes, ld_codes, d_scales, rows, cols, d_x, ldx, (cudaStream_t)stream));
     else SFS_CUDA(launch_dequantize<float>(d_codes, ld_codes, d_scales, rows, cols, d_x, ldx, (cudaStream_t)stream));
     return SFS_OK;
