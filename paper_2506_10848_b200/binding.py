@@ -237,20 +237,29 @@ class Cache4(Structure):
                     raise SfsError(ERR_INVALID_ARG, f"{name}: contiguous bytes for {batch} x {capacity} tokens of {n_kv_heads} heads needed")
         super().__init__(*_here(*parts), batch, capacity, n_kv_heads, head_dim)
         self._tensors = parts
+        self._device = next((t.get_device() for t in parts if t is not None and not isinstance(t, int)), None)
+
+    def _beside(self, *tensors):
+        """Addresses of a call's tensors, on the device of the cache's."""
+        if self._device is not None:
+            import torch
+            if torch.cuda.current_device() != self._device:
+                raise SfsError(ERR_INVALID_ARG, f"cache on cuda:{self._device}: this call takes tensors of the current CUDA device")
+        return _here(*tensors)
 
 
 def sfs_cache4_store(cache, k, ld_k, v, ld_v, in_dtype, slots, n_rows, stream=None):
-    k, v, slots = _here(k, v, slots)
+    k, v, slots = cache._beside(k, v, slots)
     _check(lib().sfs_cache4_store(byref(cache), k, ld_k, v, ld_v, in_dtype, slots, n_rows, _stream(stream)))
 
 
 def sfs_cache4_load(cache, slots, n_rows, k, ld_k, v, ld_v, out_dtype, stream=None):
-    k, v, slots = _here(k, v, slots)
+    k, v, slots = cache._beside(k, v, slots)
     _check(lib().sfs_cache4_load(byref(cache), slots, n_rows, k, ld_k, v, ld_v, out_dtype, _stream(stream)))
 
 
 def sfs_attention_cache4(cache, q, ld_q, out, ld_out, n_heads, n_q, lengths=None, positions=None, left=-1, right=-1, sinks=0, stream=None):
-    q, out, lengths, positions = _here(q, out, lengths, positions)
+    q, out, lengths, positions = cache._beside(q, out, lengths, positions)
     _check(lib().sfs_attention_cache4(byref(cache), q, ld_q, out, ld_out, n_heads, n_q, lengths, positions, left, right, sinks, _stream(stream)))
 
 

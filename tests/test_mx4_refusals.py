@@ -93,6 +93,36 @@ def test_tensors_of_the_host_are_refused():
             cache(k_codes=bad)
 
 
+class OnDevice:
+    """What the binding asks of a CUDA tensor."""
+    is_cuda = True
+
+    def __init__(self, index):
+        self.index, self.device = index, f"cuda:{index}"
+
+    def get_device(self): return self.index
+    def data_ptr(self): return A
+    def element_size(self): return 1
+    def is_contiguous(self): return True
+    def numel(self): return 1 << 20
+
+
+def test_cache_of_another_device(monkeypatch):
+    """A cache made on one device does not follow the program to another."""
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    parts = dict(zip(("k_codes", "k_scales", "v_codes", "v_scales"), (OnDevice(0),) * 4))
+    c, t = cache(**parts), OnDevice(0)
+    sfs.sfs_attention_cache4(c, t, 128, t, 128, 2, 0, stream=0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for here in (OnDevice(1), A):
+        refused(sfs.ERR_INVALID_ARG, sfs.sfs_attention_cache4, c, here, 128, here, 128, 2, 0)
+        refused(sfs.ERR_INVALID_ARG, sfs.sfs_cache4_store, c, here, 128, here, 128, 0, None, 0)
+        refused(sfs.ERR_INVALID_ARG, sfs.sfs_cache4_load, c, None, 0, here, 128, here, 128, 0)
+    with pytest.raises(sfs.SfsError):
+        cache(**{**parts, "v_scales": OnDevice(1)})
+
+
 def test_nothing_to_do_is_no_error():
     sfs.sfs_cache4_store(cache(), A, 128, A, 128, 0, None, 0, stream=0)
     sfs.sfs_cache4_load(cache(), None, 0, A, 128, A, 128, 0, stream=0)
