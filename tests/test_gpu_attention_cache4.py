@@ -152,6 +152,63 @@ def test_many_rows_beside_nan_and_infinite_values(batch, capacity, heads, kv, di
     c.check(lengths=lengths, left=200, right=0)
 
 
+# Two row tiles that share every decoded key tile, over more key tiles than the ring has places; the last pair with one tile, or a part of
+# its second.
+PAIRS = [(3, 700, 25, 25, 128, 200), (3, 450, 50, 25, 128, 101), (3, 650, 25, 25, 64, 190), (2, 400, 30, 30, 128, 300)]
+
+
+@pytest.mark.parametrize("batch,capacity,heads,kv,dim,n_q", PAIRS)
+def test_pairs_of_row_tiles(batch, capacity, heads, kv, dim, n_q):
+    c = Case(batch, capacity, heads, kv, dim, n_q, seed=capacity)
+    c.check()
+    c.check(lengths=[0, capacity, capacity // 3][:batch], ld_pad=8)
+    pos = c.rng.integers(0, capacity, size=(batch, n_q))
+    pos[:, 3], pos[0, -1], pos[-1, : n_q // 2] = -1, -1, capacity - 1
+    c.check(lengths=[capacity, capacity - 5, 129][:batch], positions=pos, left=100, right=30, sinks=5)
+    c.check(left=-1, right=0)
+
+
+@pytest.mark.parametrize("batch,capacity,heads,kv,dim,n_q", PAIRS)
+def test_pairs_of_row_tiles_beside_nan_and_infinite_values(batch, capacity, heads, kv, dim, n_q):
+    c = Case(batch, capacity, heads, kv, dim, n_q, seed=7)
+    v, k = (x.reshape(batch, capacity, kv, dim // 32) for x in (c.scales[1], c.scales[0]))
+    v[:, 40:44, 0, 1], v[:, capacity // 2, :, 0], v[0, capacity - 1] = 255, 200, 255
+    k[:, 90, 0], k[0, capacity - 1] = 255, 193
+    pos = c.rng.integers(0, capacity, size=(batch, n_q))
+    pos[:, :4] = 300 % capacity
+    c.check(positions=pos, left=20, right=20, sinks=2)
+    c.check(lengths=np.full(batch, capacity - 1), left=200, right=0)
+
+
+def test_the_same_bits_whatever_runs_beside():
+    """Row tiles in pairs, alone and over clusters: two streams at once, and a captured graph replayed, give what one call gives."""
+    for shape in (PAIRS[0], PAIRS[2], MANY[0], MANY[4], MANY[7]):
+        batch, capacity, heads, kv, dim, n_q = shape
+        c = Case(*shape, seed=11)
+        cache = sfs.Cache4(dev(R.pack(c.codes[0])), dev(c.scales[0]), dev(R.pack(c.codes[1])), dev(c.scales[1]), batch, capacity, kv, dim)
+        q, width = c.q.to(DEV), heads * dim
+        outs = [torch.zeros_like(q) for _ in range(4)]
+
+        def call(i): sfs.sfs_attention_cache4(cache, q, width, outs[i], width, heads, n_q)
+        call(0)
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        for _ in range(5):
+            for i, stream in enumerate(streams):
+                with torch.cuda.stream(stream):
+                    call(1 + i)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(3)
+        for _ in range(3):
+            graph.replay()
+        torch.cuda.synchronize()
+        sfs.sfs_check_device_status()
+        for out in outs[1:]:
+            assert torch.equal(out.view(torch.int16), outs[0].view(torch.int16))
+
+
 def test_many_rows_that_see_nothing():
     c = Case(8, 400, 8, 8, 128, 130, seed=1)
     pos = c.rng.integers(0, 400, size=(8, 130))
