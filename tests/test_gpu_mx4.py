@@ -60,6 +60,23 @@ def test_quantize_gives_the_formats_codes_and_scales(rows, cols, dtype):
         assert (scales[:-64].cpu().numpy() == R.tile_scales(want_scales)).all()       # the tiles' padding holds zeros
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("quads", [3, 4, 5, 6, 7, 8, 9, 10, 11, 13, 14, 17, 18, 21, 27])
+def test_rows_of_every_length_in_aligned_places(quads, dtype):
+    """Every length of a warp's segment, its last one full or in part, rows that end inside a vector."""
+    for cols in (quads * 128, quads * 128 - 37, quads * 128 - 96, quads * 128 - 127):
+        rows, ld, blocks = 70, quads * 128 + 16, (cols + 31) // 32
+        t, x = as_input(matrix(rows, cols, cols), dtype)
+        codes, scales = quantize_on_gpu(t, dtype, ld, 0, 16)
+        want_codes, want_scales = R.quantize(x, R.MATRIX)
+        assert (codes[:, :blocks * 16].cpu().numpy() == R.pack(want_codes)).all() and (codes[:, blocks * 16:] == GUARD).all()
+        assert (scales[:-64].cpu().numpy() == R.tile_scales(want_scales)).all() and (scales[-64:] == GUARD).all()
+        out = torch.full((rows, ld), 77.0, dtype=TYPES[dtype][0], device=DEV)
+        sfs.sfs_mx4_dequantize(codes, codes.stride(0), scales, rows, cols, out, ld, TYPES[dtype][1])
+        got = out.double().cpu().numpy()
+        assert np.array_equal(got[:, :cols], R.values(want_codes, want_scales)[:, :cols], equal_nan=True) and (got[:, cols:] == 77.0).all()
+
+
 def test_quantize_at_the_edges_of_the_numbers():
     x = np.zeros((12, 96))
     x[0, :8] = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0]         # half-way points under a scale of 1
@@ -325,6 +342,20 @@ def test_store_and_load(heads, dim, dtype):
     only = torch.full((n, width), 77.0, dtype=TYPES[dtype][0], device=DEV)
     sfs.sfs_cache4_load(c, dev(slots), n, None, 0, only, width, TYPES[dtype][1])    # values alone
     assert torch.equal(only.cpu(), out[:, 1, :width].cpu())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,dim", [(3, 128), (6, 128), (9, 128), (11, 64), (13, 64), (13, 128), (21, 128)])
+def test_store_and_load_of_many_heads(heads, dim, dtype):
+    n, width = 300, heads * dim
+    c = new_cache(1, n, heads, dim)
+    t, x = as_input(matrix(n, width, heads), dtype)
+    t = t.to(DEV)
+    sfs.sfs_cache4_store(c, t, width, t.flip(0).contiguous(), width, TYPES[dtype][1], None, n)
+    out = torch.full((2, n, width), 77.0, dtype=TYPES[dtype][0], device=DEV)
+    sfs.sfs_cache4_load(c, None, n, out[0], width, out[1], width, TYPES[dtype][1])
+    want = R.values(*R.quantize(x, R.CACHE))
+    assert np.array_equal(out[0].double().cpu().numpy(), want, equal_nan=True) and np.array_equal(out[1].double().cpu().numpy(), want[::-1], equal_nan=True)
 
 
 def test_of_rows_with_one_slot_the_last_counts():
