@@ -13,7 +13,7 @@
 //
 // Bound, where row tiles share what is decoded: the softmax warps' chain (scores, maximum, exponentials, hand-over: 3300 clocks of a tile,
 // which the decoding warps stretch by sharing the pipes) with the MMAs behind it (1300), about 5000 clocks for a tile of both streams.
-// Alone, the decoders: 3300 clocks of a tile, 16 instructions for a word of 8 codes; issue 57 % busy, shared memory 36 %, tensor pipe 21 %.
+// Alone, the decoders: 3300 clocks of a tile, 16 instructions for a word of 8 codes; issue 51 % busy, shared memory 39 %, tensor pipe 22 %.
 // Measured, 32 heads of 128, us: 2048 rows over 2048 tokens 94 (attention_kernel on bf16 values 73), 72 rows over 4 x 5344 87, 128 rows
 // over 1536 13.9.  Scores of the next tile's second half issued while this one's is in its softmax: 118 instead of 97, MMAs of 64 keys
 // read the queries twice as often.
