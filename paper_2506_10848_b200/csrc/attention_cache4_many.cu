@@ -496,6 +496,11 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
         if (n_mine > 0) {
             ok = ok && tc::mbar_wait(bar_s + 8 * w, (uint32_t)n_mine & 1u, &s_abort);       // the last P V
             if (ok && *reinterpret_cast<volatile int *>(&s_any_bad)) nan_of(key_tile(w, n_mine - 1));
+        } else if (PAIR) {
+            // Outputs pass through the queries' place below.  A stream with tiles has seen its products, which wait for all queries; this one has
+            // waited for nothing, and every softmax warp puts rows into every warp's part (24 x 256 rows, 32 heads, one sequence with keys:
+            // one zero in 1300 was a piece of a query).
+            ok = tc::mbar_wait(bar_q, 0, &s_abort);
         }
         // output columns of this thread, and the factors of the streams' accumulators
         constexpr int COLS = PAIR ? DH : DH / 2;

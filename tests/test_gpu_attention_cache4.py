@@ -371,3 +371,31 @@ def test_a_layer_of_4_bit_operators_in_a_captured_graph():
         bound = (4 + 4 + 16) * 2.0 ** -23 * (np.abs(av) @ np.abs(wov).T)
         assert (np.abs(y.double().cpu().numpy() - want) <= bound + 2.0 ** -8 * (np.abs(want) + bound)).all()
     sfs.sfs_check_device_status()
+
+
+@pytest.mark.parametrize("batch,capacity,heads,kv,dim,n_q", PAIRS + [(4, 300, 32, 32, 128, 256), (24, 300, 32, 32, 128, 256), (24, 300, 32, 32, 64, 256)])
+def test_sequences_without_keys_among_pairs_of_row_tiles(batch, capacity, heads, kv, dim, n_q):
+    """Row tiles of a sequence of which no row sees a key, beside others that do, by queries that come from memory at a time of their own:
+    zeros every time, whichever warp has its queries last."""
+    c = Case(batch, capacity, heads, kv, dim, n_q, seed=17)
+    cache = sfs.Cache4(dev(R.pack(c.codes[0])), dev(c.scales[0]), dev(R.pack(c.codes[1])), dev(c.scales[1]), batch, capacity, kv, dim)
+    width, rows = heads * dim, batch * n_q
+    queries = [torch.randn((rows, width), generator=torch.Generator(device=DEV).manual_seed(i), device=DEV).to(torch.bfloat16) for i in range(1 + 2 ** 28 // (2 * rows * width))]
+    out = torch.empty((rows, width), dtype=torch.bfloat16, device=DEV)
+    empty = torch.ones(rows, dtype=torch.bool, device=DEV)
+    empty[n_q:2 * n_q] = False                              # the second sequence has its keys
+    wrong = torch.zeros((), dtype=torch.int64, device=DEV)
+    lengths = torch.zeros(batch, dtype=torch.int32, device=DEV)
+    lengths[1] = capacity
+    behind = torch.full((batch, n_q), 2 * capacity, dtype=torch.int32, device=DEV)         # windows behind every key
+    behind[1] = torch.arange(n_q, device=DEV) % capacity
+    for i in range(400):
+        q = queries[i % len(queries)]
+        out.fill_(77.0)
+        if i % 2:
+            sfs.sfs_attention_cache4(cache, q, width, out, width, heads, n_q, lengths)
+        else:
+            sfs.sfs_attention_cache4(cache, q, width, out, width, heads, n_q, None, behind, 50, 20, 0)
+        wrong += (out[empty].view(torch.int16) != 0).sum() + (out[~empty] == 77.0).all(1).sum()
+    sfs.sfs_check_device_status()
+    assert int(wrong) == 0
