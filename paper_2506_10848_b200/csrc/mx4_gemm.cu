@@ -308,7 +308,8 @@ int32_t launch(const Mx4Args &a, const Mx4Operands &x, cudaStream_t stream)
     const int n_steps = (a.blocks + kDepth / 32 - 1) / (kDepth / 32);
     const int stages = std::min(S::stages(BN > 128 || ctas <= gemm_num_sms() ? 1 : 2), std::max(2, (n_steps + a.splits - 1) / a.splits));
     const size_t shared = (size_t)S::shared(stages);
-    SFS_CUDA(allow_shared(linear_mx4_kernel<BN>, shared));
+    // what the instance takes at most, whatever this call takes: another thread's launch may come between this and ours
+    SFS_CUDA(allow_shared(linear_mx4_kernel<BN>, (size_t)S::shared(S::stages(1))));
     if (a.splits > 1) SFS_CUDA(launch_pdl_cluster(linear_mx4_kernel<BN>, a.splits, dim3((unsigned)ctas), dim3(kThreads), shared, stream, tl, tcol, a, stages, S::tmem_columns(stages)));
     else SFS_CUDA(launch_pdl(linear_mx4_kernel<BN>, dim3((unsigned)ctas), dim3(kThreads), shared, stream, tl, tcol, a, stages, S::tmem_columns(stages)));
     return SFS_OK;

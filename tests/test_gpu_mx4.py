@@ -303,6 +303,39 @@ def test_two_products_at_once():
         assert (np.abs(x.double().cpu().numpy() - av @ bv.T) <= bound).all()
 
 
+def test_two_host_threads_with_products_of_different_depth():
+    """Short and long rings of one kernel's instance, launched by two threads at once: neither takes shared memory from the other."""
+    import threading
+    cases = [(16, 128, 64), (16, 128, 24576), (300, 512, 512), (300, 512, 8192)]
+    for short, deep in (cases[:2], cases[2:]):
+        work = []
+        for m, n, k in (short, deep):
+            a, a_s, av = operand(m, k, m)
+            b, b_s, bv = operand(n, k, n)
+            work.append((m, n, k, a, a_s, b, b_s, torch.zeros((m, n), dtype=torch.float32, device=DEV), torch.cuda.Stream(), av @ bv.T, np.abs(av) @ np.abs(bv).T))
+        torch.cuda.synchronize()
+        failed, start = [], threading.Barrier(2)
+
+        def calls(m, n, k, a, a_s, b, b_s, out, stream, *_):
+            torch.cuda.set_device(0)
+            start.wait()
+            try:
+                for _ in range(4000):
+                    sfs.sfs_linear_mx4(a, k // 2, a_s, b, k // 2, b_s, out, n, m, n, k, 1, stream=stream.cuda_stream)
+            except sfs.SfsError as e:
+                failed.append(str(e))
+        threads = [threading.Thread(target=calls, args=w) for w in work]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        torch.cuda.synchronize()
+        sfs.sfs_check_device_status()
+        assert not failed, failed
+        for m, n, k, *_, out, _, want, size in work:
+            assert (np.abs(out.double().cpu().numpy() - want) <= ((k + 63) // 64 + 21) * 2.0 ** -23 * size).all()
+
+
 # ---- the cache ------------------------------------------------------------------------------------------------------------------------
 
 def new_cache(batch, capacity, heads, dim):
