@@ -494,5 +494,12 @@ extern "C" int32_t sfs_attention_cache4(const sfs_cache4 *cache, const void *d_q
         const int32_t rc = status_word_outside_captures((cudaStream_t)stream, &a.err);
         return rc != SFS_OK ? rc : attention_cache4_many(a, tokens, cache->head_dim, (cudaStream_t)stream);
     }
+    // The few-row kernel takes no status word, but the first call of either makes it: a caller who captures a call of many rows next does
+    // not know which of the two a shape gets.
+    if (device_status_word_if_any() == nullptr) {
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        SFS_CUDA(cudaStreamIsCapturing((cudaStream_t)stream, &capture));
+        if (capture == cudaStreamCaptureStatusNone) SFS_REQUIRE(device_status_word() != nullptr, SFS_ERR_OOM, "cannot allocate the device status word");
+    }
     return cache->head_dim == 128 ? launch_few<128>(a, (int)row_tiles, log_splits, (cudaStream_t)stream) : launch_few<64>(a, (int)row_tiles, log_splits, (cudaStream_t)stream);
 }

@@ -399,3 +399,40 @@ def test_sequences_without_keys_among_pairs_of_row_tiles(batch, capacity, heads,
         wrong += (out[empty].view(torch.int16) != 0).sum() + (out[~empty] == 77.0).all(1).sum()
     sfs.sfs_check_device_status()
     assert int(wrong) == 0
+
+
+FIRST_CALLS = """
+import torch
+from paper_2506_10848_b200 import binding as sfs
+B, cap, H, dim, n_q = 8, 500, 8, 128, 130
+z = lambda *s: torch.zeros(s, dtype=torch.uint8, device="cuda:0")
+cache = sfs.Cache4(z(B * cap, H, dim // 2), z(B * cap, H, dim // 32), z(B * cap, H, dim // 2), z(B * cap, H, dim // 32), B, cap, H, dim)
+q = torch.zeros((B * n_q, H * dim), dtype=torch.bfloat16, device="cuda:0")
+out = torch.full((B * n_q, H * dim), 7.0, dtype=torch.bfloat16, device="cuda:0")
+call = lambda rows: sfs.sfs_attention_cache4(cache, q, H * dim, out, H * dim, H, rows)
+if CAPTURED_FIRST:                                          # few rows take no status word: nothing to refuse
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(1)
+    graph.replay()
+call(1)                                                     # the first call outside a capture
+torch.cuda.synchronize()
+assert not out[:B].any() and (out[B:] == 7.0).all()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    call(n_q)
+graph.replay()
+torch.cuda.synchronize()
+assert not out.any()
+sfs.sfs_check_device_status()
+"""
+
+
+@pytest.mark.parametrize("captured_first", [False, True])
+def test_a_first_call_of_few_rows_serves_a_captured_call_of_many(captured_first):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS.replace("CAPTURED_FIRST", str(captured_first))], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
