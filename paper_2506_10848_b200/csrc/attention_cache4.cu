@@ -386,7 +386,7 @@ attention_cache4_few(Cache4Args a, int log_splits, int row_tiles)
     __syncthreads();
     auto finish = [&](int r, int pair, float x, float y, float den) {
         if (!s_live[r]) return;
-        const float inv = den == 0.f ? 0.f : kUnscale / den;
+        const float inv = den == 0.f && s_hi[r] <= s_lo[r] && s_first[r] <= 0 ? 0.f : kUnscale / den;     // (0 / 0, a NaN, for scores of -inf alone)
         const int qi = (row_tile * ROWS + r) / a.group, head = kv * a.group + (row_tile * ROWS + r) % a.group;
         *reinterpret_cast<uint32_t *>(a.out + ((long long)b * a.n_q + qi) * a.ld_out + (long long)head * DH + 2 * pair) = pack_bf16(x * inv, y * inv);
     };

@@ -189,6 +189,8 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
     auto tile_start = [&](int j) { return (j + tile0) * KT; };
     // where a row's query and output lie, without the head dimension's offset
     auto row_of = [&](int r, long long ld) { const int i = s_query[r]; return ((long long)b * a.n_q + i) * ld + (long long)(kv * a.group + row0 + r - i * a.group) * DH; };
+    // what a row's sum is multiplied by: zeros only where it sees no key (scores of -inf alone are 0 times infinity, a NaN)
+    auto inverse = [&](int r, float den) { return den == 0.f && s_hi[r] <= s_lo[r] && s_first[r] <= 0 ? 0.f : kUnscale / den; };
     auto token = [&](int v) { v = min(v, n_seen - 1); return v < first ? v : v + gap; };
     const int share = QT >> log_splits;                          // rows of a rank's part of the join
     const int n_streams = PAIR ? (n_tiles == 0 ? 0 : n_rows > QT ? 2 : 1) : min(n_tiles, 2);
@@ -508,7 +510,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
         float f0 = 0.f, f1 = 0.f;                           // PAIR: f0 of the own stream
         bool write = ok && !s_abort;
         if (PAIR) {
-            f0 = l == 0.f ? 0.f : kUnscale / l;
+            f0 = inverse(r, l);
         } else {
             s_max[w][row] = m; s_den[w][row] = l; s_nan[w][row] = nan_blocks;
             tc::tc_fence_before();
@@ -519,7 +521,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
             const float den = f0 * s_den[0][row] + f1 * s_den[1][row];
             nan_blocks = s_nan[0][row] | s_nan[1][row];
             if (splits == 1) {
-                const float inv = den == 0.f ? 0.f : kUnscale / den;
+                const float inv = inverse(row, den);
                 f0 *= inv; f1 *= inv;
             } else if (w == 0) s_ml[row] = make_float2(mm, den);
         }
@@ -601,7 +603,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
                     L += f * ml[k].y;
                     sum.x += f * o[k].x; sum.y += f * o[k].y; sum.z += f * o[k].z; sum.w += f * o[k].w;
                 }
-                const float inv = L == 0.f ? 0.f : kUnscale / L;
+                const float inv = inverse(row, L);
                 const __nv_bfloat162 x0 = __floats2bfloat162_rn(sum.x * inv, sum.y * inv), x1 = __floats2bfloat162_rn(sum.z * inv, sum.w * inv);
                 *reinterpret_cast<uint2 *>(a.out + row_of(row, a.ld_out) + col * 4) =
                     make_uint2(*reinterpret_cast<const uint32_t *>(&x0), *reinterpret_cast<const uint32_t *>(&x1));

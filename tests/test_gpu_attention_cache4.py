@@ -436,3 +436,20 @@ def test_a_first_call_of_few_rows_serves_a_captured_call_of_many(captured_first)
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST_CALLS.replace("CAPTURED_FIRST", str(captured_first))], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("batch,capacity,heads,kv,dim,n_q", [(2, 200, 2, 2, 128, 1), (1, 70, 1, 1, 64, 6), PAIRS[0], PAIRS[2], MANY[0], MANY[4], MANY[7]])
+def test_a_row_whose_scores_are_all_minus_infinity_is_not_one_that_sees_nothing(batch, capacity, heads, kv, dim, n_q):
+    """exp(-inf - -inf) is no number: such a row is NaN, as it is with one score of infinity, and only a row without keys is zeros."""
+    c = Case(batch, capacity, heads, kv, dim, n_q, seed=23)
+    c.codes[0][:] = 2 + c.codes[0] % 4                      # keys positive, so that no product with an infinity is NaN by itself
+    q = c.q.clone().abs()
+    q[n_q - 1, :dim] = float("-inf")                        # first head of the first sequence's last row
+    c.q = q
+    got = c.run()
+    assert np.isnan(got[n_q - 1, :dim]).all()
+    got[n_q - 1, :dim] = 0.0
+    assert np.isfinite(got).all()
+    lengths = np.full(batch, capacity)
+    lengths[0] = 0
+    assert (c.run(lengths=lengths)[:n_q] == 0).all()
