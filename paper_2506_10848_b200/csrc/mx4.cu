@@ -378,6 +378,31 @@ dequantize_short_kernel(const uint8_t *__restrict__ codes, long long ld_codes, c
 
 constexpr int kStoreRows = 8;                               // tokens of a CTA, at most
 
+// a warp's segment of one token's keys or values, `from` its row, into the cache at `slot`
+template <typename T, int U>
+__device__ __forceinline__ void store_segment(const T *from, bool wide, int slot, int seg, uint8_t *codes, uint8_t *scales, int width)
+{
+    const int lane = threadIdx.x & 31, half = lane >> 4, l = lane & 15, blocks = width / 32;
+    const int quad0 = seg * 2 * U + half, col0 = quad0 * 128 + l * 8;
+    Eight<T> x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (col0 + u * 256 >= width) x[u].zero();           // (a width is whole blocks: eight values are in or out together)
+        else if (wide) x[u].load(from + col0 + u * 256);
+        else x[u].load_some(from + col0 + u * 256, 8);
+    }
+    uint8_t *to = codes + (size_t)slot * (width / 2) + quad0 * 64 + l * 4, *s = scales + (size_t)slot * blocks + quad0 * 4 + (l >> 2);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        int c;
+        const uint32_t w = quantize8(x[u], mx4::kCacheLo, mx4::kCacheHi, c);
+        if (col0 + u * 256 < width) {
+            *reinterpret_cast<uint32_t *>(to + u * 128) = w;
+            if ((l & 3) == 0) s[u * 8] = (uint8_t)c;
+        }
+    }
+}
+
 template <typename T, int U>
 __global__ void __launch_bounds__(kThreads)
 cache_store_kernel(uint8_t *__restrict__ k_codes, uint8_t *__restrict__ k_scales, uint8_t *__restrict__ v_codes, uint8_t *__restrict__ v_scales,
@@ -410,31 +435,70 @@ cache_store_kernel(uint8_t *__restrict__ k_codes, uint8_t *__restrict__ k_scales
     const bool keys = blockIdx.y == 0;
     const T *src = keys ? k : v;
     const long long ld = keys ? ld_k : ld_v;
-    const bool wide = keys ? wide_k : wide_v;
-    uint8_t *codes = keys ? k_codes : v_codes, *scales = keys ? k_scales : v_scales;
-    const int lane = threadIdx.x & 31, half = lane >> 4, l = lane & 15, blocks = width / 32, quads = (blocks + 3) / 4;
-    for (Walk at(threadIdx.x / 32, kWarps, (quads + 2 * U - 1) / (2 * U)); at.row < cta_rows; at.next()) {
+    for (Walk at(threadIdx.x / 32, kWarps, ((width + 127) / 128 + 2 * U - 1) / (2 * U)); at.row < cta_rows; at.next()) {
         const int slot = s_slot[at.row];
-        if (slot < 0) continue;                             // (a warp works on one row)
-        const int quad0 = at.seg * 2 * U + half, col0 = quad0 * 128 + l * 8;
-        const T *from = src + (r0 + at.row) * ld + col0;
-        Eight<T> x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (col0 + u * 256 >= width) x[u].zero();       // (a width is whole blocks: eight values are in or out together)
-            else if (wide) x[u].load(from + u * 256);
-            else x[u].load_some(from + u * 256, 8);
+        if (slot >= 0)                                      // (a warp works on one row)
+            store_segment<T, U>(src + (r0 + at.row) * ld, keys ? wide_k : wide_v, slot, at.seg, keys ? k_codes : v_codes, keys ? k_scales : v_scales, width);
+    }
+}
+
+// Many rows with slots of their own.  Which of several rows with one slot is the last is found by looking at all later slots, so the work grows
+// with the square of the rows over the rows of a CTA: here up to 1024, keys and values together, whose slots lie in a table in shared memory
+// (open addressing, at most a quarter of it taken), where a later slot is mostly looked up in one or two reads.  262144 rows of 8 heads of 128:
+// 378 us, 267 without slots, 207 of bytes; 1048576: 2145, 828 of bytes, the rest lookups.
+constexpr int kManyRows = 1024, kManyThreads = 512;
+constexpr int kTableBits = 12, kTable = 1 << kTableBits;
+static_assert(kTable >= 4 * kManyRows, "a quarter");
+
+template <typename T, int U>
+__global__ void __launch_bounds__(kManyThreads, 2)
+cache_store_many_kernel(uint8_t *__restrict__ k_codes, uint8_t *__restrict__ k_scales, uint8_t *__restrict__ v_codes, uint8_t *__restrict__ v_scales,
+                        int n_slots, int width, const T *__restrict__ k, long long ld_k, const T *__restrict__ v, long long ld_v, int wide_k, int wide_v,
+                        const int32_t *__restrict__ slots, int n_rows, int cta_rows)
+{
+    pdl_wait();
+    pdl_trigger();
+    __shared__ int s_key[kTable], s_last[kTable];           // a slot, and the last of this CTA's rows that names it
+    __shared__ int s_slot[kManyRows];                       // a row's place in the table, then its slot, or -1 for a row that is left out
+    const int r0 = blockIdx.x * cta_rows, rows = min(cta_rows, n_rows - r0);
+    auto place = [](int slot) { return ((uint32_t)slot * 2654435769u) >> (32 - kTableBits); };
+    for (int i = threadIdx.x; i < kTable; i += kManyThreads) s_key[i] = s_last[i] = -1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows; i += kManyThreads) {
+        const int slot = slots[r0 + i];
+        int at = -1;
+        if ((unsigned)slot < (unsigned)n_slots) {
+            uint32_t h = place(slot);
+            for (int had; (had = atomicCAS(&s_key[h], -1, slot)) != -1 && had != slot;) h = (h + 1) & (kTable - 1);
+            atomicMax(&s_last[h], i);
+            at = (int)h;
         }
-        uint8_t *to = codes + (size_t)slot * (width / 2) + quad0 * 64 + l * 4, *s = scales + (size_t)slot * blocks + quad0 * 4 + (l >> 2);
+        s_slot[i] = at;
+    }
+    __syncthreads();
+    for (int r = r0 + rows + threadIdx.x; r < n_rows; r += 4 * kManyThreads) {
+        int later[4];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            int c;
-            const uint32_t w = quantize8(x[u], mx4::kCacheLo, mx4::kCacheHi, c);
-            if (col0 + u * 256 < width) {
-                *reinterpret_cast<uint32_t *>(to + u * 128) = w;
-                if ((l & 3) == 0) s[u * 8] = (uint8_t)c;
-            }
+        for (int e = 0; e < 4; ++e) later[e] = r + e * kManyThreads < n_rows ? slots[r + e * kManyThreads] : -1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if ((unsigned)later[e] >= (unsigned)n_slots) continue;
+            uint32_t h = place(later[e]);
+            for (int had; (had = s_key[h]) != -1; h = (h + 1) & (kTable - 1))
+                if (had == later[e]) { s_last[h] = kManyRows; break; }       // none of this CTA's rows
         }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows; i += kManyThreads) {
+        const int at = s_slot[i];
+        s_slot[i] = at >= 0 && s_last[at] == i ? s_key[at] : -1;
+    }
+    __syncthreads();
+    for (Walk at(threadIdx.x / 32, kManyThreads / 32, ((width + 127) / 128 + 2 * U - 1) / (2 * U)); at.row < 2 * rows; at.next()) {
+        const int i = at.row >> 1, slot = s_slot[i];
+        const bool keys = (at.row & 1) == 0;
+        if (slot >= 0)
+            store_segment<T, U>((keys ? k : v) + (r0 + i) * (keys ? ld_k : ld_v), keys ? wide_k : wide_v, slot, at.seg, keys ? k_codes : v_codes, keys ? k_scales : v_scales, width);
     }
 }
 
@@ -530,15 +594,19 @@ cudaError_t launch_dequantize(const void *codes, int64_t ld_codes, const void *s
     return launch_pdl(wide ? SFS_BY_PIECES(dequantize_kernel, u, true) : SFS_BY_PIECES(dequantize_kernel, u, false), grid, dim3(kThreads), 0, stream, (const uint8_t *)codes,
                       (long long)ld_codes, (const uint8_t *)scales, rows, cols, (T *)x, (long long)ldx, quads);
 }
+// Rows up to which every CTA of a few compares all later slots with its own, and beyond which a table in shared memory holds more rows' (us,
+// 8 heads of 128, scan / table; the calls' own 12 included): 2048 rows 18.5 / 19.1, 4096 23.5 / 21.4, 6144 31.3 / 23.2, 16384 98.8 / 33.1, 262144
+// 17700 / 378; 32 heads: 2048 24.6 / 28.5, 4096 34.7 / 33.8, 6144 45.8 / 42.0.
+constexpr int kFewSlots = 4096;
 template <typename T>
 cudaError_t launch_store(const sfs_cache4 &c, const void *k, int64_t ld_k, const void *v, int64_t ld_v, const int32_t *slots, int n_rows, cudaStream_t stream)
 {
-    const int width = c.n_kv_heads * c.head_dim, quads = (width + 127) / 128;
-    // few rows: one or two for a CTA, so that they spread over the machine
-    const int cta_rows = std::min(kStoreRows, std::max(1, n_rows / gemm_num_sms()));
-    const dim3 grid((unsigned)((n_rows + cta_rows - 1) / cta_rows), 2);
-    const int u = pieces(quads, true);
-    return launch_pdl(SFS_BY_PIECES(cache_store_kernel, u), grid, dim3(kThreads), 0, stream, (uint8_t *)c.k_codes,
+    const int width = c.n_kv_heads * c.head_dim, u = pieces((width + 127) / 128, true);
+    const bool many = slots && n_rows > kFewSlots;
+    // few rows: one or two for a CTA, so that they spread over the machine; many: two CTAs on an SM
+    const int cta_rows = many ? std::min(kManyRows, (n_rows + 2 * gemm_num_sms() - 1) / (2 * gemm_num_sms())) : std::min(kStoreRows, std::max(1, n_rows / gemm_num_sms()));
+    const dim3 grid((unsigned)((n_rows + cta_rows - 1) / cta_rows), many ? 1 : 2);
+    return launch_pdl(many ? SFS_BY_PIECES(cache_store_many_kernel, u) : SFS_BY_PIECES(cache_store_kernel, u), grid, dim3(many ? kManyThreads : kThreads), 0, stream, (uint8_t *)c.k_codes,
                       (uint8_t *)c.k_scales, (uint8_t *)c.v_codes, (uint8_t *)c.v_scales, c.batch * c.capacity, width, (const T *)k, (long long)ld_k,
                       (const T *)v, (long long)ld_v, (int)wide_rows(k, ld_k, sizeof(T)), (int)wide_rows(v, ld_v, sizeof(T)), slots, n_rows, cta_rows);
 }

@@ -405,6 +405,80 @@ def test_of_rows_with_one_slot_the_last_counts():
     assert (out.double().cpu().numpy() == R.values(*R.quantize(x[last], R.CACHE))).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,slots_n,kind", [(8192, 5000, "any"), (8193, 7, "few"), (20001, 30000, "any"), (20001, 40000, "once"), (30000, 1, "few"), (50000, 3000, "far"), (9000, 9000, "reversed"),
+                                            (310000, 400000, "any"), (12345, 100000, "crowded")])
+def test_the_last_of_many_rows_counts(n, slots_n, kind, dtype):
+    """More rows than the scan of small calls takes, beside guards: random slots with repetitions, few slots, none twice, repetitions far apart,
+    slots that share the head of a table, and slots outside of the cache."""
+    heads, dim = (1, 64) if dtype == "bf16" else (3, 64)
+    if n > 100000 and dtype == "f32":
+        heads = 1
+    width = heads * dim
+    rng = np.random.default_rng(n + slots_n)
+    if kind == "once":
+        slots = rng.permutation(slots_n)[:n]
+    elif kind == "reversed":
+        slots = np.arange(n)[::-1]
+    elif kind == "far":
+        slots = np.arange(n) * 17 % slots_n
+    elif kind == "crowded":                                 # multiples of 2^10, whose products with an odd number agree in the lower bits
+        slots = rng.integers(0, slots_n // 1024, size=n) * 1024
+    else:
+        slots = rng.integers(0, slots_n, size=n)
+    slots = slots.astype(np.int32)
+    out = rng.random(n) < 0.03
+    slots[out] = rng.choice([-1, slots_n, 2 ** 31 - 1, -2 ** 31, -7], size=int(out.sum()))
+    c = new_cache(1, slots_n, heads, dim)
+    t, x = as_input(np.random.default_rng(5).normal(size=(n, 2 * width)).astype(np.float32).astype(np.float64), dtype)
+    t = t.to(DEV)
+    sfs.sfs_cache4_store(c, t, 2 * width, t[:, width:], 2 * width, TYPES[dtype][1], dev(slots), n)
+    kept = np.flatnonzero((slots >= 0) & (slots < slots_n))
+    last = np.full(slots_n, -1)
+    last[slots[kept]] = kept                                # (numpy assigns in order: the last one stays)
+    assert all(last[s] == r for r, s in zip(kept[-50:], slots[kept[-50:]]) if (slots[r + 1:] != s).all())
+    named = np.flatnonzero(last >= 0)
+    for part, codes, scales in ((0, c._tensors[0], c._tensors[1]), (1, c._tensors[2], c._tensors[3])):
+        want_codes, want_scales = R.quantize(x[last[named], part * width:(part + 1) * width], R.CACHE)
+        codes, scales = codes.cpu().numpy().reshape(slots_n, -1), scales.cpu().numpy().reshape(slots_n, -1)
+        assert (codes[named] == R.pack(want_codes)).all() and (scales[named] == want_scales).all()
+        rest = np.setdiff1d(np.arange(slots_n), named)
+        assert (codes[rest] == GUARD).all() and (scales[rest] == GUARD).all()
+
+
+def test_many_rows_at_odd_places_and_of_many_heads():
+    heads, dim, n, slots_n = 13, 128, 8500, 9001
+    width = heads * dim
+    rng = np.random.default_rng(3)
+    slots = rng.integers(-3, slots_n, size=n).astype(np.int32)
+    c = new_cache(1, slots_n, heads, dim)
+    x = torch.randn((n, 2 * width + 3), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
+    t = x.to(DEV)
+    sfs.sfs_cache4_store(c, t, t.stride(0), t[:, width + 3:], t.stride(0), 0, dev(slots), n)
+    kept = np.flatnonzero(slots >= 0)
+    last = np.full(slots_n, -1)
+    last[slots[kept]] = kept
+    named = np.flatnonzero(last >= 0)
+    at, row = torch.from_numpy(named).to(torch.int32).to(DEV), torch.from_numpy(last[named]).to(DEV)
+    out = torch.zeros((2, named.size, width), dtype=torch.bfloat16, device=DEV)
+    sfs.sfs_cache4_load(c, at, named.size, out[0], width, out[1], width, 0)
+    # the same rows stored by a small call each: no slot twice, no table
+    ref, want = new_cache(1, 4096, heads, dim), torch.zeros((2, named.size, width), dtype=torch.bfloat16, device=DEV)
+    for i in range(0, named.size, 4096):
+        part = t[row[i:i + 4096]].contiguous()
+        sfs.sfs_cache4_store(ref, part, part.stride(0), part[:, width + 3:], part.stride(0), 0, None, part.shape[0])
+        sfs.sfs_cache4_load(ref, None, part.shape[0], want[0, i:], width, want[1, i:], width, 0)
+    assert torch.equal(out, want)
+
+
+def test_many_rows_of_which_none_is_in_the_cache():
+    c = new_cache(2, 10, 2, 64)
+    t = torch.ones((9000, 128), dtype=torch.bfloat16, device=DEV)
+    for slot in (-1, 20, 2 ** 31 - 1):
+        sfs.sfs_cache4_store(c, t, 128, t, 128, 0, torch.full((9000,), slot, dtype=torch.int32, device=DEV), 9000)
+    assert all((p == GUARD).all() for p in c._tensors)
+
+
 def test_slots_in_order_and_scales_at_the_ends_of_their_range():
     heads, dim = 1, 128
     x = np.ones((4, 128))
