@@ -703,6 +703,7 @@ int32_t sfs_cache4_store(const sfs_cache4 *cache, const void *d_k, int64_t ld_k,
     SFS_REQUIRE(d_k && d_v, SFS_ERR_INVALID_ARG, "cache4_store: NULL pointer");
     SFS_REQUIRE(in_dtype == SFS_LOGITS_BF16 || in_dtype == SFS_LOGITS_F32, SFS_ERR_INVALID_ARG, "cache4_store: type %d", in_dtype);
     SFS_REQUIRE(n_rows >= 0, SFS_ERR_INVALID_ARG, "cache4_store: n_rows %d", n_rows);
+    SFS_REQUIRE(n_rows <= (1 << 30), SFS_ERR_UNSUPPORTED, "cache4_store: more than 2^30 rows");
     SFS_REQUIRE(aligned_to(d_slots, 4), SFS_ERR_INVALID_ARG, "cache4_store: misaligned slots");
     if ((rc = check_rows("cache4_store", cache, d_k, ld_k, in_dtype)) != SFS_OK || (rc = check_rows("cache4_store", cache, d_v, ld_v, in_dtype)) != SFS_OK) return rc;
     if (n_rows == 0) return SFS_OK;
@@ -718,6 +719,7 @@ int32_t sfs_cache4_load(const sfs_cache4 *cache, const int32_t *d_slots, int32_t
     if (rc != SFS_OK) return rc;
     SFS_REQUIRE(out_dtype == SFS_LOGITS_BF16 || out_dtype == SFS_LOGITS_F32, SFS_ERR_INVALID_ARG, "cache4_load: type %d", out_dtype);
     SFS_REQUIRE(n_rows >= 0, SFS_ERR_INVALID_ARG, "cache4_load: n_rows %d", n_rows);
+    SFS_REQUIRE(n_rows <= (1 << 30), SFS_ERR_UNSUPPORTED, "cache4_load: more than 2^30 rows");
     SFS_REQUIRE(aligned_to(d_slots, 4), SFS_ERR_INVALID_ARG, "cache4_load: misaligned slots");
     if (d_k && (rc = check_rows("cache4_load", cache, d_k, ld_k, out_dtype)) != SFS_OK) return rc;
     if (d_v && (rc = check_rows("cache4_load", cache, d_v, ld_v, out_dtype)) != SFS_OK) return rc;

@@ -79,6 +79,11 @@ def test_sizes_that_would_pass_an_index():
     refused(sfs.ERR_UNSUPPORTED, sfs.sfs_attention_cache4, cache(batch=1, n_kv_heads=1), A, 1 << 22, A, 1 << 22, 65535, 1 << 16)
 
 
+def test_more_rows_than_an_index_of_them_holds():
+    refused(sfs.ERR_UNSUPPORTED, sfs.sfs_cache4_store, cache(), A, 128, A, 128, 0, A, (1 << 30) + 1)
+    refused(sfs.ERR_UNSUPPORTED, sfs.sfs_cache4_load, cache(), A, (1 << 30) + 1, A, 128, A, 128, 0)
+
+
 def test_tensors_of_the_host_are_refused():
     torch = pytest.importorskip("torch")
     t, b = torch.zeros(1 << 12, dtype=torch.bfloat16), torch.zeros(1 << 12, dtype=torch.uint8)
