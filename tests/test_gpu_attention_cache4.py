@@ -453,3 +453,35 @@ def test_a_row_whose_scores_are_all_minus_infinity_is_not_one_that_sees_nothing(
     lengths = np.full(batch, capacity)
     lengths[0] = 0
     assert (c.run(lengths=lengths)[:n_q] == 0).all()
+
+
+@pytest.mark.parametrize("n_q", [1, 100, 200])
+def test_sequences_behind_two_to_the_32_bytes_of_codes(n_q):
+    """The last sequence's codes begin at byte 2^32: single tokens, one row tile and pairs of them, keys and values at the end of every
+    sequence, those of the last one read back too."""
+    batch, capacity, kv, dim = 5, 1 << 17, 128, 128
+    if torch.cuda.mem_get_info()[0] < 20 * 2 ** 30:
+        pytest.skip("needs 20 GB of device memory")
+    slots, width, n = batch * capacity, kv * dim, 240
+    z = lambda w: torch.zeros((slots, kv, w), dtype=torch.uint8, device=DEV)  # noqa: E731
+    c = sfs.Cache4(z(dim // 2), z(dim // 32), z(dim // 2), z(dim // 32), batch, capacity, kv, dim)
+    assert (batch - 1) * capacity * kv * dim // 2 == 2 ** 32
+    x = torch.randn((n, 2 * width), generator=torch.Generator().manual_seed(0)).to(torch.bfloat16)
+    xd = x.to(DEV)
+    at = torch.arange(slots - n, slots, dtype=torch.int32, device=DEV)
+    sfs.sfs_cache4_store(c, xd, 2 * width, xd[:, width:], 2 * width, 0, at, n)
+    back = torch.zeros((2, n, width), dtype=torch.float32, device=DEV)
+    sfs.sfs_cache4_load(c, at, n, back[0], width, back[1], width, 1)
+    kq, vq = (R.values(*R.quantize(t.double().numpy(), R.CACHE)).reshape(n, kv, dim) for t in (x[:, :width], x[:, width:]))
+    assert (back[0].double().cpu().numpy() == kq.reshape(n, width)).all() and (back[1].double().cpu().numpy() == vq.reshape(n, width)).all()
+    q = torch.randn((batch * n_q, width), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    out = torch.full((batch * n_q, width), 77.0, dtype=torch.bfloat16, device=DEV)
+    left = n - n_q                                          # row i sees the keys i .. n - n_q + i of the last n
+    sfs.sfs_attention_cache4(c, q.to(DEV), width, out, width, kv, n_q, None, None, left, 0, 0)
+    sfs.sfs_check_device_status()
+    mask = np.stack([(np.arange(n) >= i) & (np.arange(n) <= n - n_q + i) for i in range(n_q)])
+    for h in (0, 77, 127):
+        want, bound = R.attention(q[-n_q:].double().numpy().reshape(n_q, kv, dim)[:, h], kq[:, h], vq[:, h], mask)
+        got = out[-n_q:].double().cpu().numpy().reshape(n_q, kv, dim)[:, h]
+        assert (np.abs(got - want) <= bound + 2.0 ** -8 * (np.abs(want) + bound)).all(), h
+    assert (out[:-n_q] == 0).all()                          # the other sequences hold zeros

@@ -119,6 +119,26 @@ def test_dequantize_gives_the_values(rows, cols, dtype):
         assert np.array_equal(got[:, :cols], want, equal_nan=True) and (got[:, cols:] == 77.0).all()
 
 
+def test_rows_behind_two_to_the_32_values():
+    """Rows that lie far apart: the last ones begin behind 2^32 elements of the matrix, and of what it becomes again."""
+    rows, ld = 20, 1 << 28
+    if torch.cuda.mem_get_info()[0] < 16 * 2 ** 30:
+        pytest.skip("needs 16 GB of device memory")
+    for cols in (40, 700):
+        t, x = as_input(matrix(rows, cols, cols), "bf16")
+        buf = torch.zeros((rows - 1) * ld + cols, dtype=torch.bfloat16, device=DEV)
+        view = buf.as_strided((rows, cols), (ld, 1))
+        view.copy_(t)
+        codes = torch.full((rows, sfs.mx4_code_bytes(cols)), GUARD, dtype=torch.uint8, device=DEV)
+        scales = torch.full((sfs.mx4_scale_bytes(rows, cols),), GUARD, dtype=torch.uint8, device=DEV)
+        sfs.sfs_mx4_quantize(buf, ld, 0, rows, cols, codes, codes.stride(0), scales)
+        want_codes, want_scales = R.quantize(x, R.MATRIX)
+        assert (codes.cpu().numpy() == R.pack(want_codes)).all() and (scales.cpu().numpy() == R.tile_scales(want_scales)).all()
+        view.fill_(77.0)
+        sfs.sfs_mx4_dequantize(codes, codes.stride(0), scales, rows, cols, buf, ld, 0)
+        assert np.array_equal(view.double().cpu().numpy(), R.values(want_codes, want_scales)[:, :cols], equal_nan=True)
+
+
 # ---- the product --------------------------------------------------------------------------------------------------------------------
 
 def operand(rows, cols, seed):
