@@ -65,11 +65,8 @@ template <int DH> struct Ring {
     static constexpr int kPart = kStep * DH / 2, kScales = 2 * kPart, kStage = kScales + 2 * kStep * 4, kBlocks = DH / 32;
     static constexpr int kKeyFactors = 2 * kStage, kValueFactors = kKeyFactors + kStep * kBlocks * 4, kWarp = kValueFactors + kStep * kBlocks * 2;
 };
-__device__ __forceinline__ void copy16(uint32_t smem, const void *global) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory"); }
 // four bytes, of which the first `bytes` are read and the others 0
 __device__ __forceinline__ void copy4(uint32_t smem, const void *global, int bytes) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem), "l"(global), "r"(bytes) : "memory"); }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 // Row i of a tile of 16 holds token token_of(i): the four tokens whose values a quarter of the lanes read together then lie in different banks
 // (with the chunks of a token's values rotated, see fetch).
 __device__ __forceinline__ int token_of(int i) { return (i & 8) | ((i & 3) << 1) | ((i >> 2) & 1); }

@@ -19,6 +19,12 @@ struct Cache4Args {
 #ifdef __CUDACC__
 __device__ __forceinline__ int cache4_length(const Cache4Args &a, int b) { return a.lengths ? min(max(a.lengths[b], 0), a.capacity) : a.capacity; }
 
+// 16 bytes on their way to shared memory, of which the first `bytes` are read and the others 0
+__device__ __forceinline__ void copy16(uint32_t smem, const void *global) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory"); }
+__device__ __forceinline__ void copy16(uint32_t smem, const void *global, int bytes) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(global), "r"(bytes) : "memory"); }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+
 // The keys that a query at position p sees: [0, first) and [lo, hi), first <= lo.
 struct Seen { int first, lo, hi; };
 __device__ __forceinline__ Seen cache4_seen(const Cache4Args &a, int length, long long p)

@@ -55,7 +55,6 @@ __device__ __forceinline__ void store_chunk(uint32_t smem, uint32_t x, uint32_t 
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
-__device__ __forceinline__ void copy16(uint32_t smem, const void *global, int bytes = 16) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(global), "r"(bytes) : "memory"); }
 // Loads that keep out of the first-level cache: next to this much shared memory it has 28 KB, in lines of 128 bytes, of which a token's
 // codes and scales would each take one for as long as they are under way.
 __device__ __forceinline__ uint4 load16(const uint8_t *p)
@@ -70,8 +69,6 @@ __device__ __forceinline__ uint32_t load1(const uint8_t *p)
     asm volatile("ld.global.L1::no_allocate.u8 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ float4 load_remote4(uint32_t cluster_addr)
 {

@@ -2,9 +2,10 @@
 //
 // A half-warp takes 128 consecutive values of a row, four blocks of 32: a lane holds 8 of them (16 bytes of bf16), a block's largest
 // magnitude is the maximum of the bit patterns over 4 lanes, so a NaN or an infinity shows in it, and each value is scaled by a power of
-// two (exact) and rounded once, by the conversion instruction.  A warp works on 1024 neighbouring columns, so that addresses are computed
-// once for four loads in flight: with one piece at a time, found anew, the instructions and not the memory set the pace (126464 x 4096 to
-// codes and back: 624 us, 485 so; 2.6 GB move, 5.4 TB/s of a measured copy rate of 6.57).
+// two (exact) and rounded once, by the conversion instruction.  A warp works on 256 to 1024 neighbouring columns (see pieces), so that addresses
+// are computed once for up to four loads in flight: with one piece at a time, found anew, the instructions and not the memory set the pace
+// (126464 x 4096 to codes and back: 624 us, 483 so; 2.6 GB move, 5.4 TB/s of a measured copy rate of 6.57).  Rows of at most 256 columns go
+// several to a warp, rows off 16-byte boundaries by words that shifts put together.
 #include "attention_cache4.cuh"
 #include "gemm.cuh"
 #include <algorithm>

@@ -5,7 +5,6 @@
 namespace sfs {
 namespace mx4 {
 
-constexpr int kBlock = 32;
 constexpr int kCacheLo = 65, kCacheHi = 192;               // scales of a cache: value * 2^-64 is a normal bf16, or exact below it
 
 #ifdef __CUDACC__

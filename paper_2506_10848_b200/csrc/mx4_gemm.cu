@@ -27,7 +27,6 @@ template <int BN> struct Shape {
     static constexpr int kScaleA = 2 * kScaleTile, kScaleB = kRowTiles * 2 * kScaleTile;
     static constexpr int kStage = kA + kB + kScaleA + kScaleB;
     static constexpr int kScaleCols = 8 + 8 * kRowTiles;    // tensor-memory columns of a stage's scales
-    static constexpr int kMaxStages = 210 * 1024 / kStage;
     // stages of the ring with one or two CTAs on an SM: a lone CTA needs twice as many, or the memory's latency sets its pace
     static constexpr int stages(int per_sm) { return (per_sm == 1 ? 210 * 1024 : 106 * 1024) / kStage; }
     // every stage has scales of its own in tensor memory: a copy may overtake an MMA issued before it, but not the stage's release
@@ -37,23 +36,6 @@ template <int BN> struct Shape {
     static_assert(2 * kStage >= 128 * BN * 4 || BN > 128, "partial sums fit the ring");
 };
 
-__device__ __forceinline__ void mma_mxf4_elect(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, uint32_t accumulate)
-{
-    asm volatile("{\n\t.reg .pred P, Q;\n\telect.sync _|P, 0xffffffff;\n\tsetp.ne.b32 Q, %6, 0;\n\t"
-                 "@P tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], Q;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate) : "memory");
-}
-// 32 rows of 16 bytes -> the same 32 lanes of all four quarters of tensor memory, four columns
-__device__ __forceinline__ void copy_scales_elect(uint32_t tmem, uint32_t smem)
-{
-    asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\t"
-                 "@P tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem), "l"(scale_desc(smem)) : "memory");
-}
-__device__ __forceinline__ void bulk_load(uint32_t smem, const void *global, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem), "l"(global), "r"(bytes), "r"(bar) : "memory");
-}
 __device__ __forceinline__ float load_remote(uint32_t cluster_addr)
 {
     float v;

@@ -30,6 +30,23 @@ __host__ __device__ constexpr uint32_t idesc_mxf4(int M, int N, int half) { retu
 #ifdef __CUDACC__
 // shared-memory descriptor of 32 rows of 16 bytes, a scale tile as tcgen05.cp reads it: 8 rows are 128 consecutive bytes
 __device__ __forceinline__ uint64_t scale_desc(uint32_t smem) { return (uint64_t)((smem >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46); }
+__device__ __forceinline__ void mma_mxf4_elect(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred P, Q;\n\telect.sync _|P, 0xffffffff;\n\tsetp.ne.b32 Q, %6, 0;\n\t"
+                 "@P tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], Q;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate) : "memory");
+}
+// 32 rows of 16 bytes -> the same 32 lanes of all four quarters of tensor memory, four columns
+__device__ __forceinline__ void copy_scales_elect(uint32_t tmem, uint32_t smem)
+{
+    asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\t"
+                 "@P tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem), "l"(scale_desc(smem)) : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t smem, const void *global, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem), "l"(global), "r"(bytes), "r"(bar) : "memory");
+}
 // eight bf16 values to an aligned place of which `n` belong to the row
 __device__ __forceinline__ void put_bf16(__nv_bfloat16 *at, const uint4 &v, int n)
 {

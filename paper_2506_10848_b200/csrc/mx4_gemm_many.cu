@@ -34,24 +34,6 @@ constexpr int kShared = kStages * kStage + kStoring * kPark + 1024 + kBarriers *
 constexpr uint32_t kTmem = 512;
 static_assert(BN + kStages * kScaleCols <= (int)kTmem && (kA + kB) % 1024 == 0 && kShared <= 227 * 1024, "tile");
 
-__device__ __forceinline__ void mma_elect(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, uint32_t accumulate)
-{
-    asm volatile("{\n\t.reg .pred P, Q;\n\telect.sync _|P, 0xffffffff;\n\tsetp.ne.b32 Q, %6, 0;\n\t"
-                 "@P tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], Q;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void copy_scales_elect(uint32_t tmem, uint32_t smem)
-{
-    asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\t"
-                 "@P tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem), "l"(scale_desc(smem)) : "memory");
-}
-
-__device__ __forceinline__ void bulk_load(uint32_t smem, const void *global, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem), "l"(global), "r"(bytes), "r"(bar) : "memory");
-}
-
 __global__ void __launch_bounds__(kThreads, 1)
 linear_mx4_many_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, Mx4Args a, int row_tiles, int num_tiles)
 {
@@ -137,7 +119,7 @@ linear_mx4_many_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_co
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (i < mmas)
-                            mma_elect(tmem, da + (uint64_t)(2 * i), db + (uint64_t)(2 * i), idesc_mxf4(128, BN, i & 1), ta + 4 * (i >> 1), tb + 8 * (i >> 1), (k | i) != 0 ? 1u : 0u);
+                            mma_mxf4_elect(tmem, da + (uint64_t)(2 * i), db + (uint64_t)(2 * i), idesc_mxf4(128, BN, i & 1), ta + 4 * (i >> 1), tb + 8 * (i >> 1), (k | i) != 0 ? 1u : 0u);
                     tc::mma_commit_elect(empty + 8 * s);
                     s = ns; ph = nph;
                 }
