@@ -485,3 +485,52 @@ def test_sequences_behind_two_to_the_32_bytes_of_codes(n_q):
         got = out[-n_q:].double().cpu().numpy().reshape(n_q, kv, dim)[:, h]
         assert (np.abs(got - want) <= bound + 2.0 ** -8 * (np.abs(want) + bound)).all(), h
     assert (out[:-n_q] == 0).all()                          # the other sequences hold zeros
+
+
+def test_attention_over_clusters_beside_products_on_other_streams():
+    """Row tiles of 64 features over clusters leave room on their SMs for products, which take tensor memory too: what runs beside changes
+    no bit of either, and all of it ends."""
+    att = []
+    for shape in ((1, 1100, 64, 2, 64, 60), (1, 4000, 12, 4, 64, 350), (1, 1100, 64, 2, 128, 60)):
+        batch, capacity, heads, kv, dim, n_q = shape
+        c = Case(*shape, seed=3)
+        cache = sfs.Cache4(dev(R.pack(c.codes[0])), dev(c.scales[0]), dev(R.pack(c.codes[1])), dev(c.scales[1]), batch, capacity, kv, dim)
+        att.append((cache, c.q.to(DEV), heads, n_q, heads * dim))
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    prod = []
+    for m, n, k in ((16, 4096, 12288), (9, 512, 8192), (128, 1024, 4096), (300, 2048, 512)):
+        ops = []
+        for r in (m, n):
+            x = torch.randn((r, k), generator=gen, device=DEV).to(torch.bfloat16)
+            codes, scales = torch.zeros((r, k // 2), dtype=torch.uint8, device=DEV), torch.zeros(sfs.mx4_scale_bytes(r, k), dtype=torch.uint8, device=DEV)
+            sfs.sfs_mx4_quantize(x, k, 0, r, k, codes, k // 2, scales)
+            ops.append((x, codes, scales))
+        prod.append((m, n, k, ops))
+
+    def attentions(outs):
+        for (cache, q, heads, n_q, width), out in zip(att, outs):
+            sfs.sfs_attention_cache4(cache, q, width, out, width, heads, n_q)
+
+    def products(outs):
+        for (m, n, k, ((_, a, a_s), (_, b, b_s))), out in zip(prod, outs):
+            sfs.sfs_linear_mx4(a, k // 2, a_s, b, k // 2, b_s, out, n, m, n, k, 1)
+
+    def plain(outs):
+        for (m, n, k, ((x, _, _), (y, _, _))), out in zip(prod, outs):
+            sfs.sfs_linear(x, k, y, k, out, n, m, n, k, 1)
+    new = {attentions: lambda: [torch.zeros_like(q) for _, q, *_ in att], products: lambda: [torch.zeros((m, n), device=DEV) for m, n, *_ in prod]}
+    new[plain] = new[products]
+    alone, beside = ({f: new[f]() for f in new} for _ in range(2))
+    for f in new:
+        f(alone[f])
+    torch.cuda.synchronize()
+    streams = {f: torch.cuda.Stream() for f in new}
+    for _ in range(60):
+        for f, stream in streams.items():
+            with torch.cuda.stream(stream):
+                f(beside[f])
+    torch.cuda.synchronize()
+    sfs.sfs_check_device_status()
+    for f in new:
+        for x, y in zip(alone[f], beside[f]):
+            assert torch.equal(x, y), f.__name__

@@ -491,6 +491,37 @@ def test_many_rows_at_odd_places_and_of_many_heads():
     assert torch.equal(out, want)
 
 
+def test_many_rows_in_a_captured_graph_on_another_stream():
+    """Slots and rows are read when the graph runs; two replays at once on caches of their own."""
+    heads, dim, n, slots_n = 2, 64, 7000, 3000
+    width = heads * dim
+    caches = [new_cache(1, slots_n, heads, dim) for _ in range(2)]
+    t, slots = torch.zeros((n, 2 * width), dtype=torch.bfloat16, device=DEV), torch.full((n,), -1, dtype=torch.int32, device=DEV)
+    graphs = []
+    for c in caches:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            sfs.sfs_cache4_store(c, t, 2 * width, t[:, width:], 2 * width, 0, slots, n)
+    rng = np.random.default_rng(1)
+    for _ in range(2):
+        x = torch.randn((n, 2 * width), generator=torch.Generator().manual_seed(int(rng.integers(100)))).to(torch.bfloat16)
+        at = rng.integers(-10, slots_n, size=n).astype(np.int32)
+        t.copy_(x)
+        slots.copy_(torch.from_numpy(at))
+        torch.cuda.synchronize()
+        for g in graphs:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                g.replay()
+        torch.cuda.synchronize()
+        kept = np.flatnonzero(at >= 0)
+        last = np.full(slots_n, -1)
+        last[at[kept]] = kept
+        named = np.flatnonzero(last >= 0)
+        want = R.pack(R.quantize(x.double().numpy()[last[named], width:], R.CACHE)[0])
+        for c in caches:
+            assert (c._tensors[2].cpu().numpy().reshape(slots_n, -1)[named] == want).all()
+
+
 def test_many_rows_of_which_none_is_in_the_cache():
     c = new_cache(2, 10, 2, 64)
     t = torch.ones((9000, 128), dtype=torch.bfloat16, device=DEV)
