@@ -389,7 +389,8 @@ int32_t sfs_cache4_load(const sfs_cache4 *cache, const int32_t *d_slots, int32_t
  *     j < length_b  and  (right < 0 or j <= p + right)  and  (left < 0 or j >= p - left or j < sinks).
  * left = right = -1 is the bidirectional attention of the mask predictor, right = 0 a causal one, left = window and sinks > 0 a sliding
  * window with first tokens that stay visible.  d_lengths int32 [batch] (clamped to [0, capacity]; NULL: capacity).  d_positions int32
- * [batch * n_q], a row with a negative position is not computed and its output left as it was; NULL: row i is at length_b - n_q + i.
+ * [batch * n_q], a row with a negative position is not computed and its output left as it was; NULL: row i is at length_b - n_q + i
+ * (and computed where that is negative too).
  * A row that sees no key gets zeros, one whose scores are all -infinity NaN.  Keys and values that no row sees may hold anything.  Scores, maxima, sums and outputs are fp32,
  * probabilities are rounded to bf16 for their product with the values.  No workspace; the first call on a device, whatever its sizes,
  * allocates its status word as sfs_linear_mx4's does: make one before any stream capture. */

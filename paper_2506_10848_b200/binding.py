@@ -209,6 +209,13 @@ def _here(*tensors):
     return out
 
 
+def _indexes(name, t, count):
+    """A tensor of slots, lengths or positions holds `count` int32 in a row: read as such, torch's usual int64 would name other tokens."""
+    if t is not None and not isinstance(t, int) and (t.element_size() != 4 or t.is_floating_point() or not t.is_contiguous() or t.numel() < count):
+        raise SfsError(ERR_INVALID_ARG, f"{name}: {count} contiguous int32 needed")
+    return t
+
+
 def sfs_mx4_quantize(x, ldx, in_dtype, rows, cols, codes, ld_codes, scales, stream=None):
     x, codes, scales = _here(x, codes, scales)
     _check(lib().sfs_mx4_quantize(x, ldx, in_dtype, rows, cols, codes, ld_codes, scales, _stream(stream)))
@@ -249,17 +256,17 @@ class Cache4(Structure):
 
 
 def sfs_cache4_store(cache, k, ld_k, v, ld_v, in_dtype, slots, n_rows, stream=None):
-    k, v, slots = cache._beside(k, v, slots)
+    k, v, slots = cache._beside(k, v, _indexes("slots", slots, n_rows))
     _check(lib().sfs_cache4_store(byref(cache), k, ld_k, v, ld_v, in_dtype, slots, n_rows, _stream(stream)))
 
 
 def sfs_cache4_load(cache, slots, n_rows, k, ld_k, v, ld_v, out_dtype, stream=None):
-    k, v, slots = cache._beside(k, v, slots)
+    k, v, slots = cache._beside(k, v, _indexes("slots", slots, n_rows))
     _check(lib().sfs_cache4_load(byref(cache), slots, n_rows, k, ld_k, v, ld_v, out_dtype, _stream(stream)))
 
 
 def sfs_attention_cache4(cache, q, ld_q, out, ld_out, n_heads, n_q, lengths=None, positions=None, left=-1, right=-1, sinks=0, stream=None):
-    q, out, lengths, positions = cache._beside(q, out, lengths, positions)
+    q, out, lengths, positions = cache._beside(q, out, _indexes("lengths", lengths, cache.batch), _indexes("positions", positions, cache.batch * n_q))
     _check(lib().sfs_attention_cache4(byref(cache), q, ld_q, out, ld_out, n_heads, n_q, lengths, positions, left, right, sinks, _stream(stream)))
 
 

@@ -128,6 +128,33 @@ def test_cache_of_another_device(monkeypatch):
         cache(**{**parts, "v_scales": OnDevice(1)})
 
 
+class Indexes(OnDevice):
+    """A CUDA tensor of integers, by what the binding asks of it."""
+    def __init__(self, size=4, floating=False, contiguous=True, count=16):
+        super().__init__(0)
+        self.size, self.floating, self.contiguous, self.count = size, floating, contiguous, count
+
+    def element_size(self): return self.size
+    def is_floating_point(self): return self.floating
+    def is_contiguous(self): return self.contiguous
+    def numel(self): return self.count
+
+
+@pytest.mark.parametrize("bad", [dict(size=8), dict(size=2), dict(floating=True), dict(contiguous=False), dict(count=3)])
+def test_indexes_of_another_type_or_too_few(bad, monkeypatch):
+    """Slots, lengths and positions are int32: of int64, torch's default, every second would be read as 0."""
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    c, t = cache(batch=4), OnDevice(0)
+    refused(sfs.ERR_INVALID_ARG, sfs.sfs_cache4_store, c, t, 128, t, 128, 0, Indexes(**bad), 4)
+    refused(sfs.ERR_INVALID_ARG, sfs.sfs_cache4_load, c, Indexes(**bad), 4, t, 128, t, 128, 0)
+    refused(sfs.ERR_INVALID_ARG, sfs.sfs_attention_cache4, c, t, 128, t, 128, 2, 1, lengths=Indexes(**bad))
+    refused(sfs.ERR_INVALID_ARG, sfs.sfs_attention_cache4, c, t, 128, t, 128, 2, 1, positions=Indexes(**bad))
+    # the right ones pass, to calls that have nothing to do
+    sfs.sfs_cache4_store(c, t, 128, t, 128, 0, Indexes(), 0, stream=0)
+    sfs.sfs_attention_cache4(c, t, 128, t, 128, 2, 0, Indexes(), Indexes(), stream=0)
+
+
 def test_nothing_to_do_is_no_error():
     sfs.sfs_cache4_store(cache(), A, 128, A, 128, 0, None, 0, stream=0)
     sfs.sfs_cache4_load(cache(), None, 0, A, 128, A, 128, 0, stream=0)
