@@ -390,10 +390,10 @@ int32_t sfs_cache4_load(const sfs_cache4 *cache, const int32_t *d_slots, int32_t
  * left = right = -1 is the bidirectional attention of the mask predictor, right = 0 a causal one, left = window and sinks > 0 a sliding
  * window with first tokens that stay visible.  d_lengths int32 [batch] (clamped to [0, capacity]; NULL: capacity).  d_positions int32
  * [batch * n_q], a row with a negative position is not computed and its output left as it was; NULL: row i is at length_b - n_q + i
- * (and computed where that is negative too).
- * A row that sees no key gets zeros, one whose scores are all -infinity NaN.  Keys and values that no row sees may hold anything.  Scores, maxima, sums and outputs are fp32,
- * probabilities are rounded to bf16 for their product with the values.  No workspace; the first call on a device, whatever its sizes,
- * allocates its status word as sfs_linear_mx4's does: make one before any stream capture. */
+ * (and computed where that is negative too).  A row that sees no key gets zeros, one whose scores are all -infinity NaN.  Keys and values
+ * that no row sees may hold anything.  Scores, maxima, sums and outputs are fp32, probabilities are rounded to bf16 for their product with
+ * the values.  No workspace; the first call on a device, whatever its sizes, allocates its status word as sfs_linear_mx4's does: make one
+ * before any stream capture. */
 int32_t sfs_attention_cache4(const sfs_cache4 *cache, const void *d_q, int64_t ld_q, void *d_out, int64_t ld_out, int32_t n_heads,
                              int32_t n_q, const int32_t *d_lengths, const int32_t *d_positions, int32_t left, int32_t right, int32_t sinks,
                              void *stream);

@@ -118,6 +118,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
     __shared__ float s_max[2][QT], s_den[2][QT];
     __shared__ float2 s_ml[QT];                             // with its maxima and denominators
     __shared__ uint32_t s_nan[2][QT];
+    __shared__ bool s_sees[ROWS];                           // rows that see some key
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int splits = 1 << log_splits, rank = blockIdx.x & (splits - 1);
@@ -175,6 +176,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
         }
         s_lo[r] = s.lo; s_hi[r] = s.hi; s_first[r] = live ? s.first : -1;      // -1: a row that is left as it was
         const bool some = s.hi > s.lo || s.first > 0;
+        s_sees[r] = some;
         const int f = warp_max_i32(s.first), l = warp_min_i32(some ? s.lo : 0x7FFFFFFF), h = warp_max_i32(s.hi);
         if (lane == 0) { atomicMax(&s_range[0], f); atomicMin(&s_range[1], l); atomicMax(&s_range[2], h); }
     }
@@ -188,7 +190,7 @@ attention_cache4_many_kernel(Cache4Args a, int log_splits, int row_tiles)
     // where a row's query and output lie, without the head dimension's offset
     auto row_of = [&](int r, long long ld) { const int i = s_query[r]; return ((long long)b * a.n_q + i) * ld + (long long)(kv * a.group + row0 + r - i * a.group) * DH; };
     // what a row's sum is multiplied by: zeros only where it sees no key (scores of -inf alone are 0 times infinity, a NaN)
-    auto inverse = [&](int r, float den) { return den == 0.f && s_hi[r] <= s_lo[r] && s_first[r] <= 0 ? 0.f : kUnscale / den; };
+    auto inverse = [&](int r, float den) { return den == 0.f && !s_sees[r] ? 0.f : kUnscale / den; };
     auto token = [&](int v) { v = min(v, n_seen - 1); return v < first ? v : v + gap; };
     const int share = QT >> log_splits;                          // rows of a rank's part of the join
     const int n_streams = PAIR ? (n_tiles == 0 ? 0 : n_rows > QT ? 2 : 1) : min(n_tiles, 2);
